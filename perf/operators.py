@@ -26,7 +26,7 @@ own = False
 PAGE = 16
 ITEM = {"bf16": 2, "fp8": 1, "int8": 1}
 QMAX = {"fp8": 448.0, "int8": 127.0}
-TINY = 2.0 ** -100           # the least scale of a page and head
+TINY = 2.0 ** -64            # the least scale of a page and head
 BASE = 10000.0               # of the rotation's frequencies
 
 
