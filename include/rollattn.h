@@ -34,11 +34,15 @@
  *                                               read, nor are slots >= L_b % 16 of a
  *                                               trajectory's last page
  *   k_scale,
- *   v_scale       [num_pages] float             FP8 pools only: element = code * scale
+ *   v_scale       [num_pages] float             FP8_E4M3 pools: element = code * scale
  *                                               of its physical page (per pool)
+ *                 [num_pages][Hkv] float        FP8_E4M3_HEAD and INT8_HEAD pools: element =
+ *                                               code * scale of its physical page and KV head
  * Supported element types: q/out F32 with kv F32 (D = 64 or 128); q/out BF16 with kv
- * BF16 or FP8_E4M3 (OCP E4M3, no infinities, max 448; D = 64 or 128; page scales must be
- * positive and finite, as absmax / 448 is).  Accumulation is float.  Hq / Hkv may be any positive integer (at most 256 for BF16 attn_append).
+ * BF16, FP8_E4M3 or FP8_E4M3_HEAD (OCP E4M3, no infinities, max 448) or INT8_HEAD (two's
+ * complement; D = 64 or 128).  Page scales must be positive and finite, as absmax / 448 is; those of the
+ * _HEAD types between 2^-64, the least that is written here, and 2^100.
+ * Accumulation is float.  Hq / Hkv may be any positive integer (at most 256 for BF16 attn_append).
  *
  * Execution.  Calls enqueue kernels on `hip_stream` (a hipStream_t passed as void*,
  * NULL = the default stream) and return without synchronising; nothing is copied to
@@ -62,7 +66,9 @@ extern "C" {
 typedef enum {
   ROLLATTN_F32 = 0,
   ROLLATTN_BF16 = 1,
-  ROLLATTN_FP8_E4M3 = 2
+  ROLLATTN_FP8_E4M3 = 2,
+  ROLLATTN_FP8_E4M3_HEAD = 3, /* pools only: E4M3 codes, a scale for each page and KV head */
+  ROLLATTN_INT8_HEAD = 4      /* pools only: 8-bit integers, a scale for each page and KV head */
 } rollattn_dtype;
 
 typedef enum {
@@ -70,7 +76,7 @@ typedef enum {
   ROLLATTN_EINVAL = -1,     /* null pointer, negative size, NULL descriptor            */
   ROLLATTN_ESHAPE = -2,     /* Hq % Hkv != 0, unsupported head_dim or page_size,
                                num_pages * Hkv >= 2^31                                 */
-  ROLLATTN_EDTYPE = -3,     /* unsupported q/kv type pair, FP8 without scales          */
+  ROLLATTN_EDTYPE = -3,     /* unsupported q/kv type pair, 8-bit pools without scales  */
   ROLLATTN_EALIGN = -4,     /* a device pointer is not 16-byte aligned                 */
   ROLLATTN_EWORKSPACE = -5, /* workspace smaller than rollattn_workspace_bytes()       */
   ROLLATTN_EHIP = -6,       /* a HIP call failed; text via rollattn_last_hip_error()   */
@@ -89,8 +95,9 @@ typedef struct {
   int32_t q_dtype;           /* rollattn_dtype of q and out                         */
   int32_t kv_dtype;          /* rollattn_dtype of both pools                        */
   float sm_scale;            /* softmax scale, e.g. 1/sqrt(D)                       */
-  const float *k_scale;      /* device [num_pages], FP8 only, else NULL             */
-  const float *v_scale;      /* device [num_pages], FP8 only, else NULL             */
+  const float *k_scale;      /* device [num_pages] (FP8_E4M3) or [num_pages][Hkv] (FP8_E4M3_HEAD,
+                                INT8_HEAD), else NULL                               */
+  const float *v_scale;      /* likewise                                            */
 } rollattn_desc;
 
 /* Decode step: one query token per trajectory at position L_b - 1 (Section 3.1, the
@@ -190,7 +197,7 @@ size_t rollattn_step_workspace_bytes(const rollattn_desc *desc, int32_t total_q)
  * is allowed and leaves the plain decode).  Tokens [0, S_j) are attended through the first member's
  * table row for all members (non-causal, all query rows of the group against the same K/V tiles on
  * the matrix cores), tokens [S_j, L_b) per trajectory as in attn_decode, and the two are merged with
- * the log-sum-exp rule.  BF16 queries only (BF16 or FP8 pools).  workspace of at least
+ * the log-sum-exp rule.  BF16 queries only (pools of any type).  workspace of at least
  * rollattn_shared_workspace_bytes(desc, group_size) bytes. */
 int attn_decode_shared(const rollattn_desc *desc, const void *q, const void *k_pages, const void *v_pages,
                        const int32_t *page_table, const int32_t *ctx_lens, int32_t group_size,
@@ -206,7 +213,7 @@ size_t rollattn_shared_workspace_bytes(const rollattn_desc *desc, int32_t group_
  *   k_new, v_new [total_q][Hkv][D], elements of desc->q_dtype (F32 or BF16), rows packed in batch
  *   order as q_chunk is; q_offsets [B+1] their exclusive scan; max_q_len >= max n_b (host): it sizes
  *   the launch, so rows of a chunk beyond an understated max_q_len would silently stay unwritten.
- *   Pools of the source type take the rows bit for bit.  FP8 pools (BF16 source) hold E4M3 codes
+ *   Pools of the source type take the rows bit for bit.  FP8_E4M3 pools (BF16 source) hold E4M3 codes
  *   times one float scale per physical page and pool, k_scale / v_scale [num_pages] (device, read
  *   and written here; desc->k_scale / v_scale are ignored).  Per page that receives new rows in
  *   slots [s0, s1): amax = largest |x| of those rows over all heads; s0 == 0: scale = amax / 448,
@@ -214,6 +221,10 @@ size_t rollattn_shared_workspace_bytes(const rollattn_desc *desc, int32_t group_
  *   codes in slots [0, s0) are replaced by enc(dec(code) * old / scale); new codes are
  *   enc(x / scale).  Every product and quotient is one float32 operation, enc rounds to nearest
  *   even after clamping to [-448, 448]: the result is defined bit for bit.
+ *   FP8_E4M3_HEAD and INT8_HEAD pools have a scale for each page and KV head, [num_pages][Hkv], which the same
+ *   rule gives from that head's rows alone, with three differences: INT8 has 127 for 448 and rounds to whole
+ *   numbers (nearest even); the least scale is 2^-64, also of rows that are all zero, so that a page that begins
+ *   with them still takes the scale of what follows.
  * A page written here must belong to exactly one trajectory of the batch (shared prefix pages are
  * complete and are never written again); inputs must be finite; B <= 65535.  Pool slots and scales
  * of pages that receive nothing are left untouched.  No workspace; total_q == 0 succeeds without a
@@ -222,6 +233,39 @@ int kv_write(const rollattn_desc *desc, const void *k_new, const void *v_new, co
              const int32_t *q_offsets, int32_t total_q, int32_t max_q_len, void *k_pages, void *v_pages,
              const int32_t *page_table, const int32_t *ctx_lens, float *k_scale, float *v_scale,
              void *hip_stream);
+
+/* The position rotation that kv_write_rope applies to queries and keys.  Of the first rot_dim dimensions of a head, pair j
+ * of rot_dim / 2 is (j, j + rot_dim / 2), or (2 j, 2 j + 1) where `interleaved` is set; the others stay as they are.
+ * A token at position p turns pair j to
+ *   lo' = lo * c - hi * s,  hi' = hi * c + lo * s     with c = cos_sin[p][j], s = cos_sin[p][rot_dim / 2 + j],
+ * each product and each sum one float32 operation.  With several axes (time, height, width of images and video) pair j takes
+ * its token's position on axis pair_axes[j]. */
+typedef struct {
+  const float *cos_sin;      /* device [num_positions][rot_dim]: the cosines of the pairs, then their sines */
+  const int32_t *positions;  /* device [num_axes][total_q], or NULL: a token's place in its context (num_axes 1);
+                                one outside [0, num_positions) takes the last row of the table       */
+  const uint8_t *pair_axes;  /* host [rot_dim / 2], each below num_axes; NULL: all 0                     */
+  int32_t num_positions;     /* rows of the table, >= 1                                                 */
+  int32_t rot_dim;           /* a multiple of 8, 8 .. head_dim                                          */
+  int32_t num_axes;          /* 1 .. 4; more than 1 needs positions                                     */
+  int32_t interleaved;
+  int64_t q_stride;          /* elements between the rows of consecutive tokens of q, k_new and v_new: */
+  int64_t k_stride;          /* multiples of 16 bytes, at least a row; 0: dense.  A projection's output */
+  int64_t v_stride;          /* that holds q, k and v of a token side by side can be passed as it is    */
+} rollattn_rope;
+
+/* kv_write with the position rotation on the way: in front of either attention call the new tokens' queries and keys are
+ * turned to their positions and K and V rows put into the pages, in one launch that reads q, k and v once.
+ *   q [total_q][Hq][D] and q_out [total_q][Hq][D] (dense): the rotated queries, rounded once to desc->q_dtype; both NULL:
+ *   keys and values alone.  q_out may be q where q is dense.  k_new, v_new, lengths, pools and scales as in kv_write; keys
+ *   go into the pools from the float32 results of the rotation, rounded once (pools of the source type) or quantised by the
+ *   rule of kv_write.
+ * max_q_len sizes the launch as in kv_write: it must not understate the longest chunk.  No workspace; total_q == 0
+ * succeeds without a launch. */
+int kv_write_rope(const rollattn_desc *desc, const rollattn_rope *rope, const void *q, const void *k_new, const void *v_new,
+                  const int32_t *q_lens, const int32_t *q_offsets, int32_t total_q, int32_t max_q_len, void *q_out, void *k_pages,
+                  void *v_pages, const int32_t *page_table, const int32_t *ctx_lens, float *k_scale, float *v_scale,
+                  void *hip_stream);
 
 /* Bytes of workspace either call needs for this descriptor; total_q is the number of
  * query rows (B for decode).  Depends on the descriptor only, never on device data, and

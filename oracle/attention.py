@@ -12,6 +12,8 @@ Storage formats (raw arrays, decoded here and nowhere else in this package):
               NaN, bias 7, subnormal step 2**-9, largest finite 448), to be
               multiplied by a per-page float32 scale (one scale per physical page
               of each pool, covering all KV heads and slots of the page)
+  "fp8_e4m3_head"  the same codes, "int8_head" numpy int8, each to be multiplied by a
+              float32 scale of its page and KV head, [num_pages, Hkv]
 
 Layouts: q [B or total_q, Hq, D]; pools [num_pages, Hkv, page_size, D];
 page_table [B, max_pages] int32; ctx_lens [B]; q_lens [B].
@@ -74,7 +76,12 @@ def decode_storage(raw: np.ndarray, dtype: str) -> np.ndarray:
         if a.dtype != np.uint16:
             raise TypeError("bf16 storage must be numpy uint16 bit patterns")
         return (a.astype(np.uint32) << np.uint32(16)).view(np.float32).astype(np.float64)
-    if dtype == "fp8_e4m3":
+    if dtype == "int8_head":
+        a = np.asarray(raw)
+        if a.dtype != np.int8:
+            raise TypeError("int8_head storage must be numpy int8")
+        return a.astype(np.float64)
+    if dtype in ("fp8_e4m3", "fp8_e4m3_head"):
         a = np.asarray(raw)
         if a.dtype != np.uint8:
             raise TypeError("fp8_e4m3 storage must be numpy uint8 codes")
@@ -103,6 +110,10 @@ def gather_tokens(pages, page_table, b, g, length, dtype, scale=None, raw=False)
         if scale is None:
             raise ValueError("fp8_e4m3 pools need a per-page scale")
         x = x * np.asarray(scale, dtype=np.float32).astype(np.float64)[phys][:, None]
+    if dtype in ("fp8_e4m3_head", "int8_head"):
+        if scale is None or np.shape(scale) != pages.shape[:2]:
+            raise ValueError(f"{dtype} pools need a scale for each page and head")
+        x = x * np.asarray(scale, dtype=np.float32).astype(np.float64)[phys, g][:, None]
     return x
 
 

@@ -17,10 +17,10 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librollattn.so")
 
-F32, BF16, FP8_E4M3 = 0, 1, 2
+F32, BF16, FP8_E4M3, FP8_E4M3_HEAD, INT8_HEAD = 0, 1, 2, 3, 4
 EXPORTS = (
     "attn_decode", "attn_decode_static", "rollattn_static_scratch_bytes", "rollattn_static_init", "attn_append", "attn_decode_lse", "attn_append_lse", "attn_merge", "attn_step", "attn_decode_shared",
-    "kv_write", "rollattn_workspace_bytes",
+    "kv_write", "kv_write_rope", "rollattn_workspace_bytes",
     "rollattn_step_workspace_bytes", "rollattn_shared_workspace_bytes", "rollattn_debug_gather",
     "rollattn_debug_check_inputs",
     "rollattn_debug_plan", "rollattn_plan_capacity", "rollattn_plan_workers", "rollattn_debug_read_plan", "rollattn_debug_set_decode_workers", "rollattn_debug_read_append_plan", "rollattn_append_plan_capacity", "rollattn_step_append_offset",
@@ -35,6 +35,14 @@ class Desc(ctypes.Structure):
         ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
         ("num_pages", ctypes.c_int64), ("q_dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
         ("sm_scale", ctypes.c_float), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [
+        ("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("pair_axes", ctypes.c_char_p),
+        ("num_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
     ]
 
 
@@ -87,6 +95,8 @@ def lib() -> ctypes.CDLL:
         l.rollattn_shared_workspace_bytes.restype = ctypes.c_size_t
         l.kv_write.argtypes = [dp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         l.kv_write.restype = ctypes.c_int
+        l.kv_write_rope.argtypes = [dp, ctypes.POINTER(Rope), vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        l.kv_write_rope.restype = ctypes.c_int
         l.rollattn_workspace_bytes.argtypes = [dp, i32]
         l.rollattn_workspace_bytes.restype = ctypes.c_size_t
         l.rollattn_debug_gather.argtypes = [dp, vp, vp, vp, i32, i32, vp, vp]
@@ -128,7 +138,7 @@ def lib() -> ctypes.CDLL:
 # What follows runs on the host in front of every launch, and the smallest calls are no longer than it (a decode step of
 # four short float32 contexts: 4 us on the GPU), so it stays short: addresses as plain integers, the descriptor's fields by
 # position, the current stream's handle without a stream object.
-_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.uint8: FP8_E4M3, torch.float8_e4m3fn: FP8_E4M3}
+_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.uint8: FP8_E4M3, torch.float8_e4m3fn: FP8_E4M3, torch.int8: INT8_HEAD}
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -136,6 +146,19 @@ def _dtype_code(t: torch.Tensor) -> int:
     if code is None:
         raise TypeError(f"unsupported element type {t.dtype}")
     return code
+
+
+def _kv_code(pages: torch.Tensor, k_scale, v_scale) -> int:
+    """The pools' type: E4M3 codes have a scale for each page, or with scales [num_pages, Hkv] one for each page and KV head,
+    as int8 ones always do."""
+    code = _dtype_code(pages)
+    if code < FP8_E4M3 or k_scale is None or v_scale is None:
+        return code
+    if code == FP8_E4M3 and k_scale.dim() == 1:
+        return code
+    if k_scale.shape != pages.shape[:2] or v_scale.shape != pages.shape[:2]:
+        raise ValueError("scales of each page and KV head are [num_pages, Hkv]")
+    return INT8_HEAD if code == INT8_HEAD else FP8_E4M3_HEAD
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -153,7 +176,7 @@ def make_desc(q, k_pages, page_table, *, sm_scale, k_scale=None, v_scale=None, b
     table = page_table.shape
     # in the order of Desc._fields_
     return Desc(table[0] if batch is None else int(batch), q.shape[1], hkv, d, page_size, table[1], num_pages, _dtype_code(q),
-                _dtype_code(k_pages), float(sm_scale), _ptr(k_scale), _ptr(v_scale))
+                _kv_code(k_pages, k_scale, v_scale), float(sm_scale), _ptr(k_scale), _ptr(v_scale))
 
 
 def workspace_bytes(desc: Desc, total_q: int) -> int:
@@ -320,12 +343,65 @@ def kv_write(k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_
     """Puts the new tokens' K / V rows (packed by trajectory, [total_q, Hkv, D]) into the pools in place;
     FP8 pools also get their page scales updated in place."""
     _check_contig(k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, k_scale, v_scale)
-    desc = make_desc(k_new, k_pages, page_table, sm_scale=1.0)
+    desc = make_desc(k_new, k_pages, page_table, sm_scale=1.0, k_scale=k_scale, v_scale=v_scale)
     rc = lib().kv_write(ctypes.byref(desc), _ptr(k_new), _ptr(v_new), _ptr(q_lens), _ptr(q_offsets), int(k_new.shape[0]),
                         int(max_q_len), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(ctx_lens), _ptr(k_scale),
                         _ptr(v_scale), _stream(stream))
     if rc:
         raise RollattnError(rc, "kv_write")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements between the rows of consecutive tokens; a token's heads lie side by side."""
+    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        if t.numel():
+            raise ValueError("the heads of a token lie side by side")
+        return t.shape[1] * t.shape[2]
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+
+
+def kv_write_rope(q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, cos_sin, max_q_len,
+                  positions=None, pair_axes=None, interleaved=False, k_scale=None, v_scale=None, q_out=None, stream=None):
+    """kv_write with the position rotation on the way: returns the rotated queries (None where q is None).
+
+    q [total_q, Hq, D], k_new and v_new [total_q, Hkv, D] may be parts of one projection's output (any stride between tokens
+    that is a multiple of 16 bytes).  cos_sin [num_positions, rot_dim] float32: the cosines of the rot_dim / 2 pairs, then
+    their sines; pair j is (j, j + rot_dim / 2), or (2 j, 2 j + 1) with `interleaved`.  positions [axes, total_q] int32 (or
+    [total_q]; None: a token's place in its context), pair_axes: the axis of each pair, a sequence of rot_dim / 2 whole numbers."""
+    _check_contig(q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, cos_sin, positions, k_scale, v_scale, q_out)
+    total_q, hkv, d = k_new.shape
+    if v_new.shape != k_new.shape or k_new.shape[1:] != (k_pages.shape[1], k_pages.shape[3]) or v_pages.shape != k_pages.shape:
+        raise ValueError("k_new and v_new are [total_q, Hkv, D] rows of the pools")
+    if q is not None and (q.shape[0] != total_q or q.shape[2] != d):
+        raise ValueError("q is [total_q, Hq, D]")
+    if v_new.dtype != k_new.dtype or (q is not None and q.dtype != k_new.dtype) or v_pages.dtype != k_pages.dtype:
+        raise TypeError("q, k_new and v_new are of one type, and so are the pools")
+    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] % 2:
+        raise ValueError("cos_sin is [num_positions, rot_dim] float32")
+    axes = 1
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.shape[-1] != total_q or positions.dim() not in (1, 2):
+            raise ValueError("positions is [axes, total_q] int32")
+        axes = positions.shape[0] if positions.dim() == 2 else 1
+    if pair_axes is not None:
+        pair_axes = bytes(pair_axes)
+        if len(pair_axes) != cos_sin.shape[1] // 2:
+            raise ValueError("pair_axes has an axis for each pair")
+    elif axes > 1:
+        raise ValueError("several axes need pair_axes")
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if q_out is not None and (q is None or q_out.shape != q.shape or q_out.dtype != q.dtype):
+        raise ValueError("q_out takes the rotated q")
+    desc = make_desc(k_new if q is None else q, k_pages, page_table, sm_scale=1.0, k_scale=k_scale, v_scale=v_scale)
+    rope = Rope(_ptr(cos_sin), _ptr(positions), pair_axes, cos_sin.shape[0], cos_sin.shape[1], axes, 1 if interleaved else 0,
+                0 if q is None else _row_stride(q), _row_stride(k_new), _row_stride(v_new))
+    rc = lib().kv_write_rope(ctypes.byref(desc), ctypes.byref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_lens), _ptr(q_offsets),
+                             total_q, int(max_q_len), _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(ctx_lens),
+                             _ptr(k_scale), _ptr(v_scale), _stream(stream))
+    if rc:
+        raise RollattnError(rc, "kv_write_rope")
+    return q_out
 
 
 def debug_gather(pages, page_table, ctx_lens, b, kv_head, length, stream=None) -> torch.Tensor:

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librollattn.so")
 PEAKS_LIB = os.path.join(HERE, "libbench_peaks.so")      # the benchmark's two peak microbenchmarks, not part of the library
-SOURCES = ["api.cpp", "plan.hip", "attn_f32.hip", "decode_mfma.hip", "combine.hip", "append_mfma.hip", "kv_write.hip", "shared_prefix.hip"]
+SOURCES = ["append_mfma.hip", "append_mfma.hip:head", "decode_mfma.hip", "api.cpp", "plan.hip", "attn_f32.hip", "combine.hip", "kv_write.hip", "kv_write_rope.hip", "shared_prefix.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wall", "-Wno-unused-function"]
@@ -22,12 +22,15 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
 # Kernels that wait for their asynchronous loads by count: a register spill to scratch memory would use the same
 # counter behind the compiler's back, so their build fails if the compiler reports any scratch.
 NO_SCRATCH = {"append_mfma.hip"}
+# A source that makes several objects: what the part of its name behind the colon sets.
+PARTS = {"head": ["-DROLLATTN_HEAD_SCALES"]}
 
 
 def _compile(src: str, extra) -> str:
-    obj = os.path.join(OBJ, src + ".o")
+    src, _, part = src.partition(":")
+    obj = os.path.join(OBJ, src + (f".{part}" if part else "") + ".o")
     check = ["-Rpass-analysis=kernel-resource-usage"] if src in NO_SCRATCH else []
-    cmd = ["hipcc", *FLAGS, *extra, *check, "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = ["hipcc", *FLAGS, *PARTS.get(part, []), *extra, *check, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if check and r.returncode == 0:
         sizes = [int(m) for m in re.findall(r"ScratchSize \[bytes/lane\]: (\d+)", r.stderr)]

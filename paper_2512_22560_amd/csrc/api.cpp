@@ -43,6 +43,17 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 int dtype_bytes(int dt) { return dt == ROLLATTN_F32 ? 4 : dt == ROLLATTN_BF16 ? 2 : 1; }
 
+bool has_codes(const rollattn_desc& d) { return d.kv_dtype != ROLLATTN_F32 && d.kv_dtype != ROLLATTN_BF16; }   // one byte and scales
+
+KvKind kv_kind(const rollattn_desc& d) {
+  switch (d.kv_dtype) {
+    case ROLLATTN_FP8_E4M3: return kKvFp8;
+    case ROLLATTN_FP8_E4M3_HEAD: return kKvFp8Head;
+    case ROLLATTN_INT8_HEAD: return kKvInt8Head;
+    default: return kKvBf16;
+  }
+}
+
 // Descriptor checks shared by every entry point.
 int check_desc(const rollattn_desc* d, bool need_scales = true) {
   if (!d) return ROLLATTN_EINVAL;
@@ -52,9 +63,9 @@ int check_desc(const rollattn_desc* d, bool need_scales = true) {
   if (d->page_size != kPageSize) return ROLLATTN_ESHAPE;
   if (d->num_pages * (int64_t)d->num_kv_heads > INT32_MAX) return ROLLATTN_ESHAPE;   // (page, head) tiles are counted in 32 bits
   const bool f32 = d->q_dtype == ROLLATTN_F32 && d->kv_dtype == ROLLATTN_F32;
-  const bool bf = d->q_dtype == ROLLATTN_BF16 && (d->kv_dtype == ROLLATTN_BF16 || d->kv_dtype == ROLLATTN_FP8_E4M3);
+  const bool bf = d->q_dtype == ROLLATTN_BF16 && d->kv_dtype >= ROLLATTN_BF16 && d->kv_dtype <= ROLLATTN_INT8_HEAD;
   if (!f32 && !bf) return ROLLATTN_EDTYPE;
-  if (d->kv_dtype == ROLLATTN_FP8_E4M3 && need_scales) {
+  if (has_codes(*d) && need_scales) {
     if (!d->k_scale || !d->v_scale) return ROLLATTN_EDTYPE;
     if (!aligned16(d->k_scale) || !aligned16(d->v_scale)) return ROLLATTN_EALIGN;
   }
@@ -317,7 +328,7 @@ static int decode_prepare(const rollattn_desc* desc, const void* q, const void* 
   d.workers = plan_workers(w); d.slots = w.workers;
   // (whole rows instead, where the plan says so: not where the number of workers is forced)
   const int n_ht = w.rows_per_b / desc->num_kv_heads;
-  d.whole_busy = (desc->kv_dtype == ROLLATTN_FP8_E4M3 ? kWholeBusyFp8 : kWholeBusy) * n_ht;   // (several rows read the same K and V)
+  d.whole_busy = (has_codes(*desc) ? kWholeBusyFp8 : kWholeBusy) * n_ht;   // (several rows read the same K and V)
   d.whole_gain = kWholeGain * (a.group * desc->head_dim) / (float)(n_ht * kMfmaHeadTile * 128);   // (as large as its partials)
   a.whole_rows = desc->q_dtype != ROLLATTN_F32 && d.workers == w.workers;
   if (desc->q_dtype != ROLLATTN_F32) d.page_table = page_table;
@@ -335,7 +346,7 @@ static int decode_launch(const rollattn_desc* desc, const DecodeArgs& a, hipStre
     if (f32) {
       e = launch_decode_f32(a, desc->head_dim, kF32DecodeWgs, s);
     } else {
-      e = launch_decode_mfma(a, desc->head_dim, desc->kv_dtype == ROLLATTN_FP8_E4M3, a.whole_rows && desc->head_dim == 64 ? kMfmaDecodeWgsD64 : kMfmaDecodeWgs, s);
+      e = launch_decode_mfma(a, desc->head_dim, kv_kind(*desc), a.whole_rows && desc->head_dim == 64 ? kMfmaDecodeWgsD64 : kMfmaDecodeWgs, s);
     }
     prof.stop();
   }
@@ -440,7 +451,7 @@ struct BlockTime {
   float alone, full;
 };
 static BlockTime block_time(const rollattn_desc& d, bool half_tiles) {
-  const bool fp8 = d.kv_dtype == ROLLATTN_FP8_E4M3;
+  const bool fp8 = has_codes(d);
   if (d.head_dim == 128) return half_tiles ? (fp8 ? BlockTime{0.85f, 1.10f} : BlockTime{0.76f, 1.42f}) : (fp8 ? BlockTime{1.28f, 1.82f} : BlockTime{1.05f, 1.75f});
   return half_tiles ? (fp8 ? BlockTime{0.74f, 0.79f} : BlockTime{0.60f, 0.82f}) : (fp8 ? BlockTime{1.21f, 1.32f} : BlockTime{0.89f, 1.07f});
 }
@@ -554,7 +565,7 @@ static int append_launch(const rollattn_desc* desc, AppendCall& call, hipStream_
     const int grid = (int)std::min<int64_t>(grid64, INT32_MAX);
     int dev = -1;
     if (prof.on && hipGetDevice(&dev) == hipSuccess && dev == g_clock_dev) a.clock_sums = g_clock_sums;
-    e = launch_append_mfma(a, desc->head_dim, desc->kv_dtype == ROLLATTN_FP8_E4M3, call.half_tiles, grid, s);
+    e = launch_append_mfma(a, desc->head_dim, kv_kind(*desc), call.half_tiles, grid, s);
     prof.stop();
   }
   if (e != hipSuccess) return fail_hip(e);
@@ -766,18 +777,79 @@ int kv_write(const rollattn_desc* desc, const void* k_new, const void* v_new, co
   if (rc) return rc;
   if (total_q < 0 || max_q_len < 0) return ROLLATTN_EINVAL;
   if (desc->batch == 0 || total_q == 0) return ROLLATTN_OK;
-  const bool fp8 = desc->kv_dtype == ROLLATTN_FP8_E4M3;
+  const bool codes = has_codes(*desc);
   if (!k_new || !v_new || !q_lens || !q_offsets || !k_pages || !v_pages || !page_table || !ctx_lens) return ROLLATTN_EINVAL;
-  if (fp8 && (!k_scale || !v_scale)) return ROLLATTN_EDTYPE;
+  if (codes && (!k_scale || !v_scale)) return ROLLATTN_EDTYPE;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(q_lens) || !aligned16(q_offsets) || !aligned16(k_pages) ||
-      !aligned16(v_pages) || !aligned16(page_table) || !aligned16(ctx_lens) || (fp8 && (!aligned16(k_scale) || !aligned16(v_scale))))
+      !aligned16(v_pages) || !aligned16(page_table) || !aligned16(ctx_lens) || (codes && (!aligned16(k_scale) || !aligned16(v_scale))))
     return ROLLATTN_EALIGN;
   if (desc->batch > 65535) return ROLLATTN_ESHAPE;     // one grid row per trajectory
   hipStream_t s = (hipStream_t)hip_stream;
   ProfileScope prof(s);
+  const KvKind kv = kv_kind(*desc);
+  if (kv_has_head_scales(kv)) {
+    RopeWriteArgs a{};
+    a.k_new = k_new; a.v_new = v_new; a.k_pages = k_pages; a.v_pages = v_pages;
+    a.q_lens = q_lens; a.q_offsets = q_offsets; a.page_table = page_table; a.ctx_lens = ctx_lens;
+    a.k_scale = k_scale; a.v_scale = v_scale;
+    a.k_stride = a.v_stride = (int64_t)desc->num_kv_heads * desc->head_dim;
+    a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq; a.total_q = total_q;
+    const hipError_t e = launch_kv_write_rope(a, desc->batch, max_q_len, desc->head_dim, 2, kv, s);
+    prof.stop();
+    return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
+  }
   const hipError_t e = launch_kv_write(k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, k_scale,
                                        v_scale, desc->batch, desc->num_kv_heads, desc->max_pages_per_seq, max_q_len,
-                                       desc->head_dim, desc->q_dtype == ROLLATTN_F32 ? 4 : 2, fp8, s);
+                                       desc->head_dim, desc->q_dtype == ROLLATTN_F32 ? 4 : 2, codes, s);
+  prof.stop();
+  if (e != hipSuccess) return fail_hip(e);
+  return ROLLATTN_OK;
+}
+
+int kv_write_rope(const rollattn_desc* desc, const rollattn_rope* rope, const void* q, const void* k_new, const void* v_new,
+                  const int32_t* q_lens, const int32_t* q_offsets, int32_t total_q, int32_t max_q_len, void* q_out, void* k_pages,
+                  void* v_pages, const int32_t* page_table, const int32_t* ctx_lens, float* k_scale, float* v_scale,
+                  void* hip_stream) {
+  int rc = check_desc(desc, /*need_scales=*/false);
+  if (rc) return rc;
+  if (!rope || total_q < 0 || max_q_len < 0 || rope->num_positions < 1) return ROLLATTN_EINVAL;
+  if (rope->rot_dim < 8 || rope->rot_dim > desc->head_dim || rope->rot_dim % 8) return ROLLATTN_ESHAPE;
+  if (rope->num_axes < 1 || rope->num_axes > 4) return ROLLATTN_ESHAPE;
+  if (rope->num_axes > 1 && !rope->positions) return ROLLATTN_EINVAL;
+  const int64_t kv_row = (int64_t)desc->num_kv_heads * desc->head_dim, q_row = (int64_t)desc->num_q_heads * desc->head_dim;
+  const int src_bytes = desc->q_dtype == ROLLATTN_F32 ? 4 : 2;
+  RopeWriteArgs a{};
+  a.q_stride = rope->q_stride ? rope->q_stride : q_row;
+  a.k_stride = rope->k_stride ? rope->k_stride : kv_row;
+  a.v_stride = rope->v_stride ? rope->v_stride : kv_row;
+  if (a.q_stride < q_row || a.k_stride < kv_row || a.v_stride < kv_row) return ROLLATTN_ESHAPE;
+  if ((a.q_stride | a.k_stride | a.v_stride) * src_bytes % 16) return ROLLATTN_EALIGN;
+  if (rope->pair_axes) {
+    for (int j = 0; j < rope->rot_dim / 2; ++j) {
+      if (rope->pair_axes[j] >= rope->num_axes) return ROLLATTN_EINVAL;
+      a.pair_axes[j / 16] |= (uint32_t)rope->pair_axes[j] << (j % 16 * 2);
+    }
+  }
+  if (desc->batch == 0 || total_q == 0) return ROLLATTN_OK;
+  const bool codes = has_codes(*desc);
+  if (!k_new || !v_new || !q_lens || !q_offsets || !k_pages || !v_pages || !page_table || !ctx_lens || !rope->cos_sin) return ROLLATTN_EINVAL;
+  if (!q != !q_out) return ROLLATTN_EINVAL;
+  if (q && q == q_out && a.q_stride != q_row) return ROLLATTN_EINVAL;      // (in place: rows must lie where they are read)
+  if (codes && (!k_scale || !v_scale)) return ROLLATTN_EDTYPE;
+  if (!aligned16(q) || !aligned16(q_out) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_lens) || !aligned16(q_offsets) ||
+      !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(page_table) || !aligned16(ctx_lens) || !aligned16(rope->cos_sin) ||
+      !aligned16(rope->positions) || (codes && (!aligned16(k_scale) || !aligned16(v_scale))))
+    return ROLLATTN_EALIGN;
+  if (desc->batch > 65535) return ROLLATTN_ESHAPE;     // one grid row per trajectory
+  a.q = q; a.k_new = k_new; a.v_new = v_new; a.q_out = q_out; a.k_pages = k_pages; a.v_pages = v_pages;
+  a.q_lens = q_lens; a.q_offsets = q_offsets; a.page_table = page_table; a.ctx_lens = ctx_lens;
+  a.k_scale = k_scale; a.v_scale = v_scale;
+  a.cos_sin = rope->cos_sin; a.positions = rope->positions;
+  a.hq = desc->num_q_heads; a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq; a.total_q = total_q;
+  a.rot_dim = rope->rot_dim; a.num_positions = rope->num_positions; a.interleaved = rope->interleaved != 0;
+  hipStream_t s = (hipStream_t)hip_stream;
+  ProfileScope prof(s);
+  const hipError_t e = launch_kv_write_rope(a, desc->batch, max_q_len, desc->head_dim, src_bytes, codes ? (int)kv_kind(*desc) : -1, s);
   prof.stop();
   if (e != hipSuccess) return fail_hip(e);
   return ROLLATTN_OK;
@@ -894,7 +966,7 @@ const char* rollattn_status_string(int status) {
     case ROLLATTN_OK: return "ok";
     case ROLLATTN_EINVAL: return "invalid argument (null pointer or negative size)";
     case ROLLATTN_ESHAPE: return "unsupported shape (Hq % Hkv != 0, head_dim not 64/128, page_size not 16)";
-    case ROLLATTN_EDTYPE: return "unsupported q/kv dtype pair, or FP8 pools without scales";
+    case ROLLATTN_EDTYPE: return "unsupported q/kv dtype pair, or 8-bit pools without scales";
     case ROLLATTN_EALIGN: return "device pointer not 16-byte aligned";
     case ROLLATTN_EWORKSPACE: return "workspace smaller than rollattn_workspace_bytes()";
     case ROLLATTN_EHIP: return "HIP call failed (see rollattn_last_hip_error)";
@@ -910,6 +982,6 @@ const char* rollattn_last_hip_error(void) {
   return copy.c_str();
 }
 
-int rollattn_version(void) { return 101; }
+int rollattn_version(void) { return 102; }
 
 }  // extern "C"

@@ -1,5 +1,5 @@
 // Observation-append attention (chunked causal prefill on a cached prefix) for bf16 queries
-// over bf16 or FP8-E4M3 paged KV, on the gfx950 matrix cores.
+// over bf16 or 8-bit (E4M3, int8) paged KV, on the gfx950 matrix cores.
 //
 // One workgroup = 256 query rows of one (trajectory, KV head): a row is a (chunk token, query
 // head of the group) pair, token-major, so the G heads that share the KV head reuse every K/V
@@ -45,6 +45,12 @@
 //     addend as log2(vs), so P comes out of the exponential already weighted for the second
 //     product; the row sum divides each page's share by vs again (four multiplies per block).
 //
+// Pools with a scale for each page and KV head (E4M3 or int8 codes) take the FP8 path with f16 in the place of bf16: a code is exact
+// in either, an int8 one is cheaper to widen, and probabilities keep 11 bits instead of 8.  For f16's range queries are multiplied
+// by a power of two per row (exact; taken back with the page's K scale), and a row's reference is that of the weights p * vs,
+// 2^kWeightBits below the largest when it moves; it moves when a lane's weights of a block add up to more than kHalfSumLimit, so none
+// is ever too large for f16, and one 2^-22 of the largest still is a normal number.
+//
 // Half tiles.  A call whose chunks all fit into 128 rows gets tiles of 128 rows: waves w and w + 4 then own the
 // same 32 rows and split every step, and their two running states are merged when the tile ends.  Over FP8 pools a
 // step of a long tile is two blocks, 64 tokens to each wave (see the template parameter HALF below).
@@ -60,6 +66,9 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -75,6 +84,10 @@ constexpr int kBlockTokens = kAppendBlockTokens;   // KV tokens staged per step
 constexpr int kLongTileBlocks = 20;                // half tiles over FP8 pools: from this many blocks on a step is two of them
 constexpr int kScaleWindow = 64;                   // FP8: pages whose scales are fetched at a time, a lane each
 constexpr float kSumLimit = 16384.f;               // a lane's 32 probabilities of a block may add up to this much before the row's reference moves
+
+constexpr float kHalfSumLimit = 65000.f;           // the same for f16 weights, none of which may pass 65504
+constexpr float kWeightBits = 8.f;                 // f16: log2 of a row's largest weight when its reference moves
+constexpr int kQueryBits = 15;                     // f16: a row's largest query element is below two to this
 
 // Row t of an S^T tile holds this token of its 16-token group: the middle two quads are
 // swapped so that the 8 scores a lane ends up with are 8 consecutive tokens.
@@ -95,6 +108,35 @@ template <int PAIR>
 __device__ __forceinline__ uint32_t fp8_pair(const uintx4 codes) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[PAIR / 2], 1.0f, PAIR % 2 != 0));
 }
+
+template <int PAIR>
+__device__ __forceinline__ uint32_t fp8_pair_f16(const uintx4 codes) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[PAIR / 2], 1.0f, PAIR % 2 != 0));
+}
+// The same for sixteen 8-bit integers whose signs have been turned round, so that a byte counts from -128 up: as the low bits of
+// 1024.0 it adds itself to that, and 1152 less is the value.
+template <int PAIR>
+__device__ __forceinline__ uint32_t int8_pair(const uintx4 turned) {
+  uint32_t sel = PAIR % 2 ? 0x04030402u : 0x04010400u, off = 0xe480e480u;
+  asm("" : "+s"(sel), "+s"(off));
+  const uint32_t w = __builtin_amdgcn_perm(0x64646464u, turned[PAIR / 2], sel);
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, w) + __builtin_bit_cast(halfx2, off));
+}
+// Pair PAIR of a chunk of codes; of int8 ones the even pairs come first and turn the word's signs.
+template <int KV, int PAIR>
+__device__ __forceinline__ uint32_t widen_pair(uintx4& codes) {
+  if constexpr (KV == kKvInt8Head) {
+    if constexpr (PAIR % 2 == 0) codes[PAIR / 2] ^= 0x80808080u;
+    return int8_pair<PAIR>(codes);
+  } else if constexpr (KV == kKvFp8Head) {
+    return fp8_pair_f16<PAIR>(codes);
+  } else {
+    return fp8_pair<PAIR>(codes);
+  }
+}
+
+__device__ __forceinline__ floatx16 mfma(bf16x8 x, bf16x8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
+__device__ __forceinline__ floatx16 mfma(halfx8 x, halfx8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
 
 // 16 bytes of a pool; once: nobody reads them again, so they go past the caches' care (see load16 in decode_mfma.hip).
 template <bool ONCE>
@@ -229,8 +271,12 @@ __device__ __forceinline__ decltype(auto) choose(A& a, B& b) {
 }
 
 // kOneOfTwo: another instance in the same kernel, both in `shared`; what is worked out in one stays in it, behind the branch.
-template <int D, bool FP8, bool HALF, bool ONCE, int STEP, bool kOneOfTwo>
-__device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, AppendLds<D, FP8, HALF, STEP>* shared) {
+template <int D, int KV, bool HALF, bool ONCE, int STEP, bool kOneOfTwo>
+__device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, AppendLds<D, kv_is_codes(KV), HALF, STEP>* shared) {
+  constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
+  using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;
+  using opx4 = std::conditional_t<HEAD, halfx4, bf16x4>;
+  using op = std::conditional_t<HEAD, _Float16, __bf16>;
   auto& a = args_of<kOneOfTwo>(kernel_args);
   typedef AppendGeo<D, FP8, HALF, STEP> Geo;
   constexpr int kStepTokens = STEP;
@@ -372,13 +418,14 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 
   // Rows past the tile's last read that one again: what becomes of them is neither stored nor looked at.  (A branch around each
   // load had one of them waited for before the next was sent.)
-  bf16x8 qop[kKK];
+  opx8 qop[kKK];
   {
     const int qtok = row_ok ? tok_in_tile : tokens_here - 1, qhead = row_ok ? head : g * group;
     const __bf16* qrow = (const __bf16*)q + ((size_t)(q_off + q0 + qtok) * hq + qhead) * D;
 #pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) qop[kk] = *(const bf16x8*)(qrow + kk * 16 + h2 * 8);   // bf16 pools: scaled further down
+    for (int kk = 0; kk < kKK; ++kk) qop[kk] = *(const opx8*)(qrow + kk * 16 + h2 * 8);   // bf16 pools: scaled further down; f16: so far only moved
   }
+  float q_unit = 1.f;                            // f16: what a unit of this lane's row is worth
 
   floatx16 acc[kDT];
 #pragma unroll
@@ -448,9 +495,18 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   };
   // -- register path (FP8)
   uintx4 kreg[2][kLoads], vreg[2][kLoads];   // two units in flight
-  auto put = [&](lds_p lo_at, lds_p hi_at, int offset, const uintx4 codes) __attribute__((always_inline)) {
-    *lds_at<uintx4>(lo_at, offset) = uintx4{fp8_pair<0>(codes), fp8_pair<1>(codes), fp8_pair<2>(codes), fp8_pair<3>(codes)};
-    *lds_at<uintx4>(hi_at, offset) = uintx4{fp8_pair<4>(codes), fp8_pair<5>(codes), fp8_pair<6>(codes), fp8_pair<7>(codes)};
+  auto put = [&](lds_p lo_at, lds_p hi_at, int offset, uintx4 codes) __attribute__((always_inline)) {
+    uintx4 lo, hi;
+    static_for<4>([&](auto m_c) __attribute__((always_inline)) {
+      constexpr int m = decltype(m_c)::value;
+      lo[m] = widen_pair<KV, m>(codes);
+    });
+    static_for<4>([&](auto m_c) __attribute__((always_inline)) {
+      constexpr int m = decltype(m_c)::value;
+      hi[m] = widen_pair<KV, 4 + m>(codes);
+    });
+    *lds_at<uintx4>(lo_at, offset) = lo;
+    *lds_at<uintx4>(hi_at, offset) = hi;
   };
   // -- direct path (bf16): HBM -> LDS without a register stop.  Lane l's 16 bytes land at
   // M0 + 16 l.  The compiler does not see these loads as loads: completion is awaited by count
@@ -478,8 +534,9 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     window_k = *(const unsigned int*)((const char*)(const int32_t*)table + (unsigned int)min((blk * kPagesPerBlock + lane) * 4, page_live));
   };
   auto window_scales = [&]() __attribute__((always_inline)) {
-    window_v = a.v_scale[window_k];
-    window_k = __float_as_uint(a.k_scale[window_k]);
+    const size_t at = HEAD ? (size_t)window_k * hkv + g : (size_t)window_k;
+    window_v = a.v_scale[at];
+    window_k = __float_as_uint(a.k_scale[at]);
   };
   auto window_write = [&](int blk) __attribute__((always_inline)) {
     const int at = (blk * kPagesPerBlock + lane) % (2 * kScaleWindow);
@@ -514,7 +571,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   constexpr int kSubs = kStepTokens / (HALF ? 64 : 32);   // 32-token sub-blocks of a step that this wave works on
   constexpr int kPvSteps = 8 * kSubs, kSteps = 16 * kSubs;
   floatx16 s[kSubs];        // scores of the block between its two phases
-  bf16x8 pop[kSubs][2];     // its probabilities, as B operands of the second product
+  opx8 pop[kSubs][2];       // its probabilities, as B operands of the second product
 
   // ---- matrix phase: up to kSteps (32; HALF over bf16 pools: 16) MFMA steps, O^T += V^T P^T for the previous block (the
   // first kPvSteps, V buffer at vbo) and S^T = K Q^T for this one (the others, K buffer at kbo).  Every step
@@ -530,8 +587,8 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   // read at the end of the vector phase before it, in front of the barrier (the V tile they come from was
   // complete one phase earlier), so that the phase does not open with an LDS round trip.
   constexpr bool kEarly = !FP8;
-  bf16x8 early[kAhead];
-  auto read_v_operand = [&](int vbo, auto t_c, bf16x8& dst) __attribute__((always_inline)) {
+  opx8 early[kAhead];
+  auto read_v_operand = [&](int vbo, auto t_c, opx8& dst) __attribute__((always_inline)) {
     constexpr int t = decltype(t_c)::value;
     constexpr int sub = t >> 3, ks = (t >> 2) & 1, dt = t & 3;
     if constexpr (dt < kDT) {
@@ -539,7 +596,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       for (int hf = 0; hf < 2; ++hf) {
         const shortx4 raw = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             lds_at<shortx4>(vptr[dt], vbo + (sub * 32 + ks * 16 + hf * 4) * kRowBytes));
-        const bf16x4 h4 = __builtin_bit_cast(bf16x4, raw);
+        const opx4 h4 = __builtin_bit_cast(opx4, raw);
         dst[hf * 4 + 0] = h4[0]; dst[hf * 4 + 1] = h4[1]; dst[hf * 4 + 2] = h4[2]; dst[hf * 4 + 3] = h4[3];
       }
     }
@@ -549,21 +606,21 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   };
   auto matrix_phase = [&](auto first_c, auto last_c, int kbo, int vbo, auto&& piece) __attribute__((always_inline)) {
     constexpr int T0 = decltype(first_c)::value, T1 = decltype(last_c)::value;
-    bf16x8 ops[kSteps];
+    opx8 ops[kSteps];
     auto fetch = [&](auto t_c) __attribute__((always_inline)) {
       constexpr int t = decltype(t_c)::value;
       if constexpr (t < kPvSteps) {
         read_v_operand(vbo, t_c, ops[t]);
       } else {
         constexpr int u = t - kPvSteps, kk = u / kSubs, sub = u % kSubs;
-        if constexpr (kk < kKK) ops[t] = *lds_at<const bf16x8>(kptr[kk], kbo + sub * 32 * kRowBytes);
+        if constexpr (kk < kKK) ops[t] = *lds_at<const opx8>(kptr[kk], kbo + sub * 32 * kRowBytes);
       }
     };
     auto fire = [&](auto t_c) __attribute__((always_inline)) {
       constexpr int t = decltype(t_c)::value;
       if constexpr (t < kPvSteps) {
         constexpr int sub = t >> 3, ks = (t >> 2) & 1, dt = t & 3;
-        if constexpr (dt < kDT) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ops[t], pop[sub][ks], acc[dt], 0, 0, 0);
+        if constexpr (dt < kDT) acc[dt] = mfma(ops[t], pop[sub][ks], acc[dt]);
       } else {
         constexpr int u = t - kPvSteps, kk = u / kSubs, sub = u % kSubs;
         if constexpr (kk < kKK) {
@@ -571,12 +628,12 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
             if constexpr (FP8) {
 #pragma unroll
               for (int i = 0; i < 16; ++i) s[sub][i] = 0.f;
-              s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ops[t], qop[kk], s[sub], 0, 0, 0);
+              s[sub] = mfma(ops[t], qop[kk], s[sub]);
             } else {
-              s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ops[t], qop[kk], negm, 0, 0, 0);
+              s[sub] = mfma(ops[t], qop[kk], negm);
             }
           } else {
-            s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ops[t], qop[kk], s[sub], 0, 0, 0);
+            s[sub] = mfma(ops[t], qop[kk], s[sub]);
           }
         }
       }
@@ -617,7 +674,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     float sc[kPg], lvs[kPg], ivs[kPg];                 // this wave's pages: K scale times softmax scale, log2 of the V scale, its reciprocal
     if constexpr (FP8) {
 #pragma unroll
-      for (int p = 0; p < kPg; ++p) { sc[p] = ksc_cur[p]; lvs[p] = lvs_cur[p]; ivs[p] = ivs_cur[p]; }
+      for (int p = 0; p < kPg; ++p) { sc[p] = HEAD ? ksc_cur[p] * q_unit : ksc_cur[p]; lvs[p] = lvs_cur[p]; ivs[p] = ivs_cur[p]; }
       if (!positive_scale) {                           // rare: scale the scores themselves instead
 #pragma unroll
         for (int sub = 0; sub < kSubs; ++sub)
@@ -640,6 +697,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     const float m_old = m_ref;                         // what the exponents in s (bf16 pools) are relative to
     float p[kSubs][16];
     // exponentials of the block against reference m_old + shift, and this lane's share of the row sums
+    float weights = 0.f;                               // f16: what says whether the reference has to move
     auto exponentials = [&](auto first_c, float shift) __attribute__((always_inline)) -> float {
       float ad[kPg], psum[kPg];
       if constexpr (FP8) {
@@ -659,13 +717,14 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
           if ((i & 7) == 0) psum[pg] = p[sub][i];
           else psum[pg] += p[sub][i];
         }
+      if constexpr (HEAD) weights = kPg == 2 ? psum[0] + psum[1] : (psum[0] + psum[1]) + (psum[kPg - 2] + psum[kPg - 1]);
       if constexpr (kPg == 2) return FP8 ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1];
       else if constexpr (FP8) return (psum[0] * ivs[0] + psum[1] * ivs[1]) + (psum[2] * ivs[2] + psum[3] * ivs[3]);
       else return (psum[0] + psum[1]) + (psum[2] + psum[3]);
     };
     float lane_sum = exponentials(std::true_type{}, 0.f);
     // (an infinite or undefined sum also fails the comparison and takes the slow path)
-    if (__builtin_amdgcn_ballot_w64(!(lane_sum <= sum_limit))) {
+    if (__builtin_amdgcn_ballot_w64(!((HEAD ? weights : lane_sum) <= sum_limit))) {
       // largest exponent of the block: FP8 page scales and the softmax scale are positive here, so the maximum
       // can be taken on the raw products of each page
       float pm[kPg];
@@ -678,7 +737,12 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
         pm[q] = fmaxf(x, s[sub][o + 7]);
       }
       float mloc;
-      if constexpr (kPg == 2) mloc = FP8 ? fmaxf(pm[0] * sc[0], pm[1] * sc[1]) : fmaxf(pm[0], pm[1]) + m_old;
+      if constexpr (HEAD) {
+#pragma unroll
+        for (int q = 0; q < kPg; ++q) pm[q] = __builtin_fmaf(pm[q], sc[q], lvs[q] - kWeightBits);
+        mloc = fmaxf(pm[0], pm[1]);
+        if constexpr (kPg == 4) mloc = fmaxf(mloc, fmaxf(pm[kPg - 2], pm[kPg - 1]));
+      } else if constexpr (kPg == 2) mloc = FP8 ? fmaxf(pm[0] * sc[0], pm[1] * sc[1]) : fmaxf(pm[0], pm[1]) + m_old;
       else if constexpr (FP8) mloc = fmaxf(fmaxf(pm[0] * sc[0], pm[1] * sc[1]), fmaxf(pm[2] * sc[2], pm[3] * sc[3]));
       else mloc = fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])) + m_old;
       const float m_run = seen_max();
@@ -691,7 +755,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
       m_ref = m_safe;
-      if (row_ok && m_new != -INFINITY) sum_limit = kSumLimit;
+      if (row_ok && m_new != -INFINITY) sum_limit = HEAD ? kHalfSumLimit : kSumLimit;
       if constexpr (!FP8) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) negm[i] = -m_safe;
@@ -702,7 +766,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
     for (int sub = 0; sub < kSubs; ++sub)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) pop[sub][i >> 3][i & 7] = (__bf16)p[sub][i];
+      for (int i = 0; i < 16; ++i) pop[sub][i >> 3][i & 7] = (op)p[sub][i];
     // the probabilities are finished here, in this phase, not wherever the compiler would like to sink them
 #pragma unroll
     for (int sub = 0; sub < kSubs; ++sub)
@@ -710,7 +774,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       for (int ks = 0; ks < 2; ++ks) {
         uintx4 t = __builtin_bit_cast(uintx4, pop[sub][ks]);
         asm volatile("" : "+v"(t));
-        pop[sub][ks] = __builtin_bit_cast(bf16x8, t);
+        pop[sub][ks] = __builtin_bit_cast(opx8, t);
       }
   };
 
@@ -781,6 +845,23 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
         if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) put(wptr[j][0], wptr[j][1], 0, k0[j]);
+      if constexpr (HEAD) {
+        float top = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < kKK; ++kk) {
+          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, __builtin_fabsf((float)v[e]));
+        }
+        const int up = kQueryBits - __builtin_amdgcn_frexp_expf(xor32_max(top));
+#pragma unroll
+        for (int kk = 0; kk < kKK; ++kk) {
+          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) qop[kk][e] = (op)__builtin_amdgcn_ldexpf((float)v[e], up);
+        }
+        q_unit = __builtin_amdgcn_ldexpf(1.f, -up);
+      }
     } else {
       // The query rows have been under way as long as the page ids; their scaling (bf16 pools: the scores then leave the
       // matrix core as exponents) waits for them in front of the tile loads.  Those are no loads to the compiler: behind them,
@@ -789,7 +870,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
       for (int kk = 0; kk < kKK; ++kk) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) qop[kk][e] = (__bf16)((float)qop[kk][e] * a.scale_log2);
+        for (int e = 0; e < 8; ++e) qop[kk][e] = (op)((float)qop[kk][e] * a.scale_log2);
         asm volatile("" : "+v"(qop[kk]));
       }
 #pragma unroll
@@ -885,7 +966,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
         if constexpr (item * 31 / kItems == pos) {
           constexpr int j = item % kLoads, part = item / kLoads / 5, m = item / kLoads % 5;   // the halves of K's chunk, then V's
           if constexpr (m < 4) {
-            wide[j][m] = fp8_pair<(part & 1) * 4 + m>((part < 2 ? kreg : vreg)[slot][j]);
+            wide[j][m] = widen_pair<KV, (part & 1) * 4 + m>((part < 2 ? kreg : vreg)[slot][j]);
           } else if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) {
             if constexpr (part < 2) *lds_at<uintx4>(wptr[j][part], ring(slot_c, c1)) = wide[j];
             else *lds_at<uintx4>(part == 2 ? wptr[j][2] : flip(wptr[j][2], 16), ring(slot_c, c0)) = wide[j];
@@ -1067,22 +1148,59 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   }
 }
 
-template <int D, bool FP8, bool HALF, bool ONCE, int STEP>
+template <int D, int KV, bool HALF, bool ONCE, int STEP>
 __global__ __launch_bounds__(kThreads, HALF && D == 64 && STEP == kBlockTokens ? 4 : 2) void append_mfma_kernel(const AppendArgs a) {
   if constexpr (STEP == 0) {
     __shared__ union {
-      AppendLds<D, FP8, HALF, kBlockTokens> one;
-      AppendLds<D, FP8, HALF, 2 * kBlockTokens> two;
+      AppendLds<D, kv_is_codes(KV), HALF, kBlockTokens> one;
+      AppendLds<D, kv_is_codes(KV), HALF, 2 * kBlockTokens> two;
     } lds;
     int g;
     const int tile = tile_of(blockIdx.x, a.hkv, g);
     const int blocks = ((const __attribute__((address_space(4))) int32_t*)(a.tile_rec + (size_t)min(tile, a.tile_cap - 1) * kTileRecWords))[6];
-    if (blocks < kLongTileBlocks) append_tile<D, FP8, HALF, ONCE, kBlockTokens, true>(a, &lds.one);
-    else append_tile<D, FP8, HALF, ONCE, 2 * kBlockTokens, true>(a, &lds.two);
+    if (blocks < kLongTileBlocks) append_tile<D, KV, HALF, ONCE, kBlockTokens, true>(a, &lds.one);
+    else append_tile<D, KV, HALF, ONCE, 2 * kBlockTokens, true>(a, &lds.two);
   } else {
-    append_tile<D, FP8, HALF, ONCE, STEP, false>(a, nullptr);
+    append_tile<D, KV, HALF, ONCE, STEP, false>(a, nullptr);
   }
 }
+
+template <int KV>
+hipError_t launch_kind(const AppendArgs& a, int head_dim, bool half_tiles, int grid, hipStream_t s) {
+  constexpr bool F = kv_is_codes(KV);
+  const bool once = half_tiles && a.noncausal;
+  const bool short_tiles = a.max_pages < kLongTileBlocks * (kAppendBlockTokens / kPageSize);   // no context reaches a long tile
+  auto launch = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    if (once) {
+      hipLaunchKernelGGL((append_mfma_kernel<D, KV, true, true, F ? 2 * kAppendBlockTokens : kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
+    } else if (half_tiles && F && !short_tiles) {
+      hipLaunchKernelGGL((append_mfma_kernel<D, KV, true, false, F ? 0 : kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
+    } else if (half_tiles) {
+      hipLaunchKernelGGL((append_mfma_kernel<D, KV, true, false, kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
+    } else {
+      hipLaunchKernelGGL((append_mfma_kernel<D, KV, false, false, kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
+    }
+  };
+  if (head_dim == 128) launch(std::integral_constant<int, 128>{});
+  else if (head_dim == 64) launch(std::integral_constant<int, 64>{});
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// This file makes two objects: one for pools in bf16 and with a scale for each page, and one, with the macro set, for pools with a
+// scale for each page and head.  (The instances of both take the compiler two and a half minutes one after the other.)
+#ifdef ROLLATTN_HEAD_SCALES
+
+hipError_t launch_append_head_scales(const AppendArgs& a, int head_dim, KvKind kv, bool half_tiles, int grid, hipStream_t s) {
+  return kv == kKvInt8Head ? launch_kind<kKvInt8Head>(a, head_dim, half_tiles, grid, s) : launch_kind<kKvFp8Head>(a, head_dim, half_tiles, grid, s);
+}
+
+#else
+
+namespace {
 
 // Merge of the pieces of a tile: one wave per (cut tile, KV head, 32 rows, 32 dims), lanes as in the append kernel's
 // accumulators.  M = max_s m_s; out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.  A piece that a row did not see has
@@ -1177,30 +1295,11 @@ hipError_t launch_append_merge(const AppendArgs& a, int head_dim, int max_merges
   return hipGetLastError();
 }
 
-hipError_t launch_append_mfma(const AppendArgs& a, int head_dim, bool fp8, bool half_tiles, int grid, hipStream_t s) {
-  if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
-  const bool once = half_tiles && a.noncausal;
-  const bool short_tiles = a.max_pages < kLongTileBlocks * (kAppendBlockTokens / kPageSize);   // no context reaches a long tile
-  auto launch = [&](auto d, auto f) {
-    constexpr int D = decltype(d)::value;
-    constexpr bool F = decltype(f)::value;
-    if (once) {
-      hipLaunchKernelGGL((append_mfma_kernel<D, F, true, true, F ? 2 * kAppendBlockTokens : kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
-    } else if (half_tiles && F && !short_tiles) {
-      hipLaunchKernelGGL((append_mfma_kernel<D, F, true, false, F ? 0 : kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
-    } else if (half_tiles) {
-      hipLaunchKernelGGL((append_mfma_kernel<D, F, true, false, kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
-    } else {
-      hipLaunchKernelGGL((append_mfma_kernel<D, F, false, false, kAppendBlockTokens>), dim3(grid), dim3(kThreads), 0, s, a);
-    }
-  };
-  std::integral_constant<int, 128> d128;
-  std::integral_constant<int, 64> d64;
-  if (head_dim == 128 && fp8) launch(d128, std::true_type{});
-  else if (head_dim == 128) launch(d128, std::false_type{});
-  else if (fp8) launch(d64, std::true_type{});
-  else launch(d64, std::false_type{});
-  return hipGetLastError();
+hipError_t launch_append_mfma(const AppendArgs& a, int head_dim, KvKind kv, bool half_tiles, int grid, hipStream_t s) {
+  if (kv_has_head_scales(kv)) return launch_append_head_scales(a, head_dim, kv, half_tiles, grid, s);
+  return kv == kKvFp8 ? launch_kind<kKvFp8>(a, head_dim, half_tiles, grid, s) : launch_kind<kKvBf16>(a, head_dim, half_tiles, grid, s);
 }
+
+#endif
 
 }  // namespace rollattn

@@ -1,4 +1,4 @@
-// Decode attention for bf16 queries over bf16 or FP8-E4M3 paged KV (gfx950).
+// Decode attention for bf16 queries over bf16 or 8-bit (E4M3, int8) paged KV (gfx950).
 //
 // A row is (trajectory, KV head, tile of up to 16 query heads of its group): the heads ride
 // along as the 16 columns of an MFMA tile, so K and V are read from HBM exactly once per
@@ -16,6 +16,12 @@
 // The transposed products keep "head" on the lane axis in both results, so the online
 // softmax state (running max, running sum, rescale factor) is one scalar per lane and P
 // feeds the second product straight from the first one's accumulator registers.
+//
+// Pools with a scale for each page and KV head (E4M3 or int8 codes) are widened to f16 instead of bf16: every code is exact in
+// either, and the weights of the second product keep 11 bits instead of 8.  What f16 lacks is range, so
+//   queries are multiplied by a power of two per head that puts the largest element below 2^15 (exact; taken back on the scores),
+//   the running reference is that of the weights p * vs, scores plus log2 of the V scale, less kWeightBits: the largest weight is
+//   2^kWeightBits, and one of 2^-28 of it is still a normal number; the row sum takes p = weight / vs.
 #include <type_traits>
 
 #include "plan_device.h"
@@ -33,8 +39,14 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
 
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
+
+constexpr float kWeightBits = 14.f;   // f16 weights: log2 of the largest
+constexpr int kQueryBits = 15;        // f16 queries: the largest is below two to this
 
 template <int D, bool FP8>
 struct Geo {
@@ -85,6 +97,37 @@ __device__ __forceinline__ bf16x8 fp8x8_to_bf16(uint32_t lo, uint32_t hi) {
   return r;
 }
 
+__device__ __forceinline__ halfx8 fp8x8_to_f16(uint32_t lo, uint32_t hi) {
+  const halfx2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
+  const halfx2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+  const halfx2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
+  const halfx2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+  return halfx8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight 8-bit integers to f16, exactly: with the sign turned round a byte counts from -128 up, as the low bits of 1024.0 it adds
+// itself to that, and 1152 less is the value.
+__device__ __forceinline__ halfx8 int8x8_to_f16(uint32_t lo, uint32_t hi) {
+  lo ^= 0x80808080u;
+  hi ^= 0x80808080u;
+  const halfx2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
+  const halfx2 a = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) + off;
+  const halfx2 b = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) + off;
+  const halfx2 c = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) + off;
+  const halfx2 d = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) + off;
+  return halfx8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight codes as an operand of the matrix core, and its product with another.
+template <int KV>
+__device__ __forceinline__ auto widen8(uint32_t lo, uint32_t hi) {
+  if constexpr (KV == kKvFp8Head) return fp8x8_to_f16(lo, hi);
+  else if constexpr (KV == kKvInt8Head) return int8x8_to_f16(lo, hi);
+  else return fp8x8_to_bf16(lo, hi);
+}
+__device__ __forceinline__ floatx4 mfma(bf16x8 x, bf16x8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
+__device__ __forceinline__ floatx4 mfma(halfx8 x, halfx8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, z, 0, 0, 0); }
+
 // (worked out where it is used: the thread's index would take a register over the whole of a worker's rows)
 __device__ __forceinline__ int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }
 
@@ -107,9 +150,11 @@ __device__ __forceinline__ uint4 load16(const unsigned char* p) {
 
 // One run of blocks.  WHOLE: it is one row from its first block to its last; FOLD: whose other part, in attn_decode_shared, is there
 // and folded in.
-template <int D, bool FP8, bool STREAM, bool WHOLE, bool FOLD>
+template <int D, int KV, bool STREAM, bool WHOLE, bool FOLD>
 __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 start, int worker, unsigned char* const k_lds) {
   static_assert(WHOLE || !FOLD, "cut rows are folded by the merge");
+  constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
+  using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;
   using G_ = Geo<D, FP8>;
   int tid = lane_id();
   asm volatile("" : "+v"(tid));   // (what is worked out from it stays in this instance: shared by both in front of the branch, it would not fit the registers)
@@ -168,8 +213,9 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
     const int p1 = __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1) + 1);
     if (FP8) {
       const int pid = (q4 < 2) ? p0 : p1;        // tokens 0-15 of the block sit in its first page
-      ksc[stage] = a.k_scale[pid];
-      vsc[stage] = a.v_scale[pid];
+      const size_t at = HEAD ? (size_t)pid * hkv + g : (size_t)pid;
+      ksc[stage] = a.k_scale[at];
+      vsc[stage] = a.v_scale[at];
     }
     const unsigned char* kt0 = (const unsigned char*)a.k_pages + ((size_t)p0 * hkv + g) * tile_stride;
     const unsigned char* kt1 = (const unsigned char*)a.k_pages + ((size_t)p1 * hkv + g) * tile_stride;
@@ -222,7 +268,8 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
   };
 
   // ---- consumer state
-  bf16x8 qop[G_::kKK];       // Q^T as the B operand: lane (head r16, quarter q4), 8 dims per step
+  opx8 qop[G_::kKK];         // Q^T as the B operand: lane (head r16, quarter q4), 8 dims per step
+  float q_unit = 1.f;        // f16: what a unit of this lane's head is worth
   floatx4 acc[G_::kDT];      // O^T: lane (head r16, quarter q4) holds dims dt*16 + q4*4 + (0..3)
   float m_run = -INFINITY;   // running max (log2 units) of this lane's head
   float l_run = 0.f;         // this lane's share of the running sum
@@ -244,7 +291,25 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
           v = *(const bf16x8*)(qrow + (kk * 4 + q4) * 8);
         }
       }
-      qop[kk] = v;
+      if constexpr (!HEAD) qop[kk] = v;
+      else qop[kk] = __builtin_bit_cast(halfx8, v);      // (as it came, until all of the head is there)
+    }
+    if constexpr (HEAD) {
+      float top = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < G_::kKK; ++kk) {
+        const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, __builtin_fabsf((float)v[e]));
+      }
+      const int up = kQueryBits - __builtin_amdgcn_frexp_expf(xor32_max(xor16_max(top)));
+#pragma unroll
+      for (int kk = 0; kk < G_::kKK; ++kk) {
+        const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qop[kk][e] = (_Float16)__builtin_amdgcn_ldexpf((float)v[e], up);
+      }
+      q_unit = __builtin_amdgcn_ldexpf(a.scale_log2, -up);
     }
 #pragma unroll
     for (int dt = 0; dt < G_::kDT; ++dt) acc[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -306,42 +371,49 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
         for (int p = 0; p < G_::kChunks / 4; ++p) {
           const int c = ((p * 4 + q4) ^ key) & (G_::kChunks - 1);
           const uint4 raw = *(const uint4*)(rowp + c * 16);
-          s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw.x, raw.y), qop[2 * p], s[e], 0, 0, 0);
-          s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw.z, raw.w), qop[2 * p + 1], s[e], 0, 0, 0);
+          s[e] = mfma(widen8<KV>(raw.x, raw.y), qop[2 * p], s[e]);
+          s[e] = mfma(widen8<KV>(raw.z, raw.w), qop[2 * p + 1], s[e]);
         }
       } else {
 #pragma unroll
         for (int kk = 0; kk < G_::kKK; ++kk) {
           const int c = ((kk * 4 + q4) ^ key) & (G_::kChunks - 1);
-          const bf16x8 kop = *(const bf16x8*)(rowp + c * 16);
-          s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, qop[kk], s[e], 0, 0, 0);
+          const opx8 kop = *(const opx8*)(rowp + c * 16);
+          s[e] = mfma(kop, qop[kk], s[e]);
         }
       }
     }
     // This lane now holds, for head r16, the scores of tokens tok0 + q4*8 + (0..7):
     // s[0][i] -> +i, s[1][i] -> +4+i.
-    const float sc = FP8 ? a.scale_log2 * kscale : a.scale_log2;
-    const float vs = FP8 ? vscale : 1.f;
-    float x[8];
     const int tbase = tok0 + q4 * 8;
+    const float sc = HEAD ? q_unit * kscale : FP8 ? a.scale_log2 * kscale : a.scale_log2;
+    float vs = FP8 ? vscale : 1.f, lvs = 0.f, ivs = 1.f;
+    if constexpr (HEAD) {
+      if (tbase >= len) vs = 1.f;                  // (a page that this row does not have: its scale may be anything)
+      lvs = __builtin_amdgcn_logf(vs);
+      ivs = __builtin_amdgcn_rcpf(vs);
+    }
+    float x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float raw = (j < 4) ? s[0][j] : s[1][j - 4];
-      x[j] = (tbase + j < len) ? raw * sc : -INFINITY;
+      x[j] = (tbase + j < len) ? (HEAD ? __builtin_fmaf(raw, sc, lvs) : raw * sc) : -INFINITY;
     }
     float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     mx = xor32_max(xor16_max(mx));
+    if constexpr (HEAD) mx -= kWeightBits;
     const float m_new = fmaxf(m_run, mx);       // finite: the first token of a block is always live
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
     float psum = 0.f;
-    bf16x8 pop;
+    opx8 pop;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float p = __builtin_amdgcn_exp2f(x[j] - m_new);
       psum += p;
-      pop[j] = (__bf16)(FP8 ? p * vs : p);
+      if constexpr (HEAD) pop[j] = (_Float16)p;
+      else pop[j] = (__bf16)(FP8 ? p * vs : p);
     }
-    l_run = l_run * alpha + psum;
+    l_run = l_run * alpha + (HEAD ? psum * ivs : psum);
     if (__builtin_amdgcn_ballot_w64(m_new > m_run)) {
 #pragma unroll
       for (int dt = 0; dt < G_::kDT; ++dt) acc[dt] *= alpha;
@@ -350,14 +422,14 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
     // ---- O^T += V^T P^T : A = V^T tile (16 dims x 32 tokens) read transposed from LDS
 #pragma unroll
     for (int dt = 0; dt < G_::kDT; ++dt) {
-      bf16x8 vop;
-      if (FP8) {
+      opx8 vop;
+      if constexpr (FP8) {
         typedef __attribute__((address_space(3))) intx2 lds_i2;
         const int t = q4 * 8 + (r16 >> 1);
         const int c = (dt ^ key_v8(t)) & (G_::kChunks - 1);
         const intx2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
             (lds_i2*)(v_lds + t * G_::kRowBytes + c * 16 + (r16 & 1) * 8));
-        vop = fp8x8_to_bf16((uint32_t)raw[0], (uint32_t)raw[1]);
+        vop = widen8<KV>((uint32_t)raw[0], (uint32_t)raw[1]);
       } else {
         typedef __attribute__((address_space(3))) shortx4 lds_s4;
 #pragma unroll
@@ -370,7 +442,7 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
           vop[hf * 4 + 0] = h4[0]; vop[hf * 4 + 1] = h4[1]; vop[hf * 4 + 2] = h4[2]; vop[hf * 4 + 3] = h4[3];
         }
       }
-      acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, pop, acc[dt], 0, 0, 0);
+      acc[dt] = mfma(vop, pop, acc[dt]);
     }
   };
 
@@ -428,10 +500,10 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
 
 // IN_WAVE: no plan was launched, and rows are never whole.  FOLD: for attn_decode_shared.  (One kernel for all had 254 registers
 // instead of 246 over bf16 pools and took 0.3 us longer on a call of 30, 1 % on long ones.)
-template <int D, bool FP8, bool IN_WAVE, bool FOLD>
+template <int D, int KV, bool IN_WAVE, bool FOLD>
 __global__ __launch_bounds__(kThreads, 2) void decode_mfma_kernel(const DecodeArgs a) {
   // Per wave: one K tile and one V tile.
-  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves][2 * Geo<D, FP8>::kTileBytes];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves][2 * Geo<D, kv_is_codes(KV)>::kTileBytes];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int worker = blockIdx.x * kWaves + wave;
   // Where another worker reads some of the run's pages, too, it may find them in a cache, and the hint would cost that:
@@ -464,8 +536,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mfma_kernel(const DecodeAr
         const int len = a.ctx_lens[b], new_rows = a.q_lens ? a.q_lens[b] : 1;
         if (new_rows == 1 && len > 0) {
           const int4 all = make_int4(b, r << 20, len, (len + kBlockTokens - 1) / kBlockTokens);
-          if (read_again) decode_worker<D, FP8, false, true, FOLD>(a, all, worker, lds[wave]);
-          else decode_worker<D, FP8, true, true, FOLD>(a, all, worker, lds[wave]);
+          if (read_again) decode_worker<D, KV, false, true, FOLD>(a, all, worker, lds[wave]);
+          else decode_worker<D, KV, true, true, FOLD>(a, all, worker, lds[wave]);
         }
         unsigned int ticket = 0;
         if (lane_id() == 0) ticket = atomicAdd(&drawn, 1u);
@@ -477,27 +549,31 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mfma_kernel(const DecodeAr
   }
   start = make_int4(__builtin_amdgcn_readfirstlane(start.x), __builtin_amdgcn_readfirstlane(start.y), __builtin_amdgcn_readfirstlane(start.z), __builtin_amdgcn_readfirstlane(start.w));
   if (start.x < 0) return;
-  if (read_again) decode_worker<D, FP8, false, false, false>(a, start, worker, lds[wave]);
-  else decode_worker<D, FP8, true, false, false>(a, start, worker, lds[wave]);
+  if (read_again) decode_worker<D, KV, false, false, false>(a, start, worker, lds[wave]);
+  else decode_worker<D, KV, true, false, false>(a, start, worker, lds[wave]);
 }
 
 }  // namespace
 
-hipError_t launch_decode_mfma(const DecodeArgs& a, int head_dim, bool fp8, int grid, hipStream_t s) {
-  auto launch = [&](auto d, auto f) {
+hipError_t launch_decode_mfma(const DecodeArgs& a, int head_dim, KvKind kv, int grid, hipStream_t s) {
+  auto launch = [&](auto d, auto kind) {
     constexpr int D = decltype(d)::value;
-    constexpr bool F = decltype(f)::value;
-    if (a.plan.batch) hipLaunchKernelGGL((decode_mfma_kernel<D, F, true, false>), dim3(grid), dim3(kThreads), 0, s, a);
-    else if (a.shared.result) hipLaunchKernelGGL((decode_mfma_kernel<D, F, false, true>), dim3(grid), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((decode_mfma_kernel<D, F, false, false>), dim3(grid), dim3(kThreads), 0, s, a);
+    constexpr int KV = decltype(kind)::value;
+    if (a.plan.batch) hipLaunchKernelGGL((decode_mfma_kernel<D, KV, true, false>), dim3(grid), dim3(kThreads), 0, s, a);
+    else if (a.shared.result) hipLaunchKernelGGL((decode_mfma_kernel<D, KV, false, true>), dim3(grid), dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((decode_mfma_kernel<D, KV, false, false>), dim3(grid), dim3(kThreads), 0, s, a);
   };
-  std::integral_constant<int, 128> d128;
-  std::integral_constant<int, 64> d64;
-  if (head_dim == 128 && fp8) launch(d128, std::true_type{});
-  else if (head_dim == 128) launch(d128, std::false_type{});
-  else if (head_dim == 64 && fp8) launch(d64, std::true_type{});
-  else if (head_dim == 64) launch(d64, std::false_type{});
-  else return hipErrorInvalidValue;
+  auto of_kind = [&](auto kind) {
+    if (head_dim == 128) launch(std::integral_constant<int, 128>{}, kind);
+    else launch(std::integral_constant<int, 64>{}, kind);
+  };
+  if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
+  switch (kv) {
+    case kKvBf16: of_kind(std::integral_constant<int, kKvBf16>{}); break;
+    case kKvFp8: of_kind(std::integral_constant<int, kKvFp8>{}); break;
+    case kKvFp8Head: of_kind(std::integral_constant<int, kKvFp8Head>{}); break;
+    case kKvInt8Head: of_kind(std::integral_constant<int, kKvInt8Head>{}); break;
+  }
   return hipGetLastError();
 }
 

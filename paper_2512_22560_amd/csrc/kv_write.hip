@@ -9,36 +9,13 @@
 // encodes the new rows.  Codes are integers decided by float arithmetic, so every product and
 // quotient below is one IEEE float32 operation in a fixed order, with the clamp to [-448, 448]
 // before the hardware conversion (round to nearest even onto the E4M3 grid).
-#include "rollattn_internal.h"
+#include "codes_device.h"
 
 namespace rollattn {
 
 namespace {
 
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
-typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
-
 constexpr int kThreads = 256;
-constexpr float kE4m3Max = 448.f;
-
-// (one instruction, the median, where a minimum of a maximum is two; both make -448 of an undefined value)
-__device__ __forceinline__ float clamp448(float x) { return __builtin_amdgcn_fmed3f(x, -kE4m3Max, kE4m3Max); }
-
-// eight floats -> eight E4M3 codes
-__device__ __forceinline__ uintx2 encode8(const float* x) {
-  uintx2 r;
-  int w = 0;
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(x[0]), clamp448(x[1]), w, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(x[2]), clamp448(x[3]), w, true);
-  r[0] = (unsigned int)w;
-  w = 0;
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(x[4]), clamp448(x[5]), w, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(x[6]), clamp448(x[7]), w, true);
-  r[1] = (unsigned int)w;
-  return r;
-}
-
 __device__ __forceinline__ void bf16x8_to_float(const uintx4 raw, float* x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -209,31 +186,11 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const KvWriteArgs a)
           }
         }
       }
-      // x / s_new for every new element: ten instructions apiece as the compiler expands an IEEE division.
-      // All of them share the divisor, so its refined reciprocal is worked out once and each quotient takes
-      // the remaining steps of that same expansion (product, two residual corrections, a last fused step) and
-      // the sign of the dividend, which a quotient that rounds to zero would otherwise lose: six
-      // instructions, and the same correctly rounded result wherever the expansion's operand scaling would
-      // have done nothing, i.e. for a divisor of moderate magnitude and every quotient large enough to
-      // matter (one below 2^-10 encodes to zero whatever its last bits).  Divisors outside that range take
-      // the plain division.
-      const bool fast_div = s_new >= 0x1p-100f && s_new <= 0x1p+100f;
-      const float r0 = __builtin_amdgcn_rcpf(s_new);
-      const float r1 = __builtin_fmaf(__builtin_fmaf(-s_new, r0, 1.f), r0, r0);
+      const Quotients by_scale(s_new);
       auto emit = [&](const uintx4 raw) {
         float x[8];
         bf16x8_to_float(raw, x);
-        if (fast_div) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float q0 = x[i] * r1;
-            const float q1 = __builtin_fmaf(__builtin_fmaf(-s_new, q0, x[i]), r1, q0);
-            x[i] = __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-s_new, q1, x[i]), r1, q1), x[i]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = x[i] / s_new;
-        }
+        by_scale.divide(x);
         *(uintx2*)(tile + (size_t)(h * kPageSize + s0 + slot) * D + col * 8) = encode8(x);
       };
       if (keep) {

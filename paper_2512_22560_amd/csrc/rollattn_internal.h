@@ -37,6 +37,16 @@ constexpr float kSplitGain = 0.95f, kSplitGainUs = 1.5f;   // ... a list is cut 
 constexpr int split_extra_pieces(int hkv) { return 2 * kNumCUs / hkv; }   // append: cutting makes a list at most this much longer (two rounds)
 constexpr int kAppendXcdRun = 16;       // append: consecutive tiles of the list that one XCD takes in a row (one per CU)
 
+// What a pool holds, as the bf16 kernels are instantiated for it.
+enum KvKind {
+  kKvBf16 = 0,
+  kKvFp8 = 1,        // E4M3 codes, a scale for each page
+  kKvFp8Head = 2,    // E4M3 codes, a scale for each page and KV head
+  kKvInt8Head = 3,   // 8-bit integers, a scale for each page and KV head
+};
+constexpr bool kv_is_codes(int kv) { return kv != kKvBf16; }                          // one byte per element
+constexpr bool kv_has_head_scales(int kv) { return kv == kKvFp8Head || kv == kKvInt8Head; }
+
 // Header words of the plan, at the start of the workspace.
 enum PlanWord { kPlanPer = 0, kPlanTotal = 1, kPlanWorkers = 2, kPlanRowsPerB = 3, kPlanTiles = 4, kPlanMerges = 5, kPlanWhole = 6,
                 kPlanReadAgain = 32,   // (this word and kPlanWhole are each written by another workgroup than the rest)
@@ -172,6 +182,21 @@ struct AppendPlanArgs {
   int32_t* merge_rec;
 };
 
+// The write with the position rotation on the way (and the plain one into pools with a scale for each page and head).
+struct RopeWriteArgs {
+  const void *q, *k_new, *v_new;   // q null: keys and values alone
+  void *q_out, *k_pages, *v_pages;
+  const int32_t *q_lens, *q_offsets, *page_table, *ctx_lens;
+  float *k_scale, *v_scale;
+  const float* cos_sin;            // null: no rotation
+  const int32_t* positions;
+  int64_t q_stride, k_stride, v_stride;   // elements from a token to the next
+  int32_t hq, hkv, max_pages, total_q;
+  int32_t rot_dim, num_positions;
+  uint32_t pair_axes[4];           // two bits per pair
+  int32_t interleaved;
+};
+
 // Launchers (defined in the .hip files).  Each returns the hipError_t of its launch.
 hipError_t launch_plan_decode(const DecodePlanArgs& d, hipStream_t s);
 hipError_t launch_plan_append(const AppendPlanArgs& a, hipStream_t s);
@@ -181,13 +206,14 @@ hipError_t launch_plan_shared(const SharedPlanArgs& sh, const AppendPlanArgs& a,
 hipError_t launch_decode_f32(const DecodeArgs& a, int head_dim, int grid, hipStream_t s);
 // float32, one launch for plan, attention and output: a workgroup per row, for tables of at most kDirectPages pages and no more rows than CUs
 hipError_t launch_decode_f32_direct(const DecodeArgs& a, int head_dim, hipStream_t s);
-hipError_t launch_decode_mfma(const DecodeArgs& a, int head_dim, bool fp8, int grid, hipStream_t s);
+hipError_t launch_decode_mfma(const DecodeArgs& a, int head_dim, KvKind kv, int grid, hipStream_t s);
 hipError_t launch_combine(const DecodeArgs& a, int head_dim, bool out_bf16, hipStream_t s);
 // the same for bf16 rows of which a.shared holds another part of the context: every row is written, to a.shared.result
 hipError_t launch_combine_shared(const DecodeArgs& a, int head_dim, hipStream_t s);
 // half_tiles: every tile has at most kAppendTileRows / 2 rows (a.tile_tokens is set accordingly) and the
 // two waves of a SIMD split each block of a tile between them instead of owning different rows
-hipError_t launch_append_mfma(const AppendArgs& a, int head_dim, bool fp8, bool half_tiles, int grid, hipStream_t s);
+hipError_t launch_append_mfma(const AppendArgs& a, int head_dim, KvKind kv, bool half_tiles, int grid, hipStream_t s);
+hipError_t launch_append_head_scales(const AppendArgs& a, int head_dim, KvKind kv, bool half_tiles, int grid, hipStream_t s);   // (its half for those pools)
 // folds the pieces of the tiles that were cut (max_merges: at most this many tiles)
 hipError_t launch_append_merge(const AppendArgs& a, int head_dim, int max_merges, hipStream_t s);
 hipError_t launch_append_f32(const AppendArgs& a, int head_dim, int grid, hipStream_t s);
@@ -195,6 +221,9 @@ hipError_t launch_kv_write(const void* k_new, const void* v_new, const int32_t* 
                            void* k_pages, void* v_pages, const int32_t* page_table, const int32_t* ctx_lens,
                            float* k_scale, float* v_scale, int32_t batch, int32_t hkv, int32_t max_pages,
                            int32_t max_q_len, int head_dim, int src_bytes, bool fp8, hipStream_t s);
+// pool: -1 for one of the source type, else what its codes are (bf16 sources)
+hipError_t launch_kv_write_rope(const RopeWriteArgs& a, int32_t batch, int32_t max_q_len, int head_dim, int src_bytes, int pool,
+                                hipStream_t s);
 hipError_t launch_merge_states(const void* o1, const float* d1, const void* o2, const float* d2, void* out, float* d_out,
                                long rows, int head_dim, bool f32, hipStream_t s);
 hipError_t launch_check_inputs(const int32_t* page_table, const int32_t* ctx_lens, const int32_t* q_lens,

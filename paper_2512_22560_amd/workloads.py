@@ -20,7 +20,10 @@ order Q, K pool, V pool):
   * unused page-table entries are -1; unused slots of each trajectory's last page
     hold NaN (0x7F, the NaN code, for FP8) so that any read of them shows up;
   * FP8 pools: per physical page and per pool, scale = absmax over the live slots
-    / 448 (1.0 for an all-zero page), codes = round-to-nearest-even of x / scale.
+    / 448 (1.0 for an all-zero page), codes = round-to-nearest-even of x / scale;
+  * 8-bit pools with a scale for each page and KV head ("fp8_e4m3_head", "int8_head"): the
+    same over the head's live slots, 127 for 448 where codes are whole numbers, scales
+    2^-64 at the least; unused slots of int8 pools hold -128, which no token has.
 """
 from __future__ import annotations
 
@@ -223,12 +226,13 @@ def build(w: Workload, device="cpu", *, slab_pages: int = 8192) -> Batch:
     live = torch.from_numpy(_live_slots(ctx_lens, table, num_pages)).to(device)
     shape = (num_pages, w.num_kv_heads, PAGE_SIZE, w.head_dim)
     fp8 = w.kv_dtype == "fp8_e4m3"
-    store_dt = torch.uint8 if fp8 else _TORCH_DTYPE[w.kv_dtype]
+    head = w.kv_dtype in ("fp8_e4m3_head", "int8_head")
+    store_dt = torch.int8 if w.kv_dtype == "int8_head" else torch.uint8 if fp8 or head else _TORCH_DTYPE[w.kv_dtype]
     pools, scales = [], []
     slot_ids = torch.arange(PAGE_SIZE, device=device).view(1, 1, PAGE_SIZE, 1)
     for _ in range(2):
         pool = torch.empty(shape, device=device, dtype=store_dt)
-        scale = torch.ones(num_pages, device=device, dtype=torch.float32) if fp8 else None
+        scale = torch.ones(shape[:2] if head else num_pages, device=device, dtype=torch.float32) if fp8 or head else None
         for p0 in range(0, num_pages, slab_pages):
             p1 = min(num_pages, p0 + slab_pages)
             x = torch.randn((p1 - p0,) + shape[1:], generator=gen, device=device, dtype=torch.float32)
@@ -238,6 +242,15 @@ def build(w: Workload, device="cpu", *, slab_pages: int = 8192) -> Batch:
                 s = torch.where(amax > 0, amax / 448.0, torch.ones_like(amax))
                 codes = (x / s.view(-1, 1, 1, 1)).to(torch.float8_e4m3fn).view(torch.uint8)
                 pool[p0:p1] = codes.masked_fill(dead, 0x7F)
+                scale[p0:p1] = s
+            elif head:
+                amax = x.masked_fill(dead, 0.0).abs().amax(dim=(2, 3))
+                s = (amax / torch.full_like(amax, 127.0 if store_dt == torch.int8 else 448.0)).clamp_min(2.0 ** -64)
+                x = x / s[:, :, None, None]
+                if store_dt == torch.int8:
+                    pool[p0:p1] = x.round().clamp(-127, 127).to(torch.int8).masked_fill(dead, -128)
+                else:
+                    pool[p0:p1] = x.to(torch.float8_e4m3fn).view(torch.uint8).masked_fill(dead, 0x7F)
                 scale[p0:p1] = s
             else:
                 pool[p0:p1] = x.masked_fill(dead, float("nan")).to(store_dt)
@@ -288,14 +301,14 @@ def algorithmic_work(w: Workload, ctx_lens: np.ndarray, q_lens: np.ndarray) -> d
     """Bytes the method has to move and flops it has to do, counting K and V of each KV
     head once per call, the live page-table entries, the page scales, Q in and O out;
     attended (query, key) pairs cost 4 * Hq * D flops."""
-    kv_b = {"f32": 4, "bf16": 2, "fp8_e4m3": 1}[w.kv_dtype]
+    kv_b = {"f32": 4, "bf16": 2}.get(w.kv_dtype, 1)
     q_b = {"f32": 4, "bf16": 2}[w.q_dtype]
     L = np.asarray(ctx_lens, dtype=np.int64)
     n = np.asarray(q_lens, dtype=np.int64)
     pages = int(((L + PAGE_SIZE - 1) // PAGE_SIZE).sum())
     kv = int(2 * w.num_kv_heads * w.head_dim * kv_b * L.sum())
     table = 4 * pages
-    scales = 8 * pages if w.kv_dtype == "fp8_e4m3" else 0
+    scales = 8 * pages * (1 if w.kv_dtype == "fp8_e4m3" else w.num_kv_heads) if kv_b == 1 else 0
     qo = int(2 * n.sum() * w.num_q_heads * w.head_dim * q_b)
     pairs = int((n * (L - n) + n * (n + 1) // 2).sum())
     return {"bytes": kv + table + scales + qo, "kv_bytes": kv, "qo_bytes": qo, "pairs": pairs,
