@@ -156,7 +156,9 @@ def _kv_code(pages: torch.Tensor, k_scale, v_scale) -> int:
         return code
     if code == FP8_E4M3 and k_scale.dim() == 1:
         return code
-    if k_scale.shape != pages.shape[:2] or v_scale.shape != pages.shape[:2]:
+    pool = pages.shape
+    held = (pool[0], pool[1])
+    if k_scale.shape != held or v_scale.shape != held:
         raise ValueError("scales of each page and KV head are [num_pages, Hkv]")
     return INT8_HEAD if code == INT8_HEAD else FP8_E4M3_HEAD
 
@@ -351,13 +353,14 @@ def kv_write(k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_
         raise RollattnError(rc, "kv_write")
 
 
-def _row_stride(t: torch.Tensor) -> int:
+def _row_stride(t: torch.Tensor, heads: int, d: int) -> int:
     """Elements between the rows of consecutive tokens; a token's heads lie side by side."""
-    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
-        if t.numel():
-            raise ValueError("the heads of a token lie side by side")
-        return t.shape[1] * t.shape[2]
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+    step, head, item = t.stride()
+    if (head == d or heads == 1) and item == 1:
+        return step if t.shape[0] > 1 else heads * d
+    if t.numel():
+        raise ValueError("the heads of a token lie side by side")
+    return heads * d
 
 
 def kv_write_rope(q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, cos_sin, max_q_len,
@@ -369,36 +372,47 @@ def kv_write_rope(q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_tab
     their sines; pair j is (j, j + rot_dim / 2), or (2 j, 2 j + 1) with `interleaved`.  positions [axes, total_q] int32 (or
     [total_q]; None: a token's place in its context), pair_axes: the axis of each pair, a sequence of rot_dim / 2 whole numbers."""
     _check_contig(q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, cos_sin, positions, k_scale, v_scale, q_out)
-    total_q, hkv, d = k_new.shape
-    if v_new.shape != k_new.shape or k_new.shape[1:] != (k_pages.shape[1], k_pages.shape[3]) or v_pages.shape != k_pages.shape:
+    rows, pool, dtype = k_new.shape, k_pages.shape, k_new.dtype
+    total_q, hkv, d = rows
+    if v_new.shape != rows or v_pages.shape != pool or hkv != pool[1] or d != pool[3]:
         raise ValueError("k_new and v_new are [total_q, Hkv, D] rows of the pools")
-    if q is not None and (q.shape[0] != total_q or q.shape[2] != d):
-        raise ValueError("q is [total_q, Hq, D]")
-    if v_new.dtype != k_new.dtype or (q is not None and q.dtype != k_new.dtype) or v_pages.dtype != k_pages.dtype:
+    if v_new.dtype is not dtype or v_pages.dtype is not k_pages.dtype:
         raise TypeError("q, k_new and v_new are of one type, and so are the pools")
-    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] % 2:
-        raise ValueError("cos_sin is [num_positions, rot_dim] float32")
-    axes = 1
+    num_positions, rot_dim = cos_sin.shape
+    if cos_sin.dtype is not torch.float32:
+        raise TypeError("cos_sin is [num_positions, rot_dim] float32")
+    hq, q_stride, axes = hkv, 0, 1
+    if q is not None:
+        rows_q = q.shape
+        hq = rows_q[1]
+        if rows_q[0] != total_q or rows_q[2] != d:
+            raise ValueError("q is [total_q, Hq, D]")
+        if q.dtype is not dtype:
+            raise TypeError("q, k_new and v_new are of one type, and so are the pools")
+        q_stride = _row_stride(q, hq, d)
+        if q_out is None:
+            q_out = torch.empty(rows_q, dtype=dtype, device=q.device)
+        elif q_out.shape != rows_q or q_out.dtype is not dtype:
+            raise ValueError("q_out takes the rotated q")
+    elif q_out is not None:
+        raise ValueError("q_out takes the rotated q")
     if positions is not None:
-        if positions.dtype != torch.int32 or positions.shape[-1] != total_q or positions.dim() not in (1, 2):
-            raise ValueError("positions is [axes, total_q] int32")
         axes = positions.shape[0] if positions.dim() == 2 else 1
+        if positions.dtype is not torch.int32 or positions.numel() != axes * total_q or positions.dim() > 2:
+            raise ValueError("positions is [axes, total_q] int32")
     if pair_axes is not None:
         pair_axes = bytes(pair_axes)
-        if len(pair_axes) != cos_sin.shape[1] // 2:
+        if 2 * len(pair_axes) != rot_dim:
             raise ValueError("pair_axes has an axis for each pair")
     elif axes > 1:
         raise ValueError("several axes need pair_axes")
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if q_out is not None and (q is None or q_out.shape != q.shape or q_out.dtype != q.dtype):
-        raise ValueError("q_out takes the rotated q")
-    desc = make_desc(k_new if q is None else q, k_pages, page_table, sm_scale=1.0, k_scale=k_scale, v_scale=v_scale)
-    rope = Rope(_ptr(cos_sin), _ptr(positions), pair_axes, cos_sin.shape[0], cos_sin.shape[1], axes, 1 if interleaved else 0,
-                0 if q is None else _row_stride(q), _row_stride(k_new), _row_stride(v_new))
-    rc = lib().kv_write_rope(ctypes.byref(desc), ctypes.byref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_lens), _ptr(q_offsets),
-                             total_q, int(max_q_len), _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(ctx_lens),
-                             _ptr(k_scale), _ptr(v_scale), _stream(stream))
+    table = page_table.shape
+    desc = Desc(table[0], hq, hkv, d, pool[2], table[1], pool[0], _dtype_code(k_new), _kv_code(k_pages, k_scale, v_scale), 1.0, None, None)
+    rope = Rope(cos_sin.data_ptr(), _ptr(positions), pair_axes, num_positions, rot_dim, axes, 1 if interleaved else 0, q_stride,
+                _row_stride(k_new, hkv, d), _row_stride(v_new, hkv, d))
+    rc = lib().kv_write_rope(ctypes.byref(desc), ctypes.byref(rope), _ptr(q), k_new.data_ptr(), v_new.data_ptr(), q_lens.data_ptr(),
+                             q_offsets.data_ptr(), total_q, int(max_q_len), _ptr(q_out), k_pages.data_ptr(), v_pages.data_ptr(),
+                             page_table.data_ptr(), ctx_lens.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream))
     if rc:
         raise RollattnError(rc, "kv_write_rope")
     return q_out

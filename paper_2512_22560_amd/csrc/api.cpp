@@ -793,8 +793,8 @@ int kv_write(const rollattn_desc* desc, const void* k_new, const void* v_new, co
     a.q_lens = q_lens; a.q_offsets = q_offsets; a.page_table = page_table; a.ctx_lens = ctx_lens;
     a.k_scale = k_scale; a.v_scale = v_scale;
     a.k_stride = a.v_stride = (int64_t)desc->num_kv_heads * desc->head_dim;
-    a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq; a.total_q = total_q;
-    const hipError_t e = launch_kv_write_rope(a, desc->batch, max_q_len, desc->head_dim, 2, kv, s);
+    a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq; a.total_q = total_q; a.batch = desc->batch;
+    const hipError_t e = launch_kv_write_rope(a, max_q_len, desc->head_dim, 2, kv, s);
     prof.stop();
     return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
   }
@@ -845,11 +845,11 @@ int kv_write_rope(const rollattn_desc* desc, const rollattn_rope* rope, const vo
   a.q_lens = q_lens; a.q_offsets = q_offsets; a.page_table = page_table; a.ctx_lens = ctx_lens;
   a.k_scale = k_scale; a.v_scale = v_scale;
   a.cos_sin = rope->cos_sin; a.positions = rope->positions;
-  a.hq = desc->num_q_heads; a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq; a.total_q = total_q;
+  a.hq = desc->num_q_heads; a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq; a.total_q = total_q; a.batch = desc->batch;
   a.rot_dim = rope->rot_dim; a.num_positions = rope->num_positions; a.interleaved = rope->interleaved != 0;
   hipStream_t s = (hipStream_t)hip_stream;
   ProfileScope prof(s);
-  const hipError_t e = launch_kv_write_rope(a, desc->batch, max_q_len, desc->head_dim, src_bytes, codes ? (int)kv_kind(*desc) : -1, s);
+  const hipError_t e = launch_kv_write_rope(a, max_q_len, desc->head_dim, src_bytes, codes ? (int)kv_kind(*desc) : -1, s);
   prof.stop();
   if (e != hipSuccess) return fail_hip(e);
   return ROLLATTN_OK;

@@ -44,11 +44,12 @@ __device__ __forceinline__ unsigned int encode4_int8(const float* x) {
 // instructions, and the same correctly rounded result wherever the expansion's operand scaling would
 // have done nothing, i.e. for a divisor of moderate magnitude and every quotient large enough to
 // matter (one below 2^-10 encodes to zero whatever its last bits).  Divisors outside that range take
-// the plain division.
+// the plain division; MODERATE: there are none, as with scales from kLeastHeadScale up to the largest float over 127.
+template <bool MODERATE = false>
 struct Quotients {
   float s, r;
   bool fast;
-  __device__ __forceinline__ explicit Quotients(float divisor) : s(divisor), fast(divisor >= 0x1p-100f && divisor <= 0x1p+100f) {
+  __device__ __forceinline__ explicit Quotients(float divisor) : s(divisor), fast(MODERATE || (divisor >= 0x1p-100f && divisor <= 0x1p+100f)) {
     const float r0 = __builtin_amdgcn_rcpf(s);
     r = __builtin_fmaf(__builtin_fmaf(-s, r0, 1.f), r0, r0);
   }

@@ -213,9 +213,14 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
     const int p1 = __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1) + 1);
     if (FP8) {
       const int pid = (q4 < 2) ? p0 : p1;        // tokens 0-15 of the block sit in its first page
-      const size_t at = HEAD ? (size_t)pid * hkv + g : (size_t)pid;
-      ksc[stage] = a.k_scale[at];
-      vsc[stage] = a.v_scale[at];
+      if constexpr (HEAD) {
+        const int64_t at = (int64_t)pid * hkv + g;
+        ksc[stage] = a.k_scale[at];
+        vsc[stage] = a.v_scale[at];
+      } else {
+        ksc[stage] = a.k_scale[pid];
+        vsc[stage] = a.v_scale[pid];
+      }
     }
     const unsigned char* kt0 = (const unsigned char*)a.k_pages + ((size_t)p0 * hkv + g) * tile_stride;
     const unsigned char* kt1 = (const unsigned char*)a.k_pages + ((size_t)p1 * hkv + g) * tile_stride;
@@ -385,9 +390,9 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
     }
     // This lane now holds, for head r16, the scores of tokens tok0 + q4*8 + (0..7):
     // s[0][i] -> +i, s[1][i] -> +4+i.
-    const int tbase = tok0 + q4 * 8;
     const float sc = HEAD ? q_unit * kscale : FP8 ? a.scale_log2 * kscale : a.scale_log2;
     float vs = FP8 ? vscale : 1.f, lvs = 0.f, ivs = 1.f;
+    const int tbase = tok0 + q4 * 8;
     if constexpr (HEAD) {
       if (tbase >= len) vs = 1.f;                  // (a page that this row does not have: its scale may be anything)
       lvs = __builtin_amdgcn_logf(vs);

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(const KvWriteArgs a)
           }
         }
       }
-      const Quotients by_scale(s_new);
+      const Quotients<> by_scale(s_new);
       auto emit = [&](const uintx4 raw) {
         float x[8];
         bf16x8_to_float(raw, x);

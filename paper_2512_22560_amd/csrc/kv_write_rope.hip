@@ -6,11 +6,14 @@
 // absmax / 448 or / 127 of the head's new rows in the page, never below kLeastHeadScale and, where the page already holds tokens,
 // never below the old one; if it grew, the codes already there are quantised again.
 //
-// One workgroup per (trajectory, page that receives new tokens, and: K, V, or kQueryHeads query heads); the page belongs to that
-// trajectory alone, so nothing here needs a global atomic.  A row of D elements is the work of D / 8 lanes, eight elements to a
-// lane: two runs of four whose elements are each other's partners, so that a rotation needs no exchange between lanes.  The
-// groups of lanes are dealt to the page's new slots first and the rest of them to heads, so that a lane keeps its slot, and with
-// it the cosines and sines of its token, over all heads it walks.
+// Two kinds of workgroups share a launch.  Keys and values: one workgroup per (page that receives new tokens, pool); the page
+// belongs to one trajectory alone, so nothing here needs a global atomic.  Queries: one wave per token and some of its heads, which
+// lie side by side, so that a wave reads and writes kilobytes in a row, and what the token's position takes is looked up once.
+// A row of D elements is the work of D / 8 lanes, eight elements to a lane: two runs of four whose elements are each other's
+// partners, so that a rotation needs no exchange between lanes.  In a page's workgroup the groups of lanes are dealt to the new
+// slots first and the rest of them to heads, so that a lane keeps its slot over all heads it walks.
+#include <algorithm>
+
 #include "codes_device.h"
 
 namespace rollattn {
@@ -18,8 +21,11 @@ namespace rollattn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kQueryHeads = 16;   // query heads per workgroup
-constexpr int kKeep = 8;          // heads of a lane that are held at once
+constexpr int kWaves = kThreads / 64;
+constexpr int kKeep = 8;          // rows of a lane that are under way at once
+constexpr int kRound = 4;         // heads of a lane whose rows are held until their scales are known
+constexpr int kQueryWaves = 8192; // queries: waves wanted where there are few tokens
+constexpr int kMostPages = 4096;  // pages of a trajectory with a workgroup of their own
 
 template <int SRC_BYTES>
 struct Raw {                      // a lane's eight elements as they come
@@ -79,6 +85,133 @@ struct Turn {
   }
 };
 
+// The cosines and sines of four pairs from j on; place: the token's place in its context, token: its number among the new ones.
+__device__ __forceinline__ void look_up(const RopeWriteArgs& a, int j, int place, int64_t token, Turn& turn) {
+  const int half = a.rot_dim / 2;
+  const unsigned int last = (unsigned int)a.num_positions - 1;
+  auto row = [&](int axis) {
+    const int at = a.positions ? a.positions[(int64_t)axis * a.total_q + token] : place;
+    return a.cos_sin + (size_t)min((unsigned int)at, last) * a.rot_dim + j;
+  };
+  const unsigned int axes = a.pair_axes[j / 16] >> (j % 16 * 2) & 0xff;
+  if (axes == (axes & 3) * 0x55) {                    // one axis for the four
+    const float* r = row(axes & 3);
+    typedef float floatx4 __attribute__((ext_vector_type(4)));
+    const floatx4 c = *(const floatx4*)r, s = *(const floatx4*)(r + half);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      turn.c[i] = c[i];
+      turn.s[i] = s[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* r = row(axes >> (2 * i) & 3) + i;
+      turn.c[i] = r[0];
+      turn.s[i] = r[half];
+    }
+  }
+}
+
+// What a lane knows of the rows it works on: where its two runs of four start, and whether they are partners.
+struct Lane {
+  int e0, e1;
+  bool turns;
+  __device__ __forceinline__ Lane(const RopeWriteArgs& a, int col, bool rotate) {
+    turns = rotate && col * 8 < a.rot_dim;
+    e0 = col * 8;
+    e1 = e0 + 4;
+    if (turns && !a.interleaved) {
+      e0 = col * 4;
+      e1 = e0 + a.rot_dim / 2;
+    }
+  }
+};
+
+template <int SRC_BYTES>
+__device__ __forceinline__ Raw<SRC_BYTES> fetch(const Lane& lane, const void* rows, int64_t element) {
+  const unsigned char* p = (const unsigned char*)rows + element * SRC_BYTES;
+  Raw<SRC_BYTES> r;
+  r.lo = *(const typename Raw<SRC_BYTES>::half*)(p + lane.e0 * SRC_BYTES);
+  r.hi = *(const typename Raw<SRC_BYTES>::half*)(p + lane.e1 * SRC_BYTES);
+  return r;
+}
+
+// A row of the source type, turned where it has to be, at p.
+template <int SRC_BYTES>
+__device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, const Turn& turn, void* p, Raw<SRC_BYTES> r) {
+  if (lane.turns) {
+    float x[8];
+    to_float<SRC_BYTES>(r, x);
+    turn.apply(x, a.interleaved);
+    if constexpr (SRC_BYTES == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r.lo[i] = __float_as_uint(x[i]);
+        r.hi[i] = __float_as_uint(x[4 + i]);
+      }
+    } else {
+      r.lo = to_bf16x4(x);
+      r.hi = to_bf16x4(x + 4);
+    }
+  }
+  *(typename Raw<SRC_BYTES>::half*)((unsigned char*)p + lane.e0 * SRC_BYTES) = r.lo;
+  *(typename Raw<SRC_BYTES>::half*)((unsigned char*)p + lane.e1 * SRC_BYTES) = r.hi;
+}
+
+// The place in its context of new token `token`, the same in all lanes: the trajectory it belongs to is the last one that starts at
+// or before it and has new tokens; 64 starts are looked at a time.
+__device__ __forceinline__ int place_of(const RopeWriteArgs& a, int token) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = a.batch;                            // among trajectories [lo, lo + n), starts in order
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const bool before = at < n && a.q_offsets[lo + at] <= token;
+    const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1, 0);
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return a.ctx_lens[lo] - a.q_lens[lo] + token - a.q_offsets[lo];
+}
+
+template <int D, int SRC_BYTES>
+__device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned int block) {
+  constexpr int kLanes = D / 8, kRows = 64 / kLanes;  // lanes of a row, heads under way at a time
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned int unit = block * kWaves + wave;
+  const int token = __builtin_amdgcn_readfirstlane((int)(unit / (unsigned int)a.head_parts)), part = (int)(unit - (unsigned int)token * a.head_parts);
+  if (token >= a.total_q) return;
+  const int h0 = part * a.part_heads, h1 = min(a.hq, h0 + a.part_heads);
+  const int col = (threadIdx.x & 63) % kLanes, sub = (threadIdx.x & 63) / kLanes;
+  const Lane lane(a, col, true);
+  Turn turn;
+  auto load = [&](Raw<SRC_BYTES> (&r)[kKeep], int h) {
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i)
+      if (h + i * kRows < h1) r[i] = fetch<SRC_BYTES>(lane, a.q, token * a.q_stride + (int64_t)min(h + i * kRows + sub, h1 - 1) * D);
+  };
+  Raw<SRC_BYTES> r[kKeep] = {};
+  load(r, h0);                                        // (on their way while the position is looked up)
+  const int place = a.positions ? 0 : place_of(a, token);
+  if (lane.turns) look_up(a, col * 4, place, token, turn);
+  for (int h = h0; h < h1; h += kKeep * kRows) {
+    if (h > h0) load(r, h);
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+      const int head = h + i * kRows + sub;
+      if (head < h1) store<SRC_BYTES>(a, lane, turn, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
+    }
+  }
+}
+
+// Bound by memory where there are many tokens, by the latency of one chain (lengths, page id and rows, maximum, codes) where there
+// are few.  What the large cases gained by, 22150 tokens of 64/4/128 into E4M3 pages (three axes; 794 MB) and 26835 of 32/8/128 into
+// int8 ones (605 MB), us a call: a workgroup per page and 16 heads, heads outermost 171 and 138 (at any time all of them read and write
+// the same few kilobytes of every token's row, a part of the memory's channels), heads innermost 151 and 148 (keys on some XCDs,
+// queries on others), in 13 parts instead of 4 to 10: 154 and worse, each looking positions up again; queries by tokens, behind the
+// pages 156 and 148, among them 139 and 117: 5.7 and 5.2 TB/s where a streaming pass over as many bytes reaches 6.2.  Fewer
+// workgroups that take several pages each: slower by 5 to 20 %.  Rows held as floats until their scale is known instead of
+// turned twice: three workgroups per CU instead of five.
 // POOL: -1 the source type, else a KvKind
 template <int D, int SRC_BYTES, int POOL>
 __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWriteArgs a) {
@@ -86,129 +219,97 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   constexpr bool kInt8 = POOL == kKvInt8Head;
   constexpr int kLanes = D / 8;                 // lanes of a row
   constexpr int kGroups = kThreads / kLanes;    // rows under way at a time
-  constexpr int kMost = kKeep * kGroups;        // heads of a round, at most
-  const int b = blockIdx.y;
-  int n = a.q_lens[b], len = a.ctx_lens[b], q_off = a.q_offsets[b];
+  constexpr int kMost = kRound * kGroups;       // heads of a round, at most
+  // Workgroups go to the XCDs in turn, so in groups of eight either kind has one on each; the groups of pages are spread evenly
+  // among those of queries.
+  const unsigned int g = blockIdx.x / kXcds, at = blockIdx.x % kXcds;
+  const unsigned int pages_before = (unsigned int)((uint64_t)g * a.page_share >> 32), pages_then = (unsigned int)((uint64_t)(g + 1) * a.page_share >> 32);
+  if (pages_before == pages_then) {
+    turn_queries<D, SRC_BYTES>(a, (g - pages_before) * kXcds + at);
+    return;
+  }
+  // eight pages' keys, then their values
+  const int pool = pages_before & 1;
+  const unsigned int page_unit = (pages_before / 2) * kXcds + at;
+  const int b = __builtin_amdgcn_readfirstlane((int)(page_unit / (unsigned int)a.pages)), page_x = (int)page_unit - b * a.pages;
+  if (b >= a.batch) return;
+  // (the constant address space: nobody writes lengths or the table during the call, and scalar loads stay out of the rows' way)
+  typedef const __attribute__((address_space(4))) int32_t* const_i32_p;
+  int n = ((const_i32_p)a.q_lens)[b], len = ((const_i32_p)a.ctx_lens)[b], q_off = ((const_i32_p)a.q_offsets)[b];
   asm volatile("" : "+s"(n), "+s"(len), "+s"(q_off));   // arrived: one wait for all of them
-  const int first = len - n;
-  const int page_i = first / kPageSize + blockIdx.x;
-  if (n <= 0 || page_i * kPageSize >= len) return;
+  if (n <= 0) return;
+  const int first = len - n, hkv = a.hkv;
+  const void* rows = pool ? a.v_new : a.k_new;
+  const int64_t stride = pool ? a.v_stride : a.k_stride;
+  const int group = (int)threadIdx.x / kLanes, col = (int)threadIdx.x % kLanes;
+  const bool rotate = a.cos_sin != nullptr && pool == 0;
+  const Lane lane(a, col, rotate);
+  const bool turns = lane.turns;
+  const int e0 = lane.e0, e1 = lane.e1;
+  for (int page_i = first / kPageSize + page_x; page_i * kPageSize < len; page_i += a.pages) {
+  const bool another = page_i != first / kPageSize + page_x;
   const int lo = max(first, page_i * kPageSize), hi = min(len, (page_i + 1) * kPageSize);
   const int s0 = lo - page_i * kPageSize, slots = hi - lo;
-  const int group = (int)threadIdx.x / kLanes, col = (int)threadIdx.x % kLanes;
   const int side = kGroups / slots;             // heads under way at a time
   const int slot = group % slots, head0 = group / slots;
   const bool idle = head0 >= side;
   const int64_t token = (int64_t)q_off + lo - first + slot;
-  const bool rotate = a.cos_sin != nullptr && blockIdx.z != 1;
-  const int rotating = rotate ? a.rot_dim / 8 : 0;      // lanes of a row that hold pairs
-  int e0 = col * 8, e1 = e0 + 4;                        // where the lane's two runs of four start
-  if (!a.interleaved && col < rotating) {
-    e0 = col * 4;
-    e1 = e0 + a.rot_dim / 2;
-  }
+  const int64_t page_id = ((const_i32_p)a.page_table)[(size_t)b * a.max_pages + page_i];
   Turn turn;
-  if (col < rotating) {
-    const int half = a.rot_dim / 2, j = col * 4;
-    const unsigned int last = (unsigned int)a.num_positions - 1;
-    if (!a.positions) {
-      const float* row = a.cos_sin + (size_t)min((unsigned int)(lo + slot), last) * a.rot_dim + j;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        turn.c[i] = row[i];
-        turn.s[i] = row[half + i];
-      }
-    } else {
-      const unsigned int word = a.pair_axes[j / 16] >> (j % 16 * 2);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int axis = word >> (2 * i) & 3;
-        const float* row = a.cos_sin + (size_t)min((unsigned int)a.positions[(int64_t)axis * a.total_q + token], last) * a.rot_dim + j + i;
-        turn.c[i] = row[0];
-        turn.s[i] = row[half];
-      }
-    }
-  }
-  auto fetch = [&](const void* rows, int64_t stride, int head) {
-    const unsigned char* p = (const unsigned char*)rows + (token * stride + (int64_t)head * D) * SRC_BYTES;
-    Raw<SRC_BYTES> r;
-    r.lo = *(const typename Raw<SRC_BYTES>::half*)(p + e0 * SRC_BYTES);
-    r.hi = *(const typename Raw<SRC_BYTES>::half*)(p + e1 * SRC_BYTES);
-    return r;
-  };
-  // A row of the source type, at p.
-  auto store = [&](void* p, Raw<SRC_BYTES> r) {
-    if (col < rotating) {
-      float x[8];
-      to_float<SRC_BYTES>(r, x);
-      turn.apply(x, a.interleaved);
-      if constexpr (SRC_BYTES == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          r.lo[i] = __float_as_uint(x[i]);
-          r.hi[i] = __float_as_uint(x[4 + i]);
-        }
-      } else {
-        r.lo = to_bf16x4(x);
-        r.hi = to_bf16x4(x + 4);
-      }
-    }
-    *(typename Raw<SRC_BYTES>::half*)((unsigned char*)p + e0 * SRC_BYTES) = r.lo;
-    *(typename Raw<SRC_BYTES>::half*)((unsigned char*)p + e1 * SRC_BYTES) = r.hi;
-  };
-  // All heads of `heads` from h0 on, several under way at a time, from rows to where at(head) says.
-  auto copy = [&](const void* rows, int64_t stride, int h0, int heads, auto&& at) {
-    constexpr int kBatch = 4;
-    if (idle) return;
-    for (int h = h0 + head0; h < heads; h += kBatch * side) {
-      Raw<SRC_BYTES> r[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) r[i] = fetch(rows, stride, min(h + i * side, heads - 1));
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        if (h + i * side < heads) store(at(h + i * side), r[i]);
-    }
-  };
-
-  if (blockIdx.z >= 2) {
-    const int h0 = ((int)blockIdx.z - 2) * kQueryHeads;
-    copy(a.q, a.q_stride, h0, min(h0 + kQueryHeads, a.hq),
-         [&](int h) { return (unsigned char*)a.q_out + (token * a.hq + h) * D * SRC_BYTES; });
-    return;
-  }
-  const int pool = blockIdx.z, hkv = a.hkv;
-  const void* rows = pool ? a.v_new : a.k_new;
-  const int64_t stride = pool ? a.v_stride : a.k_stride;
-  const int64_t page_id = a.page_table[(size_t)b * a.max_pages + page_i];
+  if (turns) look_up(a, col * 4, lo + slot, token, turn);
+  auto fetch_row = [&](int head) { return fetch<SRC_BYTES>(lane, rows, token * stride + (int64_t)head * D); };
   unsigned char* tile = (unsigned char*)(pool ? a.v_pages : a.k_pages) + (size_t)page_id * hkv * kPageSize * D * (kCodes ? 1 : SRC_BYTES);
   if constexpr (!kCodes) {
-    copy(rows, stride, 0, hkv, [&](int h) { return tile + ((size_t)h * kPageSize + s0 + slot) * D * SRC_BYTES; });
+    // several heads under way at a time
+    if (!idle)
+      for (int h = head0; h < hkv; h += kKeep * side) {
+        Raw<SRC_BYTES> r[kKeep] = {};
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i)
+          if (h - head0 + i * side < hkv) r[i] = fetch_row(min(h + i * side, hkv - 1));
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i)
+          if (h + i * side < hkv) store<SRC_BYTES>(a, lane, turn, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
+      }
   } else {
     static_assert(SRC_BYTES == 2, "codes are made of bf16 rows");
-    // of a round's heads (one entry where the scale is the page's): largest magnitude, then the old and the new scale
-    __shared__ unsigned int top[kMost];
+    // of a round's heads: the rows' largest magnitudes; then the old and the new scale (one entry where the scale is the page's)
+    __shared__ float row_top[kRound][kGroups];
     __shared__ float old_scale[kMost], new_scale[kMost];
     float* const scales = (pool ? a.v_scale : a.k_scale) + page_id * (kHeadScales ? hkv : 1);
     constexpr float kMax = kInt8 ? kInt8Max : kE4m3Max;
-    auto rotated = [&](int head, float (&x)[8]) {
-      to_float<2>(fetch(rows, stride, head), x);
-      if (col < rotating) turn.apply(x, a.interleaved);
+    auto rotated = [&](const Raw<SRC_BYTES>& r, float (&x)[8]) {
+      to_float<2>(r, x);
+      if (turns) turn.apply(x, a.interleaved);
     };
     auto encode4 = [&](const float* x) { return kInt8 ? encode4_int8(x) : encode4_e4m3(x); };
-    // of `count` scales from `first` on: each thread one
-    auto settle = [&](int first, int count) {
-      for (int i = threadIdx.x; i < count; i += kThreads) {
-        const float amax = __uint_as_float(top[i]);
-        float need = amax / kMax;
-        if (kHeadScales) need = fmaxf(need, kLeastHeadScale);
-        else if (s0 == 0 && !(amax > 0.f)) need = 1.f;
-        const float before = s0 ? scales[first + i] : need;
-        old_scale[i] = before;
-        new_scale[i] = need > before ? need : before;
-        scales[first + i] = new_scale[i];
-      }
+    auto settled = [&](float amax, float before) {
+      float need = amax / kMax;
+      if (kHeadScales) need = fmaxf(need, kLeastHeadScale);
+      else if (s0 == 0 && !(amax > 0.f)) need = 1.f;
+      return s0 == 0 || need > before ? need : before;
     };
-    // the codes already in slots [0, s0) of `count` heads from `first` on whose scale grew: code <- enc(dec(code) * old / new)
+    // eight codes at p: code <- enc(dec(code) * old / new)
+    auto again8 = [&](unsigned char* at, float before, float now) {
+      uintx2* p = (uintx2*)at;
+      const uintx2 w = *p;
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if constexpr (kInt8) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * k + e] = (float)(int8_t)(w[k] >> (8 * e));
+        } else {
+          const floatx2 f0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), f1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+          x[4 * k] = f0[0]; x[4 * k + 1] = f0[1]; x[4 * k + 2] = f1[0]; x[4 * k + 3] = f1[1];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= before;
+      Quotients<kHeadScales>(now).divide(x);
+      *p = uintx2{encode4(x), encode4(x + 4)};
+    };
+    // the codes already in slots [0, s0) of `count` heads from `first` on whose scale grew
     auto again = [&](int first, int count) {
       if (!s0) return;
       const int chunks = count * s0 * (D / 8);
@@ -216,85 +317,118 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
         const int row = c / (D / 8), at = c % (D / 8);
         const int h = row / s0, i = kHeadScales ? h : 0;
         const float before = old_scale[i], now = new_scale[i];
-        if (!(now > before)) continue;
-        uintx2* p = (uintx2*)(tile + ((size_t)(first + h) * kPageSize + row % s0) * D + at * 8);
-        const uintx2 w = *p;
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if constexpr (kInt8) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * k + e] = (float)(int8_t)(w[k] >> (8 * e));
-          } else {
-            const floatx2 f0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), f1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
-            x[4 * k] = f0[0]; x[4 * k + 1] = f0[1]; x[4 * k + 2] = f1[0]; x[4 * k + 3] = f1[1];
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (x[e] * before) / now;
-        *p = uintx2{encode4(x), encode4(x + 4)};
+        if (now > before) again8(tile + ((size_t)(first + h) * kPageSize + row % s0) * D + at * 8, before, now);
       }
     };
-    const int round = kKeep * side;               // heads of a round
+    const int round = kRound * side;               // heads of a round
+    // the largest magnitude of a row, in all of its lanes
     auto largest = [&](const float (&x)[8]) {
       float m = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = fmaxf(m, __builtin_fabsf(x[i]));
-      return __float_as_uint(m);
+      int t = __float_as_int(m);                  // (as integers they order the same)
+      t = max(t, __builtin_amdgcn_mov_dpp(t, 0xb1, 0xf, 0xf, true));      // the neighbour,
+      t = max(t, __builtin_amdgcn_mov_dpp(t, 0x4e, 0xf, 0xf, true));      // ... the other two of four,
+      t = max(t, __builtin_amdgcn_mov_dpp(t, 0x141, 0xf, 0xf, true));     // ... the other four of eight,
+      if constexpr (kLanes == 16) t = max(t, __builtin_amdgcn_mov_dpp(t, 0x140, 0xf, 0xf, true));
+      return __int_as_float(t);
     };
-    auto emit = [&](int head, float (&x)[8], float scale) {
-      Quotients(scale).divide(x);
+    auto emit = [&](int head, const Raw<SRC_BYTES>& r, float scale) {
+      float x[8];
+      rotated(r, x);
+      Quotients<kHeadScales>(scale).divide(x);
       unsigned char* dst = tile + ((size_t)head * kPageSize + s0 + slot) * D;
       *(unsigned int*)(dst + e0) = encode4(x);
       *(unsigned int*)(dst + e1) = encode4(x + 4);
     };
     if constexpr (kHeadScales) {
+      if (slots == 1) {
+        // a lone token: a head is one row, whose lanes know all there is to know
+        for (int h = head0; h < hkv; h += side) {
+          const float before = s0 ? scales[h] : 0.f;
+          const Raw<SRC_BYTES> r = fetch_row(h);
+          float x[8];
+          rotated(r, x);
+          const float now = settled(largest(x), before);
+          if (s0 && now > before)
+            for (int t = 0; t < s0; ++t) again8(tile + ((size_t)h * kPageSize + t) * D + col * 8, before, now);
+          emit(h, r, now);
+          if (col == 0) scales[h] = now;          // (its lanes read the old one together)
+        }
+        continue;
+      }
       for (int r0 = 0; r0 < hkv; r0 += round) {
         const int count = min(round, hkv - r0);
-        if (r0) __syncthreads();
-        for (int i = threadIdx.x; i < count; i += kThreads) top[i] = 0;
-        __syncthreads();
-        float x[kKeep][8];
+        float before = 0.f;
+        if (s0 && (int)threadIdx.x < count) before = scales[r0 + threadIdx.x];
+        if (r0 || another) __syncthreads();
+        Raw<SRC_BYTES> keep[kRound] = {};       // (what is not loaded is nothing: else the rows of the round before, all the way)
         if (!idle) {
 #pragma unroll
-          for (int k = 0; k < kKeep; ++k)
-            if (head0 + k * side < count) {
-              rotated(r0 + head0 + k * side, x[k]);
-              atomicMax(&top[head0 + k * side], largest(x[k]));
+          for (int k = 0; k < kRound; ++k)
+            if (k * side < count) keep[k] = fetch_row(r0 + min(head0 + k * side, count - 1));
+#pragma unroll
+          for (int k = 0; k < kRound; ++k)
+            if (k * side < count) {
+              float x[8];
+              rotated(keep[k], x);
+              const float m = largest(x);
+              if (col == 0) row_top[k][group] = m;
+              __builtin_amdgcn_sched_barrier(0);
             }
         }
         __syncthreads();
-        settle(r0, count);
+        if ((int)threadIdx.x < count) {
+          const int k = (int)threadIdx.x / side, g = ((int)threadIdx.x - k * side) * slots;
+          float m = row_top[k][g];
+          for (int i = 1; i < slots; ++i) m = fmaxf(m, row_top[k][g + i]);
+          const float now = settled(m, before);
+          old_scale[threadIdx.x] = s0 ? before : now;
+          new_scale[threadIdx.x] = now;
+          scales[r0 + threadIdx.x] = now;
+        }
         __syncthreads();
         again(r0, count);
         if (!idle) {
+          // (turned once more: kept as floats over the barriers, rows would take twice the registers)
 #pragma unroll
-          for (int k = 0; k < kKeep; ++k)
-            if (head0 + k * side < count) emit(r0 + head0 + k * side, x[k], new_scale[head0 + k * side]);
+          for (int k = 0; k < kRound; ++k) asm volatile("" : "+v"(keep[k].lo), "+v"(keep[k].hi));
+#pragma unroll
+          for (int k = 0; k < kRound; ++k)
+            if (head0 + k * side < count) {
+              emit(r0 + head0 + k * side, keep[k], new_scale[head0 + k * side]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
         }
       }
     } else {
       // one scale for the page: the largest magnitude of all heads first
-      if (threadIdx.x == 0) top[0] = 0;
-      __syncthreads();
-      unsigned int most = 0;
-      float x[8];
+      float before = 0.f;
+      if (s0 && threadIdx.x == 0) before = scales[0];
+      float most = 0.f;
       if (!idle)
         for (int h = head0; h < hkv; h += side) {
-          rotated(h, x);
-          most = max(most, largest(x));
+          float x[8];
+          rotated(fetch_row(h), x);
+          most = fmaxf(most, largest(x));
         }
-      atomicMax(&top[0], most);
+      if (another) __syncthreads();
+      if (col == 0) row_top[0][group] = most;
       __syncthreads();
-      settle(0, 1);
+      if (threadIdx.x == 0) {
+        float m = row_top[0][0];
+        for (int i = 1; i < kGroups; ++i) m = fmaxf(m, row_top[0][i]);
+        const float now = settled(m, before);
+        old_scale[0] = s0 ? before : now;
+        new_scale[0] = now;
+        scales[0] = now;
+      }
       __syncthreads();
       again(0, hkv);
       if (!idle)
-        for (int h = head0; h < hkv; h += side) {
-          rotated(h, x);
-          emit(h, x, new_scale[0]);
-        }
+        for (int h = head0; h < hkv; h += side) emit(h, fetch_row(h), new_scale[0]);
     }
+  }
   }
 }
 
@@ -317,12 +451,24 @@ hipError_t launch_d(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid, 
 
 }  // namespace
 
-hipError_t launch_kv_write_rope(const RopeWriteArgs& a, int32_t batch, int32_t max_q_len, int head_dim, int src_bytes, int pool,
-                                hipStream_t s) {
+hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s) {
+  RopeWriteArgs a = args;
   // a run of n tokens touches at most this many pages, wherever it starts
-  const unsigned pages = max_q_len > 0 ? (unsigned)(((int64_t)max_q_len + kPageSize - 2) / kPageSize + 1) : 1;
-  const unsigned queries = a.q ? (unsigned)((a.hq + kQueryHeads - 1) / kQueryHeads) : 0;
-  const dim3 grid(pages, (unsigned)batch, 2 + queries);
+  const int64_t longest = std::min(max_q_len, a.total_q);
+  a.pages = longest > 0 ? (int32_t)std::min<int64_t>((longest + kPageSize - 2) / kPageSize + 1, kMostPages) : 1;
+  const int64_t page_groups = ((int64_t)a.pages * a.batch + kXcds - 1) / kXcds * 2;
+  int64_t groups = page_groups;
+  if (a.q) {
+    // a wave takes so many heads of a token that kKeep rows of each of its lanes hold them, fewer where waves are few
+    const int rows = 64 / (head_dim / 8), most = (a.hq + rows - 1) / rows;
+    const int64_t parts = std::clamp<int64_t>(kQueryWaves / a.total_q, (most + kKeep - 1) / kKeep, most);
+    a.part_heads = (int)((most + parts - 1) / parts) * rows;
+    a.head_parts = (a.hq + a.part_heads - 1) / a.part_heads;
+    groups += ((int64_t)a.total_q * a.head_parts + kWaves * kXcds - 1) / (kWaves * kXcds);
+  }
+  if (groups * kXcds > INT32_MAX || (int64_t)a.total_q * a.head_parts > INT32_MAX) return hipErrorInvalidValue;
+  a.page_share = (((uint64_t)page_groups << 32) + groups - 1) / groups;   // (rounded up: behind the last group there have been them all)
+  const dim3 grid((unsigned)(groups * kXcds));
   if (head_dim == 128) return launch_d<128>(a, src_bytes, pool, grid, s);
   if (head_dim == 64) return launch_d<64>(a, src_bytes, pool, grid, s);
   return hipErrorInvalidValue;

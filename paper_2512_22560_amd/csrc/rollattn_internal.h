@@ -193,6 +193,11 @@ struct RopeWriteArgs {
   int64_t q_stride, k_stride, v_stride;   // elements from a token to the next
   int32_t hq, hkv, max_pages, total_q;
   int32_t rot_dim, num_positions;
+  int32_t batch;
+  // set at launch: pages of a trajectory with a workgroup of their own, the share of workgroups that take pages (in 2^-32), and into
+  // how many parts of how many heads a token's queries are cut
+  int32_t pages, head_parts, part_heads;
+  uint64_t page_share;
   uint32_t pair_axes[4];           // two bits per pair
   int32_t interleaved;
 };
@@ -222,8 +227,7 @@ hipError_t launch_kv_write(const void* k_new, const void* v_new, const int32_t* 
                            float* k_scale, float* v_scale, int32_t batch, int32_t hkv, int32_t max_pages,
                            int32_t max_q_len, int head_dim, int src_bytes, bool fp8, hipStream_t s);
 // pool: -1 for one of the source type, else what its codes are (bf16 sources)
-hipError_t launch_kv_write_rope(const RopeWriteArgs& a, int32_t batch, int32_t max_q_len, int head_dim, int src_bytes, int pool,
-                                hipStream_t s);
+hipError_t launch_kv_write_rope(const RopeWriteArgs& a, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s);
 hipError_t launch_merge_states(const void* o1, const float* d1, const void* o2, const float* d2, void* out, float* d_out,
                                long rows, int head_dim, bool f32, hipStream_t s);
 hipError_t launch_check_inputs(const int32_t* page_table, const int32_t* ctx_lens, const int32_t* q_lens,
