@@ -45,10 +45,11 @@
 //     addend as log2(vs), so P comes out of the exponential already weighted for the second
 //     product; the row sum divides each page's share by vs again (four multiplies per block).
 //
-// Pools with a scale for each page and KV head (E4M3 or int8 codes) take the FP8 path with f16 in the place of bf16: a code is exact
-// in either, an int8 one is cheaper to widen, and probabilities keep 11 bits instead of 8.  For f16's range queries are multiplied
-// by a power of two per row (exact; taken back with the page's K scale), and a row's reference is that of the weights p * vs,
-// 2^kWeightBits below the largest when it moves; it moves when a lane's weights of a block add up to more than kHalfSumLimit, so none
+// Pools with a scale for each page and KV head (E4M3 or int8 codes) take the FP8 path with f16 operands in the second product: a code
+// is exact in either, and probabilities keep 11 bits instead of 8.  So are those of the first over int8 codes, which are cheaper to
+// widen that way.  For f16's range queries that meet int8 codes are multiplied by a power of two per wave (exact; taken back with
+// the page's K scale), and a row's reference is that of the weights p * vs,
+// 2^kWeightBits below the largest when it moves; it moves when a lane's weights of a page add up to more than kHalfSumLimit, so none
 // is ever too large for f16, and one 2^-22 of the largest still is a normal number.
 //
 // Half tiles.  A call whose chunks all fit into 128 rows gets tiles of 128 rows: waves w and w + 4 then own the
@@ -114,7 +115,9 @@ __device__ __forceinline__ uint32_t fp8_pair_f16(const uintx4 codes) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[PAIR / 2], 1.0f, PAIR % 2 != 0));
 }
 // The same for sixteen 8-bit integers whose signs have been turned round, so that a byte counts from -128 up: as the low bits of
-// 1024.0 it adds itself to that, and 1152 less is the value.
+// 1024.0 it adds itself to that, and 1152 less is the value, exactly.  (The constants in scalar registers: the loop has no vector
+// ones to spare.  Left out for keys and taken off the scores instead, 1152 is four multiply-adds per page behind the first product,
+// where they cost more than the subtractions here: +2 %.)
 template <int PAIR>
 __device__ __forceinline__ uint32_t int8_pair(const uintx4 turned) {
   uint32_t sel = PAIR % 2 ? 0x04030402u : 0x04010400u, off = 0xe480e480u;
@@ -122,13 +125,13 @@ __device__ __forceinline__ uint32_t int8_pair(const uintx4 turned) {
   const uint32_t w = __builtin_amdgcn_perm(0x64646464u, turned[PAIR / 2], sel);
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, w) + __builtin_bit_cast(halfx2, off));
 }
-// Pair PAIR of a chunk of codes; of int8 ones the even pairs come first and turn the word's signs.
-template <int KV, int PAIR>
+// Pair PAIR of a chunk of codes of either pool; of int8 ones the even pairs come first and turn the word's signs.
+template <int KV, bool IS_V, int PAIR>
 __device__ __forceinline__ uint32_t widen_pair(uintx4& codes) {
   if constexpr (KV == kKvInt8Head) {
     if constexpr (PAIR % 2 == 0) codes[PAIR / 2] ^= 0x80808080u;
     return int8_pair<PAIR>(codes);
-  } else if constexpr (KV == kKvFp8Head) {
+  } else if constexpr (KV == kKvFp8Head && IS_V) {
     return fp8_pair_f16<PAIR>(codes);
   } else {
     return fp8_pair<PAIR>(codes);
@@ -274,7 +277,10 @@ __device__ __forceinline__ decltype(auto) choose(A& a, B& b) {
 template <int D, int KV, bool HALF, bool ONCE, int STEP, bool kOneOfTwo>
 __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, AppendLds<D, kv_is_codes(KV), HALF, STEP>* shared) {
   constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
-  using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;
+  constexpr bool INT8 = KV == kKvInt8Head;
+  using k_op = std::conditional_t<INT8, _Float16, __bf16>;
+  using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
+  using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;  // ... and of the second
   using opx4 = std::conditional_t<HEAD, halfx4, bf16x4>;
   using op = std::conditional_t<HEAD, _Float16, __bf16>;
   auto& a = args_of<kOneOfTwo>(kernel_args);
@@ -418,14 +424,14 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 
   // Rows past the tile's last read that one again: what becomes of them is neither stored nor looked at.  (A branch around each
   // load had one of them waited for before the next was sent.)
-  opx8 qop[kKK];
+  kx8 qop[kKK];
   {
     const int qtok = row_ok ? tok_in_tile : tokens_here - 1, qhead = row_ok ? head : g * group;
     const __bf16* qrow = (const __bf16*)q + ((size_t)(q_off + q0 + qtok) * hq + qhead) * D;
 #pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) qop[kk] = *(const opx8*)(qrow + kk * 16 + h2 * 8);   // bf16 pools: scaled further down; f16: so far only moved
+    for (int kk = 0; kk < kKK; ++kk) qop[kk] = *(const kx8*)(qrow + kk * 16 + h2 * 8);   // bf16 pools: scaled further down; int8: so far only moved
   }
-  float q_unit = 1.f;                            // f16: what a unit of this lane's row is worth
+  float q_unit = 1.f;                            // int8: what a unit of this wave's rows is worth
 
   floatx16 acc[kDT];
 #pragma unroll
@@ -499,11 +505,11 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     uintx4 lo, hi;
     static_for<4>([&](auto m_c) __attribute__((always_inline)) {
       constexpr int m = decltype(m_c)::value;
-      lo[m] = widen_pair<KV, m>(codes);
+      lo[m] = widen_pair<KV, false, m>(codes);
     });
     static_for<4>([&](auto m_c) __attribute__((always_inline)) {
       constexpr int m = decltype(m_c)::value;
-      hi[m] = widen_pair<KV, 4 + m>(codes);
+      hi[m] = widen_pair<KV, false, 4 + m>(codes);
     });
     *lds_at<uintx4>(lo_at, offset) = lo;
     *lds_at<uintx4>(hi_at, offset) = hi;
@@ -606,21 +612,22 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   };
   auto matrix_phase = [&](auto first_c, auto last_c, int kbo, int vbo, auto&& piece) __attribute__((always_inline)) {
     constexpr int T0 = decltype(first_c)::value, T1 = decltype(last_c)::value;
-    opx8 ops[kSteps];
+    opx8 v_ops[kPvSteps];
+    kx8 k_ops[kSteps];
     auto fetch = [&](auto t_c) __attribute__((always_inline)) {
       constexpr int t = decltype(t_c)::value;
       if constexpr (t < kPvSteps) {
-        read_v_operand(vbo, t_c, ops[t]);
+        read_v_operand(vbo, t_c, v_ops[t]);
       } else {
         constexpr int u = t - kPvSteps, kk = u / kSubs, sub = u % kSubs;
-        if constexpr (kk < kKK) ops[t] = *lds_at<const opx8>(kptr[kk], kbo + sub * 32 * kRowBytes);
+        if constexpr (kk < kKK) k_ops[t] = *lds_at<const kx8>(kptr[kk], kbo + sub * 32 * kRowBytes);
       }
     };
     auto fire = [&](auto t_c) __attribute__((always_inline)) {
       constexpr int t = decltype(t_c)::value;
       if constexpr (t < kPvSteps) {
         constexpr int sub = t >> 3, ks = (t >> 2) & 1, dt = t & 3;
-        if constexpr (dt < kDT) acc[dt] = mfma(ops[t], pop[sub][ks], acc[dt]);
+        if constexpr (dt < kDT) acc[dt] = mfma(v_ops[t], pop[sub][ks], acc[dt]);
       } else {
         constexpr int u = t - kPvSteps, kk = u / kSubs, sub = u % kSubs;
         if constexpr (kk < kKK) {
@@ -628,19 +635,19 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
             if constexpr (FP8) {
 #pragma unroll
               for (int i = 0; i < 16; ++i) s[sub][i] = 0.f;
-              s[sub] = mfma(ops[t], qop[kk], s[sub]);
+              s[sub] = mfma(k_ops[t], qop[kk], s[sub]);
             } else {
-              s[sub] = mfma(ops[t], qop[kk], negm);
+              s[sub] = mfma(k_ops[t], qop[kk], negm);
             }
           } else {
-            s[sub] = mfma(ops[t], qop[kk], s[sub]);
+            s[sub] = mfma(k_ops[t], qop[kk], s[sub]);
           }
         }
       }
     };
     static_for<kAhead>([&](auto d_c) __attribute__((always_inline)) {
       constexpr int t = T0 + decltype(d_c)::value;
-      if constexpr (kEarly && T0 == 0) ops[t] = early[t];
+      if constexpr (kEarly && T0 == 0) v_ops[t] = early[t];
       else if constexpr (t < T1) fetch(std::integral_constant<int, t>{});
     });
     __builtin_amdgcn_sched_barrier(0);
@@ -674,7 +681,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     float sc[kPg], lvs[kPg], ivs[kPg];                 // this wave's pages: K scale times softmax scale, log2 of the V scale, its reciprocal
     if constexpr (FP8) {
 #pragma unroll
-      for (int p = 0; p < kPg; ++p) { sc[p] = HEAD ? ksc_cur[p] * q_unit : ksc_cur[p]; lvs[p] = lvs_cur[p]; ivs[p] = ivs_cur[p]; }
+      for (int p = 0; p < kPg; ++p) { sc[p] = INT8 ? ksc_cur[p] * q_unit : ksc_cur[p]; lvs[p] = lvs_cur[p]; ivs[p] = ivs_cur[p]; }
       if (!positive_scale) {                           // rare: scale the scores themselves instead
 #pragma unroll
         for (int sub = 0; sub < kSubs; ++sub)
@@ -717,7 +724,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
           if ((i & 7) == 0) psum[pg] = p[sub][i];
           else psum[pg] += p[sub][i];
         }
-      if constexpr (HEAD) weights = kPg == 2 ? psum[0] + psum[1] : (psum[0] + psum[1]) + (psum[kPg - 2] + psum[kPg - 1]);
+      if constexpr (HEAD) weights = fmaxf(fmaxf(psum[0], psum[1]), fmaxf(psum[kPg - 2], psum[kPg - 1]));
       if constexpr (kPg == 2) return FP8 ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1];
       else if constexpr (FP8) return (psum[0] * ivs[0] + psum[1] * ivs[1]) + (psum[2] * ivs[2] + psum[3] * ivs[3]);
       else return (psum[0] + psum[1]) + (psum[2] + psum[3]);
@@ -845,7 +852,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
         if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) put(wptr[j][0], wptr[j][1], 0, k0[j]);
-      if constexpr (HEAD) {
+      if constexpr (INT8) {
         float top = 0.f;
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
@@ -853,14 +860,18 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
           for (int e = 0; e < 8; ++e) top = fmaxf(top, __builtin_fabsf((float)v[e]));
         }
-        const int up = kQueryBits - __builtin_amdgcn_frexp_expf(xor32_max(top));
+        // (the wave's largest element, so that the power stays in a scalar register: exact for all above 2^-32 of it)
+        top = xor32_max(top);
+#pragma unroll
+        for (int x = 16; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const int up = kQueryBits - __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top));
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
           const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) qop[kk][e] = (op)__builtin_amdgcn_ldexpf((float)v[e], up);
+          for (int e = 0; e < 8; ++e) qop[kk][e] = (k_op)__builtin_amdgcn_ldexpf((float)v[e], up);
         }
-        q_unit = __builtin_amdgcn_ldexpf(1.f, -up);
+        q_unit = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(__builtin_amdgcn_ldexpf(1.f, -up))));
       }
     } else {
       // The query rows have been under way as long as the page ids; their scaling (bf16 pools: the scores then leave the
@@ -870,7 +881,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
       for (int kk = 0; kk < kKK; ++kk) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) qop[kk][e] = (op)((float)qop[kk][e] * a.scale_log2);
+        for (int e = 0; e < 8; ++e) qop[kk][e] = (k_op)((float)qop[kk][e] * a.scale_log2);
         asm volatile("" : "+v"(qop[kk]));
       }
 #pragma unroll
@@ -960,13 +971,14 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   auto stage_widen = [&](auto slot_c, auto pos_c) __attribute__((always_inline)) {
     if constexpr (FP8) {
       constexpr int slot = decltype(slot_c)::value, pos = decltype(pos_c)::value;
+      // (int8: two or three instructions for a pair; one at a time, 44 items for a chunk, or the signs in the vector phase: no difference)
       constexpr int kItems = 20 * kLoads;
       static_for<kItems>([&](auto item_c) __attribute__((always_inline)) {
         constexpr int item = decltype(item_c)::value;
         if constexpr (item * 31 / kItems == pos) {
           constexpr int j = item % kLoads, part = item / kLoads / 5, m = item / kLoads % 5;   // the halves of K's chunk, then V's
           if constexpr (m < 4) {
-            wide[j][m] = widen_pair<KV, (part & 1) * 4 + m>((part < 2 ? kreg : vreg)[slot][j]);
+            wide[j][m] = widen_pair<KV, part >= 2, (part & 1) * 4 + m>((part < 2 ? kreg : vreg)[slot][j]);
           } else if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) {
             if constexpr (part < 2) *lds_at<uintx4>(wptr[j][part], ring(slot_c, c1)) = wide[j];
             else *lds_at<uintx4>(part == 2 ? wptr[j][2] : flip(wptr[j][2], 16), ring(slot_c, c0)) = wide[j];

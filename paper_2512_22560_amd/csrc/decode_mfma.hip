@@ -17,9 +17,11 @@
 // softmax state (running max, running sum, rescale factor) is one scalar per lane and P
 // feeds the second product straight from the first one's accumulator registers.
 //
-// Pools with a scale for each page and KV head (E4M3 or int8 codes) are widened to f16 instead of bf16: every code is exact in
-// either, and the weights of the second product keep 11 bits instead of 8.  What f16 lacks is range, so
-//   queries are multiplied by a power of two per head that puts the largest element below 2^15 (exact; taken back on the scores),
+// Over pools with a scale for each page and KV head (E4M3 or int8 codes) the second product is one of f16 instead of bf16: every
+// code is exact in either, and the weights keep 11 bits instead of 8.  So is the first over int8 codes, which are cheaper to widen
+// that way.  What f16 lacks is range, so
+//   queries that meet int8 codes are multiplied by a power of two per head that puts the largest element below 2^15 (exact; taken
+//   back on the scores),
 //   the running reference is that of the weights p * vs, scores plus log2 of the V scale, less kWeightBits: the largest weight is
 //   2^kWeightBits, and one of 2^-28 of it is still a normal number; the row sum takes p = weight / vs.
 #include <type_traits>
@@ -106,7 +108,7 @@ __device__ __forceinline__ halfx8 fp8x8_to_f16(uint32_t lo, uint32_t hi) {
 }
 
 // Eight 8-bit integers to f16, exactly: with the sign turned round a byte counts from -128 up, as the low bits of 1024.0 it adds
-// itself to that, and 1152 less is the value.
+// itself to that, and 1152 less is the value.  (Left out for keys and taken off the scores instead: 73.0 -> 72.6 us, not worth it.)
 __device__ __forceinline__ halfx8 int8x8_to_f16(uint32_t lo, uint32_t hi) {
   lo ^= 0x80808080u;
   hi ^= 0x80808080u;
@@ -118,9 +120,14 @@ __device__ __forceinline__ halfx8 int8x8_to_f16(uint32_t lo, uint32_t hi) {
   return halfx8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Eight codes as an operand of the matrix core, and its product with another.
+// Eight codes as an operand of the first or second product, and the product with another.
 template <int KV>
-__device__ __forceinline__ auto widen8(uint32_t lo, uint32_t hi) {
+__device__ __forceinline__ auto widen_k8(uint32_t lo, uint32_t hi) {
+  if constexpr (KV == kKvInt8Head) return int8x8_to_f16(lo, hi);
+  else return fp8x8_to_bf16(lo, hi);
+}
+template <int KV>
+__device__ __forceinline__ auto widen_v8(uint32_t lo, uint32_t hi) {
   if constexpr (KV == kKvFp8Head) return fp8x8_to_f16(lo, hi);
   else if constexpr (KV == kKvInt8Head) return int8x8_to_f16(lo, hi);
   else return fp8x8_to_bf16(lo, hi);
@@ -154,7 +161,9 @@ template <int D, int KV, bool STREAM, bool WHOLE, bool FOLD>
 __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 start, int worker, unsigned char* const k_lds) {
   static_assert(WHOLE || !FOLD, "cut rows are folded by the merge");
   constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
-  using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;
+  constexpr bool INT8 = KV == kKvInt8Head;
+  using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
+  using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;  // ... and of the second
   using G_ = Geo<D, FP8>;
   int tid = lane_id();
   asm volatile("" : "+v"(tid));   // (what is worked out from it stays in this instance: shared by both in front of the branch, it would not fit the registers)
@@ -273,8 +282,8 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
   };
 
   // ---- consumer state
-  opx8 qop[G_::kKK];         // Q^T as the B operand: lane (head r16, quarter q4), 8 dims per step
-  float q_unit = 1.f;        // f16: what a unit of this lane's head is worth
+  kx8 qop[G_::kKK];          // Q^T as the B operand: lane (head r16, quarter q4), 8 dims per step
+  float q_unit = 1.f;        // int8: what a unit of this lane's head is worth
   floatx4 acc[G_::kDT];      // O^T: lane (head r16, quarter q4) holds dims dt*16 + q4*4 + (0..3)
   float m_run = -INFINITY;   // running max (log2 units) of this lane's head
   float l_run = 0.f;         // this lane's share of the running sum
@@ -296,10 +305,10 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
           v = *(const bf16x8*)(qrow + (kk * 4 + q4) * 8);
         }
       }
-      if constexpr (!HEAD) qop[kk] = v;
+      if constexpr (!INT8) qop[kk] = v;
       else qop[kk] = __builtin_bit_cast(halfx8, v);      // (as it came, until all of the head is there)
     }
-    if constexpr (HEAD) {
+    if constexpr (INT8) {
       float top = 0.f;
 #pragma unroll
       for (int kk = 0; kk < G_::kKK; ++kk) {
@@ -376,21 +385,21 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
         for (int p = 0; p < G_::kChunks / 4; ++p) {
           const int c = ((p * 4 + q4) ^ key) & (G_::kChunks - 1);
           const uint4 raw = *(const uint4*)(rowp + c * 16);
-          s[e] = mfma(widen8<KV>(raw.x, raw.y), qop[2 * p], s[e]);
-          s[e] = mfma(widen8<KV>(raw.z, raw.w), qop[2 * p + 1], s[e]);
+          s[e] = mfma(widen_k8<KV>(raw.x, raw.y), qop[2 * p], s[e]);
+          s[e] = mfma(widen_k8<KV>(raw.z, raw.w), qop[2 * p + 1], s[e]);
         }
       } else {
 #pragma unroll
         for (int kk = 0; kk < G_::kKK; ++kk) {
           const int c = ((kk * 4 + q4) ^ key) & (G_::kChunks - 1);
-          const opx8 kop = *(const opx8*)(rowp + c * 16);
+          const kx8 kop = *(const kx8*)(rowp + c * 16);
           s[e] = mfma(kop, qop[kk], s[e]);
         }
       }
     }
     // This lane now holds, for head r16, the scores of tokens tok0 + q4*8 + (0..7):
     // s[0][i] -> +i, s[1][i] -> +4+i.
-    const float sc = HEAD ? q_unit * kscale : FP8 ? a.scale_log2 * kscale : a.scale_log2;
+    const float sc = INT8 ? q_unit * kscale : FP8 ? a.scale_log2 * kscale : a.scale_log2;
     float vs = FP8 ? vscale : 1.f, lvs = 0.f, ivs = 1.f;
     const int tbase = tok0 + q4 * 8;
     if constexpr (HEAD) {
@@ -434,7 +443,7 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
         const int c = (dt ^ key_v8(t)) & (G_::kChunks - 1);
         const intx2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
             (lds_i2*)(v_lds + t * G_::kRowBytes + c * 16 + (r16 & 1) * 8));
-        vop = widen8<KV>((uint32_t)raw[0], (uint32_t)raw[1]);
+        vop = widen_v8<KV>((uint32_t)raw[0], (uint32_t)raw[1]);
       } else {
         typedef __attribute__((address_space(3))) shortx4 lds_s4;
 #pragma unroll
