@@ -47,8 +47,14 @@
 //
 // Pools with a scale for each page and KV head (E4M3 or int8 codes) take the FP8 path with f16 operands in the second product: a code
 // is exact in either, and probabilities keep 11 bits instead of 8.  So are those of the first over int8 codes, which are cheaper to
-// widen that way.  For f16's range queries that meet int8 codes are multiplied by a power of two per wave (exact; taken back with
-// the page's K scale), and a row's reference is that of the weights p * vs,
+// widen that way.  E4M3 keys are not widened at all (RAW_K): a bf16 number has 8 bits and an E4M3 one 4, so the query is the sum of
+// two E4M3 numbers, its nearest one and the rest (exact for elements down to 2^-10 of the wave's largest; below that the error is at
+// most 2^-18 of the largest, where bf16 itself leaves 2^-9 of each element), and the scores are two products with the codes as they
+// lie in the pool, at twice the depth per instruction and half the bytes in LDS:
+//   64 chunks of 64 .. 1024 tokens behind 2k .. 16k (32/8/128) 2741 -> 2573 us, 32 of 256 behind 8k (64/4/128) 1695 -> 1585, the
+//   shared half of 64 groups of 8 behind 8192 tokens (64/4/128) 138 -> 130; 64 chunks of 8 behind 4k (half tiles) 124.6 -> 126.3.
+// For the ranges of f16 and E4M3 these queries are multiplied by a power of two per wave (exact; taken back with
+// the page's K scale); for that of f16 a row's reference is that of the weights p * vs,
 // 2^kWeightBits below the largest when it moves; it moves when a lane's weights of a page add up to more than kHalfSumLimit, so none
 // is ever too large for f16, and one 2^-22 of the largest still is a normal number.
 //
@@ -76,6 +82,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
 typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
@@ -88,6 +95,7 @@ constexpr float kSumLimit = 16384.f;               // a lane's 32 probabilities 
 
 constexpr float kHalfSumLimit = 65000.f;           // the same for f16 weights, none of which may pass 65504
 constexpr float kWeightBits = 8.f;                 // f16: log2 of a row's largest weight when its reference moves
+constexpr int kDigitBits = 8;                      // E4M3 parts of a query: a wave's largest element is below two to this
 constexpr int kQueryBits = 15;                     // f16: a row's largest query element is below two to this
 
 // Row t of an S^T tile holds this token of its 16-token group: the middle two quads are
@@ -139,6 +147,8 @@ __device__ __forceinline__ uint32_t widen_pair(uintx4& codes) {
 }
 
 __device__ __forceinline__ floatx16 mfma(bf16x8 x, bf16x8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
+// E4M3 codes times E4M3 codes, 64 deep
+__device__ __forceinline__ floatx16 mfma(intx8 x, intx8 y, floatx16 z) { return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, z, 0, 0, 0, 0, 0, 0); }
 __device__ __forceinline__ floatx16 mfma(halfx8 x, halfx8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
 
 // 16 bytes of a pool; once: nobody reads them again, so they go past the caches' care (see load16 in decode_mfma.hip).
@@ -279,6 +289,10 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
   constexpr bool INT8 = KV == kKvInt8Head;
   using k_op = std::conditional_t<INT8, _Float16, __bf16>;
+  // E4M3 keys with a scale for each head are operands as they are: the query is split into two E4M3 numbers instead (see below)
+  constexpr bool RAW_K = KV == kKvFp8Head;
+  constexpr int kKRowBytes = RAW_K ? D : D * 2;    // rows of K in LDS
+  constexpr int kDigitSteps = D / 64;              // RAW_K: 64-deep steps of the QK product, each once for either part of the query
   using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
   using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;  // ... and of the second
   using opx4 = std::conditional_t<HEAD, halfx4, bf16x4>;
@@ -429,9 +443,10 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     const int qtok = row_ok ? tok_in_tile : tokens_here - 1, qhead = row_ok ? head : g * group;
     const __bf16* qrow = (const __bf16*)q + ((size_t)(q_off + q0 + qtok) * hq + qhead) * D;
 #pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) qop[kk] = *(const kx8*)(qrow + kk * 16 + h2 * 8);   // bf16 pools: scaled further down; int8: so far only moved
+    for (int kk = 0; kk < kKK; ++kk) qop[kk] = *(const kx8*)(qrow + (RAW_K ? kk / 4 * 64 + h2 * 32 + kk % 4 * 8 : kk * 16 + h2 * 8));   // bf16 pools: scaled further down; int8: so far only moved
   }
-  float q_unit = 1.f;                            // int8: what a unit of this wave's rows is worth
+  float q_unit = 1.f;                            // int8, RAW_K: what a unit of this wave's rows is worth
+  intx8 q_digit[RAW_K ? 2 : 1][kDigitSteps];     // RAW_K: the query's leading and trailing parts
 
   floatx16 acc[kDT];
 #pragma unroll
@@ -464,6 +479,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   // four chunks of each of two rows, one in even positions and the other (both keys have the row's last bit) in odd ones, they
   // meet all banks; with a row's eight they meet half of them twice: 8.5 M conflicts in 35.5 M busy cycles of the LDS over the
   // shared half of 64 groups of 8 behind 8192 tokens (64/4/128), none in 27.0 M this way; 64 chunks of 8 tokens behind 8k 195 -> 186 us.
+  auto k_key = [](int row) __attribute__((always_inline)) { return RAW_K ? row / (256 / D) & (D / 16 - 1) : row & 15; };
   auto v_key = [](int row) __attribute__((always_inline)) { return (row & 3) << 2 | (FP8 ? row & 1 : 0); };
   unsigned int goff[kLoads][2], goff_last[kLoads][2];   // [][0]: K, [][1]: V
   lds_p wptr[kLoads][3];                                // FP8: where a widened chunk goes, K's two halves and V
@@ -475,7 +491,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     const int trow = kPairs ? idx / 16 * 2 + (idx >> 2 & 1) : idx / kSrcChunks;
     const int tslot = trow % kPageSize;               // token slot within its page
     const int c = kPairs ? (idx >> 3 & 1) * 4 + (idx & 3) : idx % kSrcChunks;
-    const int kkey = trow & 15, vkey = v_key(trow);
+    const int kkey = k_key(trow), vkey = v_key(trow);
     const int ck = FP8 ? c : ((c ^ kkey) & (kChunks - 1)), cv = FP8 ? c : ((c ^ vkey) & (kChunks - 1));
     goff[j][0] = tslot * kSrcRowBytes + ck * 16;
     goff[j][1] = tslot * kSrcRowBytes + cv * 16;
@@ -484,9 +500,10 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     if constexpr (FP8) {
       // the two 16-byte halves of the widened chunk sit in chunks 2c and 2c + 1: 16 bytes apart after the swizzle, one behind the
       // other or in front of it
-      const int kat = trow * kRowBytes + (((2 * c) ^ kkey) & (kChunks - 1)) * 16;
+      // (RAW_K: a chunk stays one)
+      const int kat = RAW_K ? trow * kKRowBytes + (c ^ kkey) * 16 : trow * kRowBytes + (((2 * c) ^ kkey) & (kChunks - 1)) * 16;
       wptr[j][0] = (lds_p)(k_lds[0] + kat);
-      wptr[j][1] = (lds_p)(k_lds[0] + (kat ^ 16));
+      wptr[j][1] = (lds_p)(k_lds[0] + (RAW_K ? kat : kat ^ 16));
       wptr[j][2] = (lds_p)(v_lds[0] + trow * kRowBytes + (((2 * c) ^ vkey) & (kChunks - 1)) * 16);
     }
   }
@@ -502,6 +519,10 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   // -- register path (FP8)
   uintx4 kreg[2][kLoads], vreg[2][kLoads];   // two units in flight
   auto put = [&](lds_p lo_at, lds_p hi_at, int offset, uintx4 codes) __attribute__((always_inline)) {
+    if constexpr (RAW_K) {
+      *lds_at<uintx4>(lo_at, offset) = codes;
+      return;
+    }
     uintx4 lo, hi;
     static_for<4>([&](auto m_c) __attribute__((always_inline)) {
       constexpr int m = decltype(m_c)::value;
@@ -560,12 +581,14 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   // Per-lane LDS pointers that do not change over the loop: the K row this lane feeds as an A
   // operand for each 16-dim step, and the V row / column pair it addresses in each transposed
   // read.  Everything else (buffer, sub-block, token group) is a compile-time immediate.
-  lds_p kptr[kKK], vptr[kDT];
-  const int sub_bytes = tok_wave * kRowBytes;           // HALF: where this wave's tokens start in a K or V tile
+  constexpr int kKptrs = RAW_K ? D / 32 : kKK;
+  lds_p kptr[kKptrs], vptr[kDT];
+  const int sub_bytes = tok_wave * kRowBytes, k_sub_bytes = tok_wave * kKRowBytes;   // HALF: where this wave's tokens start in a V or K tile
   {
     const int t = (n32 & 16) + tau(n32 & 15);
 #pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) kptr[kk] = (lds_p)(k_lds[0] + sub_bytes + t * kRowBytes + (((kk * 2 + h2) ^ (t & 15)) & (kChunks - 1)) * 16);
+    for (int i = 0; i < kKptrs; ++i)
+      kptr[i] = (lds_p)(k_lds[0] + k_sub_bytes + t * kKRowBytes + ((RAW_K ? (i >> 1) * 4 + h2 * 2 + (i & 1) : i * 2 + h2) ^ k_key(t) & (RAW_K ? D / 16 : kChunks) - 1) * 16);
     const int j = lane & 15;
     const int tv = h2 * 8 + (j >> 2);
 #pragma unroll
@@ -575,7 +598,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   }
 
   constexpr int kSubs = kStepTokens / (HALF ? 64 : 32);   // 32-token sub-blocks of a step that this wave works on
-  constexpr int kPvSteps = 8 * kSubs, kSteps = 16 * kSubs;
+  constexpr int kPvSteps = 8 * kSubs, kSteps = kPvSteps + (RAW_K ? 2 * kDigitSteps : 8) * kSubs;
   floatx16 s[kSubs];        // scores of the block between its two phases
   opx8 pop[kSubs][2];       // its probabilities, as B operands of the second product
 
@@ -613,11 +636,18 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   auto matrix_phase = [&](auto first_c, auto last_c, int kbo, int vbo, auto&& piece) __attribute__((always_inline)) {
     constexpr int T0 = decltype(first_c)::value, T1 = decltype(last_c)::value;
     opx8 v_ops[kPvSteps];
-    kx8 k_ops[kSteps];
+    kx8 k_ops[RAW_K ? 1 : kSteps];
+    intx8 k_raw[kDigitSteps][kSubs];
     auto fetch = [&](auto t_c) __attribute__((always_inline)) {
       constexpr int t = decltype(t_c)::value;
       if constexpr (t < kPvSteps) {
         read_v_operand(vbo, t_c, v_ops[t]);
+      } else if constexpr (RAW_K) {
+        constexpr int u = t - kPvSteps, sub = u % kSubs, digit = u / kSubs % 2, kk = u / kSubs / 2;
+        if constexpr (digit == 0) {
+          const uintx4 lo = *lds_at<const uintx4>(kptr[2 * kk], kbo + sub * 32 * kKRowBytes), hi = *lds_at<const uintx4>(kptr[2 * kk + 1], kbo + sub * 32 * kKRowBytes);
+          k_raw[kk][sub] = intx8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        }
       } else {
         constexpr int u = t - kPvSteps, kk = u / kSubs, sub = u % kSubs;
         if constexpr (kk < kKK) k_ops[t] = *lds_at<const kx8>(kptr[kk], kbo + sub * 32 * kRowBytes);
@@ -628,6 +658,13 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       if constexpr (t < kPvSteps) {
         constexpr int sub = t >> 3, ks = (t >> 2) & 1, dt = t & 3;
         if constexpr (dt < kDT) acc[dt] = mfma(v_ops[t], pop[sub][ks], acc[dt]);
+      } else if constexpr (RAW_K) {
+        constexpr int u = t - kPvSteps, sub = u % kSubs, digit = u / kSubs % 2, kk = u / kSubs / 2;
+        if constexpr (u < kSubs) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[sub][i] = 0.f;
+        }
+        s[sub] = mfma(k_raw[kk][sub], q_digit[digit][kk], s[sub]);
       } else {
         constexpr int u = t - kPvSteps, kk = u / kSubs, sub = u % kSubs;
         if constexpr (kk < kKK) {
@@ -681,7 +718,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     float sc[kPg], lvs[kPg], ivs[kPg];                 // this wave's pages: K scale times softmax scale, log2 of the V scale, its reciprocal
     if constexpr (FP8) {
 #pragma unroll
-      for (int p = 0; p < kPg; ++p) { sc[p] = INT8 ? ksc_cur[p] * q_unit : ksc_cur[p]; lvs[p] = lvs_cur[p]; ivs[p] = ivs_cur[p]; }
+      for (int p = 0; p < kPg; ++p) { sc[p] = HEAD ? ksc_cur[p] * q_unit : ksc_cur[p]; lvs[p] = lvs_cur[p]; ivs[p] = ivs_cur[p]; }
       if (!positive_scale) {                           // rare: scale the scores themselves instead
 #pragma unroll
         for (int sub = 0; sub < kSubs; ++sub)
@@ -852,7 +889,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
         if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) put(wptr[j][0], wptr[j][1], 0, k0[j]);
-      if constexpr (INT8) {
+      if constexpr (HEAD) {
         float top = 0.f;
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
@@ -864,12 +901,28 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
         top = xor32_max(top);
 #pragma unroll
         for (int x = 16; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-        const int up = kQueryBits - __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top));
+        const int up = (RAW_K ? kDigitBits : kQueryBits) - __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top));
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
           const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+          float x[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) qop[kk][e] = (k_op)__builtin_amdgcn_ldexpf((float)v[e], up);
+          for (int e = 0; e < 8; ++e) {
+            x[e] = __builtin_amdgcn_ldexpf((float)v[e], up);
+            if constexpr (!RAW_K) qop[kk][e] = (k_op)x[e];
+          }
+          if constexpr (RAW_K) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              int code = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w], x[4 * w + 1], 0, false);
+              code = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2], x[4 * w + 3], code, true);
+              const floatx2 a0 = __builtin_amdgcn_cvt_pk_f32_fp8(code, false), a1 = __builtin_amdgcn_cvt_pk_f32_fp8(code, true);
+              int rest = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w] - a0[0], x[4 * w + 1] - a0[1], 0, false);
+              rest = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2] - a1[0], x[4 * w + 3] - a1[1], rest, true);
+              q_digit[0][kk / 4][kk % 4 * 2 + w] = code;
+              q_digit[1][kk / 4][kk % 4 * 2 + w] = rest;
+            }
+          }
         }
         q_unit = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(__builtin_amdgcn_ldexpf(1.f, -up))));
       }
@@ -972,12 +1025,15 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     if constexpr (FP8) {
       constexpr int slot = decltype(slot_c)::value, pos = decltype(pos_c)::value;
       // (int8: two or three instructions for a pair; one at a time, 44 items for a chunk, or the signs in the vector phase: no difference)
-      constexpr int kItems = 20 * kLoads;
+      // (RAW_K: K's chunk is written as it came)
+      constexpr int kItems = (RAW_K ? 11 : 20) * kLoads;
       static_for<kItems>([&](auto item_c) __attribute__((always_inline)) {
         constexpr int item = decltype(item_c)::value;
         if constexpr (item * 31 / kItems == pos) {
-          constexpr int j = item % kLoads, part = item / kLoads / 5, m = item / kLoads % 5;   // the halves of K's chunk, then V's
-          if constexpr (m < 4) {
+          constexpr int j = item % kLoads, nth = item / kLoads + (RAW_K ? 9 : 0), part = nth / 5, m = nth % 5;   // the halves of K's chunk, then V's
+          if constexpr (RAW_K && part == 1) {
+            if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) *lds_at<uintx4>(wptr[j][0], ring(slot_c, c1)) = kreg[slot][j];
+          } else if constexpr (m < 4) {
             wide[j][m] = widen_pair<KV, part >= 2, (part & 1) * 4 + m>((part < 2 ? kreg : vreg)[slot][j]);
           } else if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) {
             if constexpr (part < 2) *lds_at<uintx4>(wptr[j][part], ring(slot_c, c1)) = wide[j];
@@ -1013,13 +1069,14 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       // the pointers could be others in every block, as far as the compiler can tell: it would keep each sum of one and an
       // offset in a register of its own, two hundred of them, instead of using the offset as it is
 #pragma unroll
-      for (int kk = 0; kk < kKK; ++kk) asm volatile("" : "+v"(kptr[kk]));
+      for (int kk = 0; kk < kKptrs; ++kk) asm volatile("" : "+v"(kptr[kk]));
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) asm volatile("" : "+v"(vptr[dt]));
       if constexpr (FP8) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-          asm volatile("" : "+v"(wptr[j][0]), "+v"(wptr[j][1]), "+v"(wptr[j][2]));
+          asm volatile("" : "+v"(wptr[j][0]), "+v"(wptr[j][2]));
+          if constexpr (!RAW_K) asm volatile("" : "+v"(wptr[j][1]));
           asm volatile("" : "+v"(goff[j][0]), "+v"(goff_last[j][0]));   // (nor widened to 64 bits)
         }
       }
