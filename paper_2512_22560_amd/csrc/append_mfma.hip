@@ -479,7 +479,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   // four chunks of each of two rows, one in even positions and the other (both keys have the row's last bit) in odd ones, they
   // meet all banks; with a row's eight they meet half of them twice: 8.5 M conflicts in 35.5 M busy cycles of the LDS over the
   // shared half of 64 groups of 8 behind 8192 tokens (64/4/128), none in 27.0 M this way; 64 chunks of 8 tokens behind 8k 195 -> 186 us.
-  auto k_key = [](int row) __attribute__((always_inline)) { return RAW_K ? row / (256 / D) & (D / 16 - 1) : row & 15; };
+  auto raw_key = [](int row) __attribute__((always_inline)) { return row / (256 / D) & (D / 16 - 1); };   // RAW_K: sixteen rows meet all banks
   auto v_key = [](int row) __attribute__((always_inline)) { return (row & 3) << 2 | (FP8 ? row & 1 : 0); };
   unsigned int goff[kLoads][2], goff_last[kLoads][2];   // [][0]: K, [][1]: V
   lds_p wptr[kLoads][3];                                // FP8: where a widened chunk goes, K's two halves and V
@@ -491,7 +491,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     const int trow = kPairs ? idx / 16 * 2 + (idx >> 2 & 1) : idx / kSrcChunks;
     const int tslot = trow % kPageSize;               // token slot within its page
     const int c = kPairs ? (idx >> 3 & 1) * 4 + (idx & 3) : idx % kSrcChunks;
-    const int kkey = k_key(trow), vkey = v_key(trow);
+    const int kkey = trow & 15, vkey = v_key(trow);
     const int ck = FP8 ? c : ((c ^ kkey) & (kChunks - 1)), cv = FP8 ? c : ((c ^ vkey) & (kChunks - 1));
     goff[j][0] = tslot * kSrcRowBytes + ck * 16;
     goff[j][1] = tslot * kSrcRowBytes + cv * 16;
@@ -501,9 +501,13 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       // the two 16-byte halves of the widened chunk sit in chunks 2c and 2c + 1: 16 bytes apart after the swizzle, one behind the
       // other or in front of it
       // (RAW_K: a chunk stays one)
-      const int kat = RAW_K ? trow * kKRowBytes + (c ^ kkey) * 16 : trow * kRowBytes + (((2 * c) ^ kkey) & (kChunks - 1)) * 16;
-      wptr[j][0] = (lds_p)(k_lds[0] + kat);
-      wptr[j][1] = (lds_p)(k_lds[0] + (RAW_K ? kat : kat ^ 16));
+      if constexpr (RAW_K) {
+        wptr[j][0] = (lds_p)(k_lds[0] + trow * kKRowBytes + (c ^ raw_key(trow)) * 16);
+      } else {
+        const int kat = trow * kRowBytes + (((2 * c) ^ kkey) & (kChunks - 1)) * 16;
+        wptr[j][0] = (lds_p)(k_lds[0] + kat);
+        wptr[j][1] = (lds_p)(k_lds[0] + (kat ^ 16));
+      }
       wptr[j][2] = (lds_p)(v_lds[0] + trow * kRowBytes + (((2 * c) ^ vkey) & (kChunks - 1)) * 16);
     }
   }
@@ -587,8 +591,10 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
   {
     const int t = (n32 & 16) + tau(n32 & 15);
 #pragma unroll
-    for (int i = 0; i < kKptrs; ++i)
-      kptr[i] = (lds_p)(k_lds[0] + k_sub_bytes + t * kKRowBytes + ((RAW_K ? (i >> 1) * 4 + h2 * 2 + (i & 1) : i * 2 + h2) ^ k_key(t) & (RAW_K ? D / 16 : kChunks) - 1) * 16);
+    for (int i = 0; i < kKptrs; ++i) {
+      if constexpr (RAW_K) kptr[i] = (lds_p)(k_lds[0] + k_sub_bytes + t * kKRowBytes + (((i >> 1) * 4 + h2 * 2 + (i & 1)) ^ raw_key(t)) * 16);
+      else kptr[i] = (lds_p)(k_lds[0] + sub_bytes + t * kRowBytes + (((i * 2 + h2) ^ (t & 15)) & (kChunks - 1)) * 16);
+    }
     const int j = lane & 15;
     const int tv = h2 * 8 + (j >> 2);
 #pragma unroll
@@ -1075,8 +1081,8 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       if constexpr (FP8) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-          asm volatile("" : "+v"(wptr[j][0]), "+v"(wptr[j][2]));
-          if constexpr (!RAW_K) asm volatile("" : "+v"(wptr[j][1]));
+          if constexpr (RAW_K) asm volatile("" : "+v"(wptr[j][0]), "+v"(wptr[j][2]));
+          else asm volatile("" : "+v"(wptr[j][0]), "+v"(wptr[j][1]), "+v"(wptr[j][2]));
           asm volatile("" : "+v"(goff[j][0]), "+v"(goff_last[j][0]));   // (nor widened to 64 bits)
         }
       }
