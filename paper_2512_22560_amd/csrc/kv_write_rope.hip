@@ -24,7 +24,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kKeep = 8;          // rows of a lane that are under way at once
 constexpr int kRound = 4;         // heads of a lane whose rows are held until their scales are known
-constexpr int kQueryWaves = 8192; // queries: waves wanted where there are few tokens
+constexpr int kQueryWaves = 2048; // queries: waves wanted where there are few tokens
 constexpr int kMostPages = 4096;  // pages of a trajectory with a workgroup of their own
 
 template <int SRC_BYTES>
@@ -162,6 +162,7 @@ __device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, 
 // The place in its context of new token `token`, the same in all lanes: the trajectory it belongs to is the last one that starts at
 // or before it and has new tokens; 64 starts are looked at a time.
 __device__ __forceinline__ int place_of(const RopeWriteArgs& a, int token) {
+  if (a.one_each) return ((const __attribute__((address_space(4))) int32_t*)a.ctx_lens)[token] - 1;
   const int lane = threadIdx.x & 63;
   int lo = 0, n = a.batch;                            // among trajectories [lo, lo + n), starts in order
   while (n > 1) {
@@ -212,6 +213,8 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 // pages 156 and 148, among them 139 and 117: 5.7 and 5.2 TB/s where a streaming pass over as many bytes reaches 6.2.  Fewer
 // workgroups that take several pages each: slower by 5 to 20 %.  Rows held as floats until their scale is known instead of
 // turned twice: three workgroups per CU instead of five.
+// 512 single tokens (64/4/128, int8; between events around the launch): 11.4 us with a search for each token's trajectory and a wave per
+// four query heads, 10.2 without the search, 8.8 with a wave per sixteen.
 // POOL: -1 the source type, else a KvKind
 template <int D, int SRC_BYTES, int POOL>
 __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWriteArgs a) {
@@ -453,6 +456,7 @@ hipError_t launch_d(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid, 
 
 hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s) {
   RopeWriteArgs a = args;
+  a.one_each = max_q_len == 1 && a.total_q == a.batch;   // (no trajectory has more, so each has one)
   // a run of n tokens touches at most this many pages, wherever it starts
   const int64_t longest = std::min(max_q_len, a.total_q);
   a.pages = longest > 0 ? (int32_t)std::min<int64_t>((longest + kPageSize - 2) / kPageSize + 1, kMostPages) : 1;
