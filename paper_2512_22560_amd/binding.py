@@ -159,6 +159,8 @@ def _kv_code(pages: torch.Tensor, k_scale, v_scale) -> int:
     pool = pages.shape
     held = (pool[0], pool[1])
     if k_scale.shape != held or v_scale.shape != held:
+        if code == FP8_E4M3 and k_scale.numel() == v_scale.numel() == pool[0]:
+            return code
         raise ValueError("scales of each page and KV head are [num_pages, Hkv]")
     return INT8_HEAD if code == INT8_HEAD else FP8_E4M3_HEAD
 
