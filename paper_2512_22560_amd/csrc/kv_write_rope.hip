@@ -25,6 +25,10 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kKeep = 8;          // rows of a lane that are under way at once
 constexpr int kRound = 4;         // heads of a lane whose rows are held until their scales are known
 constexpr int kQueryWaves = 2048; // queries: waves wanted where there are few tokens
+// Rotated queries of more bytes than this do not stay in the memory-side cache (256 MB) until attention reads them, and are written
+// with the streaming hint, by instances of their own (a branch between the two in one instance: 139 -> 147 us): 363 and 220 MB of
+// them 139 -> 133 and 117 -> 112 us alone, 719 -> 719 and 376 -> 375 with attn_append behind; 41 MB of them 244 -> 246 with it.
+constexpr int64_t kStreamQueries = 128 << 20;
 constexpr int kMostPages = 4096;  // pages of a trajectory with a workgroup of their own
 
 template <int SRC_BYTES>
@@ -137,8 +141,8 @@ __device__ __forceinline__ Raw<SRC_BYTES> fetch(const Lane& lane, const void* ro
   return r;
 }
 
-// A row of the source type, turned where it has to be, at p.
-template <int SRC_BYTES>
+// A row of the source type, turned where it has to be, at p; STREAM: past the caches' care.
+template <int SRC_BYTES, bool STREAM>
 __device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, const Turn& turn, void* p, Raw<SRC_BYTES> r) {
   if (lane.turns) {
     float x[8];
@@ -155,8 +159,15 @@ __device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, 
       r.hi = to_bf16x4(x + 4);
     }
   }
-  *(typename Raw<SRC_BYTES>::half*)((unsigned char*)p + lane.e0 * SRC_BYTES) = r.lo;
-  *(typename Raw<SRC_BYTES>::half*)((unsigned char*)p + lane.e1 * SRC_BYTES) = r.hi;
+  typedef typename Raw<SRC_BYTES>::half half;
+  half *lo = (half*)((unsigned char*)p + lane.e0 * SRC_BYTES), *hi = (half*)((unsigned char*)p + lane.e1 * SRC_BYTES);
+  if constexpr (STREAM) {
+    __builtin_nontemporal_store(r.lo, lo);
+    __builtin_nontemporal_store(r.hi, hi);
+  } else {
+    *lo = r.lo;
+    *hi = r.hi;
+  }
 }
 
 // The place in its context of new token `token`, the same in all lanes: the trajectory it belongs to is the last one that starts at
@@ -175,7 +186,7 @@ __device__ __forceinline__ int place_of(const RopeWriteArgs& a, int token) {
   return a.ctx_lens[lo] - a.q_lens[lo] + token - a.q_offsets[lo];
 }
 
-template <int D, int SRC_BYTES>
+template <int D, int SRC_BYTES, bool STREAM>
 __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned int block) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;  // lanes of a row, heads under way at a time
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -200,7 +211,7 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
       const int head = h + i * kRows + sub;
-      if (head < h1) store<SRC_BYTES>(a, lane, turn, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
+      if (head < h1) store<SRC_BYTES, STREAM>(a, lane, turn, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
     }
   }
 }
@@ -210,13 +221,13 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 // int8 ones (605 MB), us a call: a workgroup per page and 16 heads, heads outermost 171 and 138 (at any time all of them read and write
 // the same few kilobytes of every token's row, a part of the memory's channels), heads innermost 151 and 148 (keys on some XCDs,
 // queries on others), in 13 parts instead of 4 to 10: 154 and worse, each looking positions up again; queries by tokens, behind the
-// pages 156 and 148, among them 139 and 117: 5.7 and 5.2 TB/s where a streaming pass over as many bytes reaches 6.2.  Fewer
-// workgroups that take several pages each: slower by 5 to 20 %.  Rows held as floats until their scale is known instead of
-// turned twice: three workgroups per CU instead of five.
+// pages 156 and 148, among them 139 and 117, with the streaming hint 133 and 112: 6.0 and 5.4 TB/s where a streaming pass over as
+// many bytes reaches 6.2.  Fewer workgroups that take several pages each: slower by 5 to 20 %.  Rows held as floats until their scale is
+// known instead of turned twice: three workgroups per CU instead of five.
 // 512 single tokens (64/4/128, int8; between events around the launch): 11.4 us with a search for each token's trajectory and a wave per
 // four query heads, 10.2 without the search, 8.8 with a wave per sixteen.
-// POOL: -1 the source type, else a KvKind
-template <int D, int SRC_BYTES, int POOL>
+// POOL: -1 the source type, else a KvKind; STREAM: rotated queries are written with the streaming hint
+template <int D, int SRC_BYTES, int POOL, bool STREAM>
 __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWriteArgs a) {
   constexpr bool kCodes = POOL >= 0, kHeadScales = kCodes && kv_has_head_scales(POOL);
   constexpr bool kInt8 = POOL == kKvInt8Head;
@@ -228,7 +239,8 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   const unsigned int g = blockIdx.x / kXcds, at = blockIdx.x % kXcds;
   const unsigned int pages_before = (unsigned int)((uint64_t)g * a.page_share >> 32), pages_then = (unsigned int)((uint64_t)(g + 1) * a.page_share >> 32);
   if (pages_before == pages_then) {
-    turn_queries<D, SRC_BYTES>(a, (g - pages_before) * kXcds + at);
+    const unsigned int unit = (g - pages_before) * kXcds + at;
+    turn_queries<D, SRC_BYTES, STREAM>(a, unit);
     return;
   }
   // eight pages' keys, then their values
@@ -272,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
           if (h - head0 + i * side < hkv) r[i] = fetch_row(min(h + i * side, hkv - 1));
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
-          if (h + i * side < hkv) store<SRC_BYTES>(a, lane, turn, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
+          if (h + i * side < hkv) store<SRC_BYTES, false>(a, lane, turn, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
       }
   } else {
     static_assert(SRC_BYTES == 2, "codes are made of bf16 rows");
@@ -435,17 +447,17 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   }
 }
 
-template <int D>
-hipError_t launch_d(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid, hipStream_t s) {
+template <int D, bool STREAM>
+hipError_t launch_as(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid, hipStream_t s) {
   if (src_bytes == 4) {
     if (pool != -1) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((kv_write_rope_kernel<D, 4, -1>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((kv_write_rope_kernel<D, 4, -1, STREAM>), grid, dim3(kThreads), 0, s, a);
   } else {
     switch (pool) {
-      case -1: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, -1>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvFp8: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvFp8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8Head>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvInt8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvInt8Head>), grid, dim3(kThreads), 0, s, a); break;
+      case -1: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, -1, STREAM>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvFp8: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8, STREAM>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvFp8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8Head, STREAM>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvInt8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvInt8Head, STREAM>), grid, dim3(kThreads), 0, s, a); break;
       default: return hipErrorInvalidValue;
     }
   }
@@ -462,19 +474,21 @@ hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, in
   a.pages = longest > 0 ? (int32_t)std::min<int64_t>((longest + kPageSize - 2) / kPageSize + 1, kMostPages) : 1;
   const int64_t page_groups = ((int64_t)a.pages * a.batch + kXcds - 1) / kXcds * 2;
   int64_t groups = page_groups;
+  bool stream = false;
   if (a.q) {
     // a wave takes so many heads of a token that kKeep rows of each of its lanes hold them, fewer where waves are few
     const int rows = 64 / (head_dim / 8), most = (a.hq + rows - 1) / rows;
     const int64_t parts = std::clamp<int64_t>(kQueryWaves / a.total_q, (most + kKeep - 1) / kKeep, most);
     a.part_heads = (int)((most + parts - 1) / parts) * rows;
     a.head_parts = (a.hq + a.part_heads - 1) / a.part_heads;
+    stream = (int64_t)a.total_q * a.hq * head_dim * src_bytes > kStreamQueries;
     groups += ((int64_t)a.total_q * a.head_parts + kWaves * kXcds - 1) / (kWaves * kXcds);
   }
   if (groups * kXcds > INT32_MAX || (int64_t)a.total_q * a.head_parts > INT32_MAX) return hipErrorInvalidValue;
   a.page_share = (((uint64_t)page_groups << 32) + groups - 1) / groups;   // (rounded up: behind the last group there have been them all)
   const dim3 grid((unsigned)(groups * kXcds));
-  if (head_dim == 128) return launch_d<128>(a, src_bytes, pool, grid, s);
-  if (head_dim == 64) return launch_d<64>(a, src_bytes, pool, grid, s);
+  if (head_dim == 128) return stream ? launch_as<128, true>(a, src_bytes, pool, grid, s) : launch_as<128, false>(a, src_bytes, pool, grid, s);
+  if (head_dim == 64) return stream ? launch_as<64, true>(a, src_bytes, pool, grid, s) : launch_as<64, false>(a, src_bytes, pool, grid, s);
   return hipErrorInvalidValue;
 }
 

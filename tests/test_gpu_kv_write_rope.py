@@ -213,6 +213,17 @@ def test_a_pool_past_four_gigabytes():
     same((None, pool[ids], other[ids], scale[ids], vscale[ids]), want)
 
 
+def test_queries_past_what_the_caches_hold():
+    """More than 128 MB of them are written with another kind of store."""
+    b = batch_of("t", (96, 2), 128, "bf16", "int8_head", ("uniform", 0, 30), ("uniform", 500, 900), 85)
+    gen = torch.Generator().manual_seed(15)
+    q, k, v = (rows_of(gen, b.total_q, h, 128, "bf16") for h in (96, 2, 2))
+    assert q.numel() * 2 > 128 << 20
+    for interleaved in (False, True):
+        got, want = both(b, q, k, v, table_of(1024, 128), interleaved=interleaved)
+        same(got, want)
+
+
 def test_the_write_is_captured_and_replayed():
     b = batch_of("t", (8, 4), 128, "bf16", "int8_head", ("uniform", 0, 30), ("const", 1), 81)
     gen = torch.Generator().manual_seed(13)
