@@ -87,8 +87,12 @@ def _parts(batch, c, W):
     """(kind, sub-batch) legs of one step of configuration c."""
     if c in (2, 3):
         return [("decode", batch)]
-    if c in (4, "recompute"):
+    if c in (4, "recompute", "c4_int8_head", "c4_fp8_head"):
         return [("append", batch)]
+    if c in ("c2_int8_head", "c2_fp8_head"):
+        return [("decode", batch)]
+    if c == "kv_write_rope_c4":
+        return [("kv_write_rope", batch)]
     if c == "kv_write_c4":
         return [("kv_write", batch)]
     if c in ("shared_prompt", "shared_prompt_plain"):
@@ -132,19 +136,26 @@ class Leg:
             pages = n_groups * (W.SHARED_PROMPT_TOKENS // 16) + int(((bb.ctx_lens_host - W.SHARED_PROMPT_TOKENS + 15) // 16).sum())
             self.work = {"bytes": int(2 * w.num_kv_heads * w.head_dim * kvb * uniq + pages * (4 + (8 if kvb == 1 else 0))
                                       + 2 * bb.total_q * w.num_q_heads * w.head_dim * 2), "flops": 0}
-        if kind == "kv_write":
+        if kind in ("kv_write", "kv_write_rope"):
             # new K / V rows for the chunk region of the cache; unit-scale values as everywhere else
             g = torch.Generator(device=bb.q.device).manual_seed(w.seed)
             shape = (bb.total_q, w.num_kv_heads, w.head_dim)
             self.k_new = torch.randn(shape, generator=g, device=bb.q.device, dtype=torch.float32).to(bb.q.dtype)
             self.v_new = torch.randn(shape, generator=g, device=bb.q.device, dtype=torch.float32).to(bb.q.dtype)
-            kvb = {"f32": 4, "bf16": 2, "fp8_e4m3": 1}[w.kv_dtype]
+            kvb = {"f32": 4, "bf16": 2}.get(w.kv_dtype, 1)
             srcb = {"f32": 4, "bf16": 2}[w.q_dtype]
             first = bb.ctx_lens_host - bb.q_lens_host
             pages = np.where(bb.q_lens_host > 0, (bb.ctx_lens_host + 15) // 16 - first // 16, 0).sum()
             rows = int(bb.q_lens_host.sum()) * w.num_kv_heads * w.head_dim
             # rows read once and written once per pool, one table entry per touched page, FP8: its two scales read and written
-            self.work = {"bytes": int(2 * rows * (srcb + kvb) + 4 * pages + (16 * pages if w.kv_dtype == "fp8_e4m3" else 0)), "flops": 0}
+            self.work = {"bytes": int(2 * rows * (srcb + kvb) + 4 * pages + (16 * pages * (1 if w.kv_dtype == "fp8_e4m3" else w.num_kv_heads) if kvb == 1 else 0)), "flops": 0}
+        if kind == "kv_write_rope":
+            # queries as well, read and written once, and a row of cosines and sines for each position
+            d, n = w.head_dim, int(bb.ctx_lens_host.max())
+            angle = torch.arange(n, device=bb.q.device, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, d, 2, device=bb.q.device, dtype=torch.float64) / d)
+            self.cos_sin = torch.cat([angle.cos(), angle.sin()], dim=1).to(torch.float32)
+            taken = np.unique(np.concatenate([np.arange(l - m, l) for l, m in zip(bb.ctx_lens_host, bb.q_lens_host)]))
+            self.work = dict(self.work, bytes=self.work["bytes"] + 2 * bb.total_q * w.num_q_heads * d * srcb + 4 * d * len(taken))
         # Rotating copies of the pools keep the 256 MB last-level cache from serving a small KV set.
         self.pools = [(bb.k_pages, bb.v_pages)]
         for _ in range(n_pools - 1):
@@ -162,6 +173,9 @@ class Leg:
         elif self.kind == "kv_write":
             B.kv_write(self.k_new, self.v_new, bb.q_lens, bb.q_offsets, k, v, bb.page_table, bb.ctx_lens, max_q_len=self.max_q,
                        k_scale=bb.k_scale, v_scale=bb.v_scale)
+        elif self.kind == "kv_write_rope":
+            B.kv_write_rope(bb.q, self.k_new, self.v_new, bb.q_lens, bb.q_offsets, k, v, bb.page_table, bb.ctx_lens, cos_sin=self.cos_sin,
+                            max_q_len=self.max_q, k_scale=bb.k_scale, v_scale=bb.v_scale, q_out=self.out)
         elif self.kind == "step":
             B.attn_step(bb.q, bb.q_lens, bb.q_offsets, k, v, bb.page_table, bb.ctx_lens, sm_scale=w.sm_scale,
                         max_q_len=self.max_q, k_scale=bb.k_scale, v_scale=bb.v_scale, out=self.out, workspace=self.ws)
@@ -256,7 +270,7 @@ def leg_report(leg, kms, call_ms, peaks, step_ms=None):
     the events around a call cost a few microseconds themselves, which matters for the short decode calls)."""
     k, c = _stats(kms), _stats(call_ms)
     work = leg.work
-    hbm = leg.kind in ("decode", "kv_write", "decode_shared", "decode_aliased")
+    hbm = leg.kind in ("decode", "kv_write", "kv_write_rope", "decode_shared", "decode_aliased")
     amount = work["bytes"] if hbm else work["flops"]
     unit, peak, scale = ("GB/s", HBM_PEAK_GBS, 1e6) if hbm else ("TFLOP/s", MFMA_BF16_PEAK_TFLOPS, 1e9)
     ach = amount / k["avg"] / scale
@@ -395,7 +409,7 @@ def main():
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=50)
     ap.add_argument("--warmup", type=int, default=10)
-    ap.add_argument("--only", default=None, help="run a single workload: c2, c3, c4, c5, c5_one_call, recompute, kv_write_c4, kv_write_c5, shared_prompt or shared_prompt_plain; `peaks`: the two peak microbenchmarks alone; `copy`: 1 GiB copy for counter calibration")
+    ap.add_argument("--only", default=None, help="run a single workload: c2, c3, c4, c5, c5_one_call, recompute, kv_write_c4, kv_write_c5, shared_prompt or shared_prompt_plain; 8-bit pools with a scale for each page and head: c2_int8_head, c2_fp8_head, c4_int8_head, c4_fp8_head, kv_write_rope_c4; `peaks`: the two peak microbenchmarks alone; `copy`: 1 GiB copy for counter calibration")
     ap.add_argument("--no-cpu", action="store_true", help="skip the CPU oracle baselines")
     ap.add_argument("--no-peaks", action="store_true", help="skip the peak microbenchmarks")
     a = ap.parse_args()
@@ -431,6 +445,11 @@ def main():
         return
     extra = {"recompute": W.RECOMPUTE, "kv_write_c4": W.CONFIGS[4], "kv_write_c5": W.CONFIGS[5], "c5_one_call": W.CONFIGS[5],
              "shared_prompt": W.SHARED_PROMPT, "shared_prompt_plain": W.SHARED_PROMPT}
+    # the same lengths over 8-bit pools with a scale for each page and head, on request
+    for c in (2, 4):
+        for kv in ("int8_head", "fp8_e4m3_head"):
+            extra[f"c{c}_{kv.replace('_e4m3', '')}"] = W.scaled(W.CONFIGS[c], kv_dtype=kv, name=f"{W.CONFIGS[c].name.replace('bf16', kv)}")
+    extra["kv_write_rope_c4"] = extra["c4_int8_head"]
     if a.only:
         selected = [a.only] if a.only in extra else [int(a.only.lstrip("c"))]
     else:
@@ -469,7 +488,7 @@ def main():
 
     w, rep, legs = headline
     lead = rep["legs"][0]
-    if lead["kind"] == "decode":
+    if lead["bound"] == "hbm":
         value = legs[0].work["bytes"] / rep["ms_per_step"] / 1e6      # whole step: plan + main + merge
         unit = "GB/s"
     else:

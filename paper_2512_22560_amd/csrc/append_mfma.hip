@@ -111,6 +111,18 @@ __device__ __forceinline__ float xor32_add(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Largest of a whole number per lane, in all lanes.
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true));    // the neighbour, the other two of four, ...
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));
+  uintx2 r = __builtin_amdgcn_permlane16_swap((unsigned int)x, (unsigned int)x, false, false);
+  x = max((int)r[0], (int)r[1]);
+  r = __builtin_amdgcn_permlane32_swap((unsigned int)x, (unsigned int)x, false, false);
+  return max((int)r[0], (int)r[1]);
+}
+
 // Pair PAIR of sixteen E4M3 codes to bf16, exactly (every E4M3 value is a bf16 value): the hardware's scaled
 // conversion with a scale of one turns two codes into a packed pair per instruction.
 template <int PAIR>
@@ -896,17 +908,19 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       for (int j = 0; j < kLoads; ++j)
         if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) put(wptr[j][0], wptr[j][1], 0, k0[j]);
       if constexpr (HEAD) {
-        float top = 0.f;
+        // the wave's largest element, so that the power stays in a scalar register: two magnitudes at a time, as whole numbers, which order
+        // the same (f16: exact for all above 2^-32 of it); raised so far that infinite and undefined ones, which concern their own
+        // rows alone, wrap round to below zero
+        typedef short shortx2 __attribute__((ext_vector_type(2)));
+        typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
+        shortx2 tops = {0x80, 0x80};
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+          const uintx4 v = __builtin_bit_cast(uintx4, qop[kk]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, __builtin_fabsf((float)v[e]));
+          for (int w = 0; w < 4; ++w) tops = __builtin_elementwise_max(tops, __builtin_bit_cast(shortx2, __builtin_bit_cast(ushortx2, v[w] & 0x7fff7fffu) + ushortx2{0x80, 0x80}));
         }
-        // (the wave's largest element, so that the power stays in a scalar register: exact for all above 2^-32 of it)
-        top = xor32_max(top);
-#pragma unroll
-        for (int x = 16; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const float top = __int_as_float((wave_max(max((int)tops[0], (int)tops[1])) - 0x80) << 16);
         const int up = (RAW_K ? kDigitBits : kQueryBits) - __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top));
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {

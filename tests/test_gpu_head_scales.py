@@ -218,6 +218,24 @@ def test_scales_and_queries_far_from_one(kv, which):
 
 @pytest.mark.parametrize("which", ["decode", "append"])
 @pytest.mark.parametrize("kv", KV)
+def test_queries_that_are_undefined_or_zero_concern_their_rows_alone(kv, which):
+    b = build(kv, (8, 2), 128, ("uniform", 100, 400), qlen=("const", 1 if which == "decode" else 40), batch=6, seed=25, prefix=which == "append")
+    bad = torch.zeros(b.q.shape[:2], dtype=torch.bool)
+    bad[::3, 5] = bad[1::4, 2] = True
+    b.q[1::2, 0] = 0
+    clean = b.q.clone()
+    for value in (float("inf"), float("nan"), -float("inf")):
+        b.q = clean.clone()
+        b.q[bad.to(DEV), 17] = value
+        out = call(b, which)
+        assert not torch.isfinite(out[bad.to(DEV)]).all(dim=-1).any()
+        b.q = clean
+        out[bad.to(DEV)] = call(b, which)[bad.to(DEV)]
+        check(out, b, which)
+
+
+@pytest.mark.parametrize("which", ["decode", "append"])
+@pytest.mark.parametrize("kv", KV)
 def test_pages_of_zero_values(kv, which):
     """Their scale is the least there is; next to others, and alone."""
     b = build(kv, (8, 2), 128, ("uniform", 60, 300), qlen=("const", 1 if which == "decode" else 9), batch=4, seed=18, prefix=which == "append")
