@@ -29,6 +29,7 @@ constexpr int kQueryWaves = 2048; // queries: waves wanted where there are few t
 // with the streaming hint, by instances of their own (a branch between the two in one instance: 139 -> 147 us): 363 and 220 MB of
 // them 139 -> 133 and 117 -> 112 us alone, 719 -> 719 and 376 -> 375 with attn_append behind; 41 MB of them 244 -> 246 with it.
 constexpr int64_t kStreamQueries = 128 << 20;
+constexpr int kSmallPage = 512;   // elements of a token's keys up to which pages are small
 constexpr int kMostPages = 4096;  // pages of a trajectory with a workgroup of their own
 
 template <int SRC_BYTES>
@@ -170,18 +171,25 @@ __device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, 
   }
 }
 
-// The place in its context of new token `token`, the same in all lanes: the trajectory it belongs to is the last one that starts at
-// or before it and has new tokens; 64 starts are looked at a time.
-__device__ __forceinline__ int place_of(const RopeWriteArgs& a, int token) {
-  if (a.one_each) return ((const __attribute__((address_space(4))) int32_t*)a.ctx_lens)[token] - 1;
+// The place in its context of new token `token`; `first` is the smallest token of the wave and the same in all lanes.  The trajectory a
+// token belongs to is the last one that starts at or before it: for the first by looking at 64 starts at a time, from there on by
+// steps that double, then halve.
+__device__ __forceinline__ int place_of(const RopeWriteArgs& a, int first, int token) {
+  if (a.one_each) return a.ctx_lens[token] - 1;
   const int lane = threadIdx.x & 63;
   int lo = 0, n = a.batch;                            // among trajectories [lo, lo + n), starts in order
   while (n > 1) {
     const int step = (n + 63) / 64, at = lane * step;
-    const bool before = at < n && a.q_offsets[lo + at] <= token;
+    const bool before = at < n && a.q_offsets[lo + at] <= first;
     const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1, 0);
     lo += k * step;
     n = min(step, n - k * step);
+  }
+  if (a.wave_tokens > 1) {
+    int ahead = 1;
+    for (; lo + ahead < a.batch && a.q_offsets[lo + ahead] <= token; ahead *= 2) lo += ahead;
+    while (ahead /= 2)
+      if (lo + ahead < a.batch && a.q_offsets[lo + ahead] <= token) lo += ahead;
   }
   return a.ctx_lens[lo] - a.q_lens[lo] + token - a.q_offsets[lo];
 }
@@ -191,26 +199,32 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;  // lanes of a row, heads under way at a time
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned int unit = block * kWaves + wave;
-  const int token = __builtin_amdgcn_readfirstlane((int)(unit / (unsigned int)a.head_parts)), part = (int)(unit - (unsigned int)token * a.head_parts);
-  if (token >= a.total_q) return;
-  const int h0 = part * a.part_heads, h1 = min(a.hq, h0 + a.part_heads);
-  const int col = (threadIdx.x & 63) % kLanes, sub = (threadIdx.x & 63) / kLanes;
+  const int group = __builtin_amdgcn_readfirstlane((int)(unit / (unsigned int)a.head_parts)), part = (int)(unit - (unsigned int)group * a.head_parts);
+  const int first = group * a.wave_tokens;
+  if (first >= a.total_q) return;
+  // the wave's rows of lanes: to tokens, and to heads of theirs
+  const int col = (threadIdx.x & 63) % kLanes, row = (threadIdx.x & 63) / kLanes;
+  const int side = kRows / a.wave_tokens;             // heads of a token under way at a time
+  const int mine = row / side, sub = row - mine * side;
+  const int token = min(first + mine, a.total_q - 1);
+  const int h0 = part * a.part_heads, h1 = first + mine < a.total_q ? min(a.hq, h0 + a.part_heads) : 0;
   const Lane lane(a, col, true);
   Turn turn;
+  const int heads = min(a.hq - h0, a.part_heads);     // (the same in all lanes)
   auto load = [&](Raw<SRC_BYTES> (&r)[kKeep], int h) {
 #pragma unroll
     for (int i = 0; i < kKeep; ++i)
-      if (h + i * kRows < h1) r[i] = fetch<SRC_BYTES>(lane, a.q, token * a.q_stride + (int64_t)min(h + i * kRows + sub, h1 - 1) * D);
+      if (h + i * side < heads) r[i] = fetch<SRC_BYTES>(lane, a.q, token * a.q_stride + (int64_t)(h0 + min(h + i * side + sub, heads - 1)) * D);
   };
   Raw<SRC_BYTES> r[kKeep] = {};
-  load(r, h0);                                        // (on their way while the position is looked up)
-  const int place = a.positions ? 0 : place_of(a, token);
+  load(r, 0);                                         // (on their way while the position is looked up)
+  const int place = a.positions ? 0 : place_of(a, first, token);
   if (lane.turns) look_up(a, col * 4, place, token, turn);
-  for (int h = h0; h < h1; h += kKeep * kRows) {
-    if (h > h0) load(r, h);
+  for (int h = 0; h < heads; h += kKeep * side) {
+    if (h) load(r, h);
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      const int head = h + i * kRows + sub;
+      const int head = h0 + h + i * side + sub;
       if (head < h1) store<SRC_BYTES, STREAM>(a, lane, turn, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
     }
   }
@@ -224,6 +238,7 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 // pages 156 and 148, among them 139 and 117, with the streaming hint 133 and 112: 6.0 and 5.4 TB/s where a streaming pass over as
 // many bytes reaches 6.2.  Fewer workgroups that take several pages each: slower by 5 to 20 %.  Rows held as floats until their scale is
 // known instead of turned twice: three workgroups per CU instead of five.
+// 180000 tokens of 8/2/64 (540 MB), whose queries fill a wave's registers eight tokens at a time: 212 us with a wave per token, 143 so.
 // 512 single tokens (64/4/128, int8; between events around the launch): 11.4 us with a search for each token's trajectory and a wave per
 // four query heads, 10.2 without the search, 8.8 with a wave per sixteen.
 // POOL: -1 the source type, else a KvKind; STREAM: rotated queries are written with the streaming hint
@@ -472,6 +487,10 @@ hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, in
   // a run of n tokens touches at most this many pages, wherever it starts
   const int64_t longest = std::min(max_q_len, a.total_q);
   a.pages = longest > 0 ? (int32_t)std::min<int64_t>((longest + kPageSize - 2) / kPageSize + 1, kMostPages) : 1;
+  // Small pages: a workgroup costs about as much to start as one's rows do, and most of those for the longest chunk's pages would
+  // have nothing to do, so there are as many as the mean chunk has pages, and they take turns.  512 chunks of 64 .. 1024 tokens
+  // (8/2/64, int8) 143 -> 133 us, 128 of 32 .. 512 (64/4/128) 148 -> 143; with 8 heads of 128 (64 chunks of 64 .. 1024) 109 -> 118.
+  if ((int64_t)a.hkv * head_dim <= kSmallPage) a.pages = (int32_t)std::min<int64_t>(a.pages, a.total_q / ((int64_t)kPageSize * a.batch) + 2);
   const int64_t page_groups = ((int64_t)a.pages * a.batch + kXcds - 1) / kXcds * 2;
   int64_t groups = page_groups;
   bool stream = false;
@@ -481,8 +500,11 @@ hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, in
     const int64_t parts = std::clamp<int64_t>(kQueryWaves / a.total_q, (most + kKeep - 1) / kKeep, most);
     a.part_heads = (int)((most + parts - 1) / parts) * rows;
     a.head_parts = (a.hq + a.part_heads - 1) / a.part_heads;
+    // ... and several tokens where their heads are few and there are waves enough even so
+    a.wave_tokens = 1;
+    while (2 * a.wave_tokens <= rows && 2 * a.wave_tokens * a.hq <= rows * kKeep && a.total_q / (2 * a.wave_tokens) >= kQueryWaves) a.wave_tokens *= 2;
     stream = (int64_t)a.total_q * a.hq * head_dim * src_bytes > kStreamQueries;
-    groups += ((int64_t)a.total_q * a.head_parts + kWaves * kXcds - 1) / (kWaves * kXcds);
+    groups += ((((int64_t)a.total_q + a.wave_tokens - 1) / a.wave_tokens) * a.head_parts + kWaves * kXcds - 1) / (kWaves * kXcds);
   }
   if (groups * kXcds > INT32_MAX || (int64_t)a.total_q * a.head_parts > INT32_MAX) return hipErrorInvalidValue;
   a.page_share = (((uint64_t)page_groups << 32) + groups - 1) / groups;   // (rounded up: behind the last group there have been them all)

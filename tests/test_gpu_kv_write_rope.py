@@ -213,6 +213,34 @@ def test_a_pool_past_four_gigabytes():
     same((None, pool[ids], other[ids], scale[ids], vscale[ids]), want)
 
 
+@pytest.mark.parametrize("heads,d,tokens", [((8, 2), 64, 5000), ((8, 2), 64, 10000), ((4, 1), 64, 36000), ((3, 1), 128, 9000), ((1, 1), 128, 20000), ((20, 4), 64, 5000)])
+@pytest.mark.parametrize("kv", ["int8_head", "bf16"])
+def test_many_tokens_of_few_heads(heads, d, tokens, kv):
+    """Several tokens to a wave, of trajectories that come and go between them; workgroups that take several pages of one chunk."""
+    rng = np.random.default_rng(tokens)
+    new = rng.integers(0, 3, 400) * rng.integers(0, 2, 400)
+    long = rng.permutation(400)[:12]
+    new[long] = 0
+    new[long] = rng.multinomial(tokens - int(new.sum()), np.arange(1, 13) / 78)
+    b = batch_of("t", heads, d, "bf16", kv, ("uniform", 0, 40), ("const", 0), 97, batch=400)
+    ctx = b.ctx_lens_host + new
+    pages = -(-ctx // 16)
+    perm, at = rng.permutation(int(pages.sum())), 0
+    table = np.full((400, int(pages.max())), -1, dtype=np.int32)
+    for i, n in enumerate(pages):
+        table[i, :n] = perm[at:at + n]
+        at += n
+    ints = lambda x: torch.from_numpy(np.asarray(x).astype(np.int32)).to(DEV)
+    b.ctx_lens_host, b.q_lens_host, b.ctx_lens, b.q_lens = ctx, new, ints(ctx), ints(new)
+    b.q_offsets, b.page_table = ints(np.concatenate([[0], np.cumsum(new)])), ints(table)
+    grow = lambda t: None if t is None else torch.zeros((at, *t.shape[1:]), dtype=t.dtype, device=DEV) + (1 if t.dtype == torch.float32 else 0)
+    b.k_pages, b.v_pages, b.k_scale, b.v_scale = (grow(t) for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale))
+    gen = torch.Generator().manual_seed(16)
+    q, k, v = (rows_of(gen, tokens, h, d, "bf16") for h in (heads[0], heads[1], heads[1]))
+    got, want = both(b, q, k, v, table_of(int(ctx.max()), d))
+    same(got, want)
+
+
 def test_queries_past_what_the_caches_hold():
     """More than 128 MB of them are written with another kind of store."""
     b = batch_of("t", (96, 2), 128, "bf16", "int8_head", ("uniform", 0, 30), ("uniform", 500, 900), 85)
