@@ -238,7 +238,8 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 // pages 156 and 148, among them 139 and 117, with the streaming hint 133 and 112: 6.0 and 5.4 TB/s where a streaming pass over as
 // many bytes reaches 6.2.  Fewer workgroups that take several pages each: slower by 5 to 20 %.  Rows held as floats until their scale is
 // known instead of turned twice: three workgroups per CU instead of five.
-// 180000 tokens of 8/2/64 (540 MB), whose queries fill a wave's registers eight tokens at a time: 212 us with a wave per token, 143 so.
+// 180000 tokens of 8/2/64 (540 MB), whose queries fill a wave's registers eight tokens at a time: 212 us with a wave per token, 143 so,
+// 133 with fewer workgroups for its small pages (below).
 // 512 single tokens (64/4/128, int8; between events around the launch): 11.4 us with a search for each token's trajectory and a wave per
 // four query heads, 10.2 without the search, 8.8 with a wave per sixteen.
 // POOL: -1 the source type, else a KvKind; STREAM: rotated queries are written with the streaming hint
