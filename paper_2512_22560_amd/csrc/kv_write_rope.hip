@@ -29,7 +29,7 @@ constexpr int kQueryWaves = 2048; // queries: waves wanted where there are few t
 // with the streaming hint, by instances of their own (a branch between the two in one instance: 139 -> 147 us): 363 and 220 MB of
 // them 139 -> 133 and 117 -> 112 us alone, 719 -> 719 and 376 -> 375 with attn_append behind; 41 MB of them 244 -> 246 with it.
 constexpr int64_t kStreamQueries = 128 << 20;
-constexpr int kSmallPage = 512;   // elements of a token's keys up to which pages are small
+constexpr int kSmallPage = 256;   // elements of a token's keys up to which pages are small
 constexpr int kMostPages = 4096;  // pages of a trajectory with a workgroup of their own
 
 template <int SRC_BYTES>
@@ -490,7 +490,8 @@ hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, in
   a.pages = longest > 0 ? (int32_t)std::min<int64_t>((longest + kPageSize - 2) / kPageSize + 1, kMostPages) : 1;
   // Small pages: a workgroup costs about as much to start as one's rows do, and most of those for the longest chunk's pages would
   // have nothing to do, so there are as many as the mean chunk has pages, and they take turns.  512 chunks of 64 .. 1024 tokens
-  // (8/2/64, int8) 143 -> 133 us, 128 of 32 .. 512 (64/4/128) 148 -> 143; with 8 heads of 128 (64 chunks of 64 .. 1024) 109 -> 118.
+  // (8/2/64, int8) 143 -> 133 us, 256 of them with 8/1/128 101 -> 100, with 8/4/64 the same; with 512 elements of a token's keys
+  // 148 -> 144 or 134 -> 138 (128 chunks of 32 .. 512, 64/4/128), 137 -> 140 (16/8/64), with 1024 109 -> 118 (32/8/128).
   if ((int64_t)a.hkv * head_dim <= kSmallPage) a.pages = (int32_t)std::min<int64_t>(a.pages, a.total_q / ((int64_t)kPageSize * a.batch) + 2);
   const int64_t page_groups = ((int64_t)a.pages * a.batch + kXcds - 1) / kXcds * 2;
   int64_t groups = page_groups;
