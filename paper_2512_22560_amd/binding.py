@@ -359,7 +359,11 @@ def _row_stride(t: torch.Tensor, heads: int, d: int) -> int:
     """Elements between the rows of consecutive tokens; a token's heads lie side by side."""
     step, head, item = t.stride()
     if (head == d or heads == 1) and item == 1:
-        return step if t.shape[0] > 1 else heads * d
+        if t.shape[0] <= 1:
+            return heads * d
+        if step < heads * d:                  # (one row for all of them, say: a step of 0 means dense rows to the library)
+            raise ValueError("the rows of tokens do not overlap")
+        return step
     if t.numel():
         raise ValueError("the heads of a token lie side by side")
     return heads * d

@@ -840,7 +840,7 @@ int kv_write_rope(const rollattn_desc* desc, const rollattn_rope* rope, const vo
       !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(page_table) || !aligned16(ctx_lens) || !aligned16(rope->cos_sin) ||
       !aligned16(rope->positions) || (codes && (!aligned16(k_scale) || !aligned16(v_scale))))
     return ROLLATTN_EALIGN;
-  if (desc->batch > 65535) return ROLLATTN_ESHAPE;     // one grid row per trajectory
+  if (desc->batch > 65535) return ROLLATTN_ESHAPE;     // as kv_write, whose grid has a row per trajectory
   a.q = q; a.k_new = k_new; a.v_new = v_new; a.q_out = q_out; a.k_pages = k_pages; a.v_pages = v_pages;
   a.q_lens = q_lens; a.q_offsets = q_offsets; a.page_table = page_table; a.ctx_lens = ctx_lens;
   a.k_scale = k_scale; a.v_scale = v_scale;

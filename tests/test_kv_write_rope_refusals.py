@@ -88,3 +88,15 @@ def test_the_binding_refuses_what_the_library_cannot_see():
                             stream=0)
     with pytest.raises(ValueError):
         B.make_desc(base["q"], base["k_pages"], base["page_table"], sm_scale=1.0, k_scale=torch.zeros(5), v_scale=torch.zeros(5))
+
+
+@pytest.mark.parametrize("name", ["q", "k_new", "v_new"])
+def test_one_row_for_all_tokens_is_refused(name):
+    """A step of zero between tokens means dense rows to the library, which would read past an expanded row."""
+    bf = torch.bfloat16
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)
+    rows = {n: torch.zeros(3, h, 64, dtype=bf) for n, h in (("q", 4), ("k_new", 2), ("v_new", 2))}
+    rows[name] = rows[name][:1].expand(3, -1, -1)
+    with pytest.raises(ValueError, match="overlap"):
+        B.kv_write_rope(*rows.values(), ints(1), ints(2), torch.zeros(5, 2, 16, 64, dtype=bf), torch.zeros(5, 2, 16, 64, dtype=bf), ints(1, 4), ints(1),
+                        cos_sin=torch.zeros(8, 64), max_q_len=3, stream=0)
