@@ -424,7 +424,7 @@ def main():
     if not torch.cuda.is_available():
         print("bench.py: no GPU visible", file=sys.stderr)
         sys.exit(1)
-    if not os.path.exists(B.LIB_PATH):      # fresh checkout: build once; what is built is used as it is
+    if not (os.path.exists(B.LIB_PATH) and os.path.exists(B.HOST_PATH)):      # fresh checkout: build once; what is built is used as it is
         import __graft_entry__
         __graft_entry__.build()
     B.lib()   # fails loudly if the HIP library still is not there

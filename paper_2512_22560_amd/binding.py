@@ -1,4 +1,4 @@
-"""ctypes binding of librollattn's C ABI for torch tensors.
+"""Binding of librollattn's C ABI for torch tensors, through ctypes and a small module for the calls of every step.
 
 Argument marshalling only: every step of the attention path (planning, paged loads,
 softmax, the split-K merge) runs in the library's HIP kernels.  torch supplies device
@@ -16,6 +16,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librollattn.so")
+HOST_PATH = os.path.join(_HERE, "_host_calls.so")
 
 F32, BF16, FP8_E4M3, FP8_E4M3_HEAD, INT8_HEAD = 0, 1, 2, 3, 4
 EXPORTS = (
@@ -135,9 +136,26 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_host = None
+
+
+def _load_host():
+    """The checks and the unpacking of attn_decode, attn_append and kv_write_rope as a module of its own (csrc/host_calls.cpp), which is
+    told the library's addresses."""
+    global _host
+    l = lib()
+    try:
+        from . import _host_calls
+    except ImportError as e:
+        raise RuntimeError("the _host_calls module is missing: build it with `python -m paper_2512_22560_amd.build`") from e
+    _host_calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (l.kv_write_rope, l.attn_decode, l.attn_append)))
+    _host = _host_calls
+    return _host
+
+
 # What follows runs on the host in front of every launch, and the smallest calls are no longer than it (a decode step of
 # four short float32 contexts: 4 us on the GPU), so it stays short: addresses as plain integers, the descriptor's fields by
-# position, the current stream's handle without a stream object.
+# position, the current stream's handle without a stream object.  The calls of every step leave theirs to the module above.
 _DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.uint8: FP8_E4M3, torch.float8_e4m3fn: FP8_E4M3, torch.int8: INT8_HEAD}
 
 
@@ -203,14 +221,11 @@ def _check_contig(*ts):
 def attn_decode(q, k_pages, v_pages, page_table, ctx_lens, *, sm_scale, k_scale=None, v_scale=None,
                 out=None, workspace=None, stream=None) -> torch.Tensor:
     """out[b, h, :] = attention of q[b, h, :] over trajectory b's cached tokens."""
-    _check_contig(q, k_pages, v_pages, page_table, ctx_lens, k_scale, v_scale, out)
-    desc = make_desc(q, k_pages, page_table, sm_scale=sm_scale, k_scale=k_scale, v_scale=v_scale)
     if out is None:
-        out = torch.empty_like(q)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if workspace is None:
-        workspace = alloc_workspace(desc, q.shape[0], q.device)
-    rc = lib().attn_decode(ctypes.byref(desc), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
-                           _ptr(ctx_lens), _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream))
+        workspace = alloc_workspace(make_desc(q, k_pages, page_table, sm_scale=sm_scale, k_scale=k_scale, v_scale=v_scale), q.shape[0], q.device)
+    rc = (_host or _load_host()).attn_decode(q, k_pages, v_pages, page_table, ctx_lens, sm_scale, k_scale, v_scale, out, workspace, _stream(stream))
     if rc:
         raise RollattnError(rc, "attn_decode")
     return out
@@ -232,16 +247,12 @@ def attn_decode_static(q, k_pages, v_pages, page_table, ctx_lens, *, sm_scale, k
 def attn_append(q_chunk, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, sm_scale, max_q_len,
                 k_scale=None, v_scale=None, out=None, workspace=None, stream=None) -> torch.Tensor:
     """Rows of q_chunk (packed by trajectory) attend causally inside their chunk and fully to the prefix."""
-    _check_contig(q_chunk, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, k_scale, v_scale, out)
-    desc = make_desc(q_chunk, k_pages, page_table, sm_scale=sm_scale, k_scale=k_scale, v_scale=v_scale)
-    total_q = int(q_chunk.shape[0])
     if out is None:
-        out = torch.empty_like(q_chunk)
+        out = torch.empty_like(q_chunk, memory_format=torch.contiguous_format)
     if workspace is None:
-        workspace = alloc_workspace(desc, total_q, q_chunk.device)
-    rc = lib().attn_append(ctypes.byref(desc), _ptr(q_chunk), _ptr(q_lens), _ptr(q_offsets), total_q,
-                           int(max_q_len), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(ctx_lens),
-                           _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream))
+        workspace = alloc_workspace(make_desc(q_chunk, k_pages, page_table, sm_scale=sm_scale, k_scale=k_scale, v_scale=v_scale), q_chunk.shape[0], q_chunk.device)
+    rc = (_host or _load_host()).attn_append(q_chunk, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, sm_scale, max_q_len, k_scale, v_scale, out,
+                                             workspace, _stream(stream))
     if rc:
         raise RollattnError(rc, "attn_append")
     return out
@@ -355,20 +366,6 @@ def kv_write(k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_
         raise RollattnError(rc, "kv_write")
 
 
-def _row_stride(t: torch.Tensor, heads: int, d: int) -> int:
-    """Elements between the rows of consecutive tokens; a token's heads lie side by side."""
-    step, head, item = t.stride()
-    if (head == d or heads == 1) and item == 1:
-        if t.shape[0] <= 1:
-            return heads * d
-        if step < heads * d:                  # (one row for all of them, say: a step of 0 means dense rows to the library)
-            raise ValueError("the rows of tokens do not overlap")
-        return step
-    if t.numel():
-        raise ValueError("the heads of a token lie side by side")
-    return heads * d
-
-
 def kv_write_rope(q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, cos_sin, max_q_len,
                   positions=None, pair_axes=None, interleaved=False, k_scale=None, v_scale=None, q_out=None, stream=None):
     """kv_write with the position rotation on the way: returns the rotated queries (None where q is None).
@@ -377,48 +374,11 @@ def kv_write_rope(q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_tab
     that is a multiple of 16 bytes).  cos_sin [num_positions, rot_dim] float32: the cosines of the rot_dim / 2 pairs, then
     their sines; pair j is (j, j + rot_dim / 2), or (2 j, 2 j + 1) with `interleaved`.  positions [axes, total_q] int32 (or
     [total_q]; None: a token's place in its context), pair_axes: the axis of each pair, a sequence of rot_dim / 2 whole numbers."""
-    _check_contig(q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, cos_sin, positions, k_scale, v_scale, q_out)
-    rows, pool, dtype = k_new.shape, k_pages.shape, k_new.dtype
-    total_q, hkv, d = rows
-    if v_new.shape != rows or v_pages.shape != pool or hkv != pool[1] or d != pool[3]:
-        raise ValueError("k_new and v_new are [total_q, Hkv, D] rows of the pools")
-    if v_new.dtype is not dtype or v_pages.dtype is not k_pages.dtype:
-        raise TypeError("q, k_new and v_new are of one type, and so are the pools")
-    num_positions, rot_dim = cos_sin.shape
-    if cos_sin.dtype is not torch.float32:
-        raise TypeError("cos_sin is [num_positions, rot_dim] float32")
-    hq, q_stride, axes = hkv, 0, 1
-    if q is not None:
-        rows_q = q.shape
-        hq = rows_q[1]
-        if rows_q[0] != total_q or rows_q[2] != d:
-            raise ValueError("q is [total_q, Hq, D]")
-        if q.dtype is not dtype:
-            raise TypeError("q, k_new and v_new are of one type, and so are the pools")
-        q_stride = _row_stride(q, hq, d)
-        if q_out is None:
-            q_out = torch.empty(rows_q, dtype=dtype, device=q.device)
-        elif q_out.shape != rows_q or q_out.dtype is not dtype:
-            raise ValueError("q_out takes the rotated q")
-    elif q_out is not None:
-        raise ValueError("q_out takes the rotated q")
-    if positions is not None:
-        axes = positions.shape[0] if positions.dim() == 2 else 1
-        if positions.dtype is not torch.int32 or positions.numel() != axes * total_q or positions.dim() > 2:
-            raise ValueError("positions is [axes, total_q] int32")
-    if pair_axes is not None:
-        pair_axes = bytes(pair_axes)
-        if 2 * len(pair_axes) != rot_dim:
-            raise ValueError("pair_axes has an axis for each pair")
-    elif axes > 1:
-        raise ValueError("several axes need pair_axes")
-    table = page_table.shape
-    desc = Desc(table[0], hq, hkv, d, pool[2], table[1], pool[0], _dtype_code(k_new), _kv_code(k_pages, k_scale, v_scale), 1.0, None, None)
-    rope = Rope(cos_sin.data_ptr(), _ptr(positions), pair_axes, num_positions, rot_dim, axes, 1 if interleaved else 0, q_stride,
-                _row_stride(k_new, hkv, d), _row_stride(v_new, hkv, d))
-    rc = lib().kv_write_rope(ctypes.byref(desc), ctypes.byref(rope), _ptr(q), k_new.data_ptr(), v_new.data_ptr(), q_lens.data_ptr(),
-                             q_offsets.data_ptr(), total_q, int(max_q_len), _ptr(q_out), k_pages.data_ptr(), v_pages.data_ptr(),
-                             page_table.data_ptr(), ctx_lens.data_ptr(), _ptr(k_scale), _ptr(v_scale), _stream(stream))
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    rc = (_host or _load_host()).kv_write_rope(
+        q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, cos_sin, max_q_len, positions,
+        None if pair_axes is None else bytes(pair_axes), interleaved, k_scale, v_scale, q_out, _stream(stream))
     if rc:
         raise RollattnError(rc, "kv_write_rope")
     return q_out

@@ -1,4 +1,5 @@
-"""Builds librollattn.so (gfx950) from csrc/ with hipcc, in-tree, and libbench_peaks.so (bench.py's peak microbenchmarks)."""
+"""Builds librollattn.so (gfx950) from csrc/ with hipcc, in-tree, libbench_peaks.so (bench.py's peak microbenchmarks), and with g++ the
+module that checks and unpacks the binding's tensors."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -13,6 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librollattn.so")
 PEAKS_LIB = os.path.join(HERE, "libbench_peaks.so")      # the benchmark's two peak microbenchmarks, not part of the library
+HOST_CALLS = os.path.join(HERE, "_host_calls.so")        # host_calls.cpp, a Python module: torch's headers, no GPU code
 SOURCES = ["append_mfma.hip", "append_mfma.hip:head", "decode_mfma.hip", "api.cpp", "plan.hip", "attn_f32.hip", "combine.hip", "kv_write.hip", "kv_write_rope.hip", "shared_prefix.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -44,8 +46,21 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
+def _build_host_calls() -> None:
+    import sysconfig
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-Wall",
+           "-isystem", os.path.join(at, "include"), "-isystem", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
+           os.path.join(CSRC, "host_calls.cpp"), "-o", HOST_CALLS, "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        raise RuntimeError("g++ failed on host_calls.cpp:\n" + r.stderr)
+
+
 def build(extra_flags=(), verbose=False) -> str:
     os.makedirs(OBJ, exist_ok=True)
+    _build_host_calls()
     with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         objs = list(ex.map(lambda s: _compile(s, list(extra_flags)), SOURCES))
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
@@ -58,7 +73,7 @@ def build(extra_flags=(), verbose=False) -> str:
     if r.returncode:
         raise RuntimeError("link failed:\n" + r.stderr)
     if verbose:
-        print("built", LIB, "and", PEAKS_LIB)
+        print("built", LIB, PEAKS_LIB, "and", HOST_CALLS)
     return LIB
 
 

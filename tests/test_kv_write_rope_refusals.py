@@ -100,3 +100,39 @@ def test_one_row_for_all_tokens_is_refused(name):
     with pytest.raises(ValueError, match="overlap"):
         B.kv_write_rope(*rows.values(), ints(1), ints(2), torch.zeros(5, 2, 16, 64, dtype=bf), torch.zeros(5, 2, 16, 64, dtype=bf), ints(1, 4), ints(1),
                         cos_sin=torch.zeros(8, 64), max_q_len=3, stream=0)
+
+
+def test_decode_refuses_what_the_library_cannot_see():
+    bf = torch.bfloat16
+    base = dict(q=torch.zeros(3, 4, 64, dtype=bf), k_pages=torch.zeros(5, 2, 16, 64, dtype=torch.int8), v_pages=torch.zeros(5, 2, 16, 64, dtype=torch.int8),
+                page_table=torch.zeros(3, 4, dtype=torch.int32), ctx_lens=torch.zeros(3, dtype=torch.int32), sm_scale=0.1, k_scale=torch.zeros(5, 2),
+                v_scale=torch.zeros(5, 2), out=torch.zeros(3, 4, 64, dtype=bf), workspace=torch.zeros(16, dtype=torch.uint8))
+    bad = [dict(q=torch.zeros(3, 64, 4, dtype=bf).transpose(1, 2)), dict(out=torch.zeros(4, 3, 64, dtype=bf).transpose(0, 1)), dict(q=torch.zeros(3, 4, 64, dtype=torch.float64)),
+           dict(k_pages=torch.zeros(5, 2, 16, 64, dtype=torch.int16)), dict(page_table=torch.zeros(4, 3, dtype=torch.int32).T), dict(k_scale=torch.zeros(5)),
+           dict(k_pages=torch.zeros(5, 2, 64, dtype=torch.int8)), dict(ctx_lens=[1, 2, 3]), dict(sm_scale="0.1"), dict(workspace=None, k_scale=torch.zeros(4, 2))]
+    for change in bad:
+        with pytest.raises((ValueError, TypeError)):
+            B.attn_decode(**dict(base, **change), stream=0)
+    with pytest.raises(B.RollattnError) as e:                       # what the library says comes back as it is
+        B.attn_decode(**base, stream=0)
+    assert e.value.status == -5                                     # 16 bytes of workspace
+    assert B.attn_decode(**dict(base, q=base["q"][:0], page_table=base["page_table"][:0], ctx_lens=base["ctx_lens"][:0], out=base["out"][:0]), stream=0).shape == (0, 4, 64)
+
+
+def test_append_refuses_what_the_library_cannot_see():
+    bf = torch.bfloat16
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)
+    base = dict(q_chunk=torch.zeros(6, 4, 64, dtype=bf), q_lens=ints(3), q_offsets=ints(4), k_pages=torch.zeros(5, 2, 16, 64, dtype=torch.int8),
+                v_pages=torch.zeros(5, 2, 16, 64, dtype=torch.int8), page_table=ints(3, 4), ctx_lens=ints(3), sm_scale=0.1, max_q_len=4, k_scale=torch.zeros(5, 2),
+                v_scale=torch.zeros(5, 2), out=torch.zeros(6, 4, 64, dtype=bf), workspace=torch.zeros(16, dtype=torch.uint8))
+    bad = [dict(q_chunk=torch.zeros(6, 64, 4, dtype=bf).transpose(1, 2)), dict(q_lens=ints(6)[::2]), dict(v_pages=torch.zeros(5, 16, 2, 64, dtype=torch.int8).transpose(1, 2)),
+           dict(q_chunk=torch.zeros(6, 4, 64, dtype=torch.int64)), dict(v_scale=torch.zeros(5)), dict(page_table=ints(12)), dict(ctx_lens=None), dict(max_q_len=1 << 40),
+           dict(max_q_len=None), dict(workspace=None, v_scale=torch.zeros(4, 2))]
+    for change in bad:
+        with pytest.raises((ValueError, TypeError)):
+            B.attn_append(**dict(base, **change), stream=0)
+    with pytest.raises(B.RollattnError) as e:
+        B.attn_append(**base, stream=0)
+    assert e.value.status == -5
+    none = dict(base, q_chunk=base["q_chunk"][:0], out=base["out"][:0])
+    assert B.attn_append(**none, stream=0).shape == (0, 4, 64)
