@@ -337,10 +337,25 @@ static int decode_prepare(const rollattn_desc* desc, const void* q, const void* 
   return ROLLATTN_OK;
 }
 
+// Whether a call's rows are a workgroup's each, without plan, partials and merge: short contexts whose rows are resident at once, two
+// workgroups to a CU.  us a call, planned and so (int8): 37 contexts of up to 300 tokens (8/2/64) 9.3 -> 6.2, 24 of 100 .. 300
+// (32/8/128) 12.5 -> 8.9, 64 of 30 .. 500 (32/8/128) 20.3 -> 15.7, 128 of 100 .. 500 (64/1/128) 26.4 -> 16.3; but with more rows 211 of
+// 7 .. 25 (32/8/128) 15.1 -> 17.3, 256 of 256 .. 500 49.7 -> 58.7.
+static bool decode_direct(const rollattn_desc* desc, const DecodeArgs& a) {
+  return kv_has_head_scales(kv_kind(*desc)) && desc->max_pages_per_seq <= kDirectPages && (int64_t)desc->batch * a.rows_per_b <= 2 * kNumCUs &&
+         a.whole_rows && !a.shared.result;         // (whole_rows: not where the number of workers is forced)
+}
+
 // The launches behind the plan.
 static int decode_launch(const rollattn_desc* desc, const DecodeArgs& a, hipStream_t s) {
   const bool f32 = desc->q_dtype == ROLLATTN_F32;
   hipError_t e;
+  if (decode_direct(desc, a)) {
+    ProfileScope prof(s);
+    e = launch_decode_direct(a, desc->head_dim, kv_kind(*desc), s);
+    prof.stop();
+    return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
+  }
   {
     ProfileScope prof(s);
     if (f32) {
@@ -365,6 +380,10 @@ static int decode_impl(const rollattn_desc* desc, const void* q, const void* k_p
   if (rc || call.args.batch == 0) return rc;
   hipStream_t s = (hipStream_t)hip_stream;
   const bool f32 = desc->q_dtype == ROLLATTN_F32;
+  if (decode_direct(desc, call.args)) {
+    call.args.plan.header = call.plan.header;
+    return decode_launch(desc, call.args, s);
+  }
   // A launch of its own for the plan costs its 3 to 5 us and the gap behind it.  Small batches do without.  Over MFMA every
   // wave finds its own start, a lane per trajectory (64 contexts of 512 .. 8k, 32/8/128, bf16: 159.6 -> 155.0 us; with more
   // trajectories the step is long enough not to notice).  Short float32 contexts are not cut at all while their rows fit the

@@ -158,10 +158,12 @@ __device__ __forceinline__ uint4 load16(const unsigned char* p) {
 }
 
 // One run of blocks.  WHOLE: it is one row from its first block to its last; FOLD: whose other part, in attn_decode_shared, is there
-// and folded in.
-template <int D, int KV, bool STREAM, bool WHOLE, bool FOLD>
-__device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 start, int worker, unsigned char* const k_lds) {
+// and folded in.  PART: it lies in one row and its result stays in LDS, un-normalised, [heads][D] in the wave's tiles and (max, sum) of
+// every head in part_ml.
+template <int D, int KV, bool STREAM, bool WHOLE, bool FOLD, bool PART = false>
+__device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 start, int worker, unsigned char* const k_lds, float2* const part_ml = nullptr) {
   static_assert(WHOLE || !FOLD, "cut rows are folded by the merge");
+  static_assert(!PART || (WHOLE && !FOLD), "the loop of a whole row, which does not look for the next");
   constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
   constexpr bool INT8 = KV == kKvInt8Head;
   using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
@@ -483,7 +485,14 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
       }
     }
   }
-  if constexpr (WHOLE && !FOLD) end_segment();
+  if constexpr (PART) {
+    static_assert(2 * G_::kTileBytes >= kMfmaHeadTile * D * 4, "a head tile's sums in the place of K and V");
+    const float l_tot = xor32_add(xor16_add(l_run));
+#pragma unroll
+    for (int dt = 0; dt < G_::kDT; ++dt) *(floatx4*)(k_lds + (r16 * D + dt * 16 + q4 * 4) * 4) = acc[dt];
+    if (q4 == 0) part_ml[r16] = make_float2(m_run, l_tot);
+  }
+  if constexpr (WHOLE && !FOLD && !PART) end_segment();
   if constexpr (FOLD) {
     // the private part of a row whose other part is there: both weighted by their denominators, as the merge would
     int b = __builtin_amdgcn_readfirstlane(start.x), r = __builtin_amdgcn_readfirstlane(start.y) >> 20, tid = lane_id();
@@ -569,7 +578,69 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mfma_kernel(const DecodeAr
   else decode_worker<D, KV, true, false, false>(a, start, worker, lds[wave]);
 }
 
+// Contexts that are not worth a plan, partials in memory and a merge: a workgroup per row, whose waves have a quarter of its blocks each
+// and are folded through LDS.  Bound by one chain: length, page ids, tiles (all of a wave's under way at once), products, the fold.  37
+// contexts of up to 300 tokens (8/2/64, E4M3): 5.0 us on the GPU where the two launches of a cut call take 7.5.
+template <int D, int KV>
+__global__ __launch_bounds__(kThreads, 2) void decode_direct_kernel(const DecodeArgs a) {
+  constexpr int kTile = 2 * Geo<D, true>::kTileBytes, kPerThread = kMfmaHeadTile * D / kThreads;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves][kTile];
+  __shared__ float2 ml[kWaves][kMfmaHeadTile];
+  const int b = blockIdx.x / a.rows_per_b, r = blockIdx.x - b * a.rows_per_b;
+  if (a.q_lens && a.q_lens[b] != 1) return;             // mixed step: not a decode row
+  if (a.plan.header && blockIdx.x == 0 && threadIdx.x == 0) a.plan.header[kPlanPer] = a.plan.header[kPlanTotal] = 0;   // (for who reads the plan)
+  const int len = a.ctx_lens[b], n = (len + kBlockTokens - 1) / kBlockTokens;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blk0 = n * wave / kWaves, mine = n * (wave + 1) / kWaves - blk0;
+  if (mine > 0) decode_worker<D, KV, false, true, false, true>(a, make_int4(b, r << 20 | blk0, len, mine), 0, lds[wave], ml[wave]);
+  else if (lane_id() < kMfmaHeadTile) ml[wave][lane_id()] = make_float2(-INFINITY, 0.f);
+  __syncthreads();
+  const int n_ht = a.rows_per_b / a.hkv, g = r / n_ht, h0 = (r - g * n_ht) * kMfmaHeadTile;
+  const int h = threadIdx.x / (D / kPerThread), d0 = threadIdx.x % (D / kPerThread) * kPerThread;
+  if (h0 + h >= a.group) return;
+  float top = -INFINITY, sum = 0.f, o[kPerThread] = {};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][h].x);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float2 part = ml[w][h];
+    if (n * w / kWaves == n * (w + 1) / kWaves) continue;   // (a wave without blocks has left nothing in its tiles)
+    const float weight = __builtin_amdgcn_exp2f(part.x - top);
+    sum += weight * part.y;
+#pragma unroll
+    for (int i = 0; i < kPerThread; i += 4) {
+      const floatx4 x = *(const floatx4*)(lds[w] + (h * D + d0 + i) * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i + e] += weight * x[e];
+    }
+  }
+  const size_t orow = (size_t)(a.q_offsets ? a.q_offsets[b] : b) * a.hq + (size_t)g * a.group + h0 + h;
+  const float inv = n > 0 ? 1.f / sum : 0.f;            // (no tokens: a row of zeros)
+#pragma unroll
+  for (int i = 0; i < kPerThread; i += 4) {
+    bf16x4 pk;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) pk[e] = (__bf16)(o[i + e] * inv);
+    *(bf16x4*)((__bf16*)a.out + orow * D + d0 + i) = pk;
+  }
+  if (a.lse && d0 == 0) a.lse[orow] = n > 0 ? top + __builtin_amdgcn_logf(sum) : -INFINITY;
+}
+
 }  // namespace
+
+hipError_t launch_decode_direct(const DecodeArgs& a, int head_dim, KvKind kv, hipStream_t s) {
+  const dim3 grid((unsigned)a.batch * a.rows_per_b);
+  auto of_kind = [&](auto kind) {
+    constexpr int KV = decltype(kind)::value;
+    if (head_dim == 128) hipLaunchKernelGGL((decode_direct_kernel<128, KV>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((decode_direct_kernel<64, KV>), grid, dim3(kThreads), 0, s, a);
+  };
+  if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
+  if (kv == kKvFp8Head) of_kind(std::integral_constant<int, kKvFp8Head>{});
+  else if (kv == kKvInt8Head) of_kind(std::integral_constant<int, kKvInt8Head>{});
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
 
 hipError_t launch_decode_mfma(const DecodeArgs& a, int head_dim, KvKind kv, int grid, hipStream_t s) {
   auto launch = [&](auto d, auto kind) {

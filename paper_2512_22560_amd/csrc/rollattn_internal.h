@@ -19,7 +19,7 @@ constexpr int kF32HeadTile = 4;         // query heads per float32 decode row
 constexpr int kWavePlanBatch = 64;      // batches up to this size are planned by every decode wave for itself
 constexpr float kWholeBusyFp8 = 900.f, kWholeBusy = 450.f, kWholeGain = 1.f / 130;   // MFMA decode: what rows that stay whole are priced with (plan_whole)
 constexpr int kMfmaDecodeWgsD64 = 3 * kNumCUs;   // MFMA decode, D = 64: workgroups that run at once, all of them where rows stay whole
-constexpr int kDirectPages = 32;        // float32 contexts of at most this many pages are not cut
+constexpr int kDirectPages = 32;        // contexts of at most this many pages are not cut (float32, and 8-bit pools with a scale per head)
 constexpr int kAppendTileRows = 256;    // query rows (token, head-in-group pairs) per append workgroup
 constexpr int kXcds = 8;                // accelerator dies, each with its own L2; workgroups are dealt to them round-robin
 constexpr int kAppendBlockTokens = 64;  // KV tokens staged per step of the append kernel
@@ -212,6 +212,8 @@ hipError_t launch_decode_f32(const DecodeArgs& a, int head_dim, int grid, hipStr
 // float32, one launch for plan, attention and output: a workgroup per row, for tables of at most kDirectPages pages and no more rows than CUs
 hipError_t launch_decode_f32_direct(const DecodeArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_decode_mfma(const DecodeArgs& a, int head_dim, KvKind kv, int grid, hipStream_t s);
+// decode over pools with a scale for each page and head in one launch, without a plan or a merge: a workgroup per row
+hipError_t launch_decode_direct(const DecodeArgs& a, int head_dim, KvKind kv, hipStream_t s);
 hipError_t launch_combine(const DecodeArgs& a, int head_dim, bool out_bf16, hipStream_t s);
 // the same for bf16 rows of which a.shared holds another part of the context: every row is written, to a.shared.result
 hipError_t launch_combine_shared(const DecodeArgs& a, int head_dim, hipStream_t s);

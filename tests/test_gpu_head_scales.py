@@ -321,3 +321,64 @@ def test_gather_of_int8_pages():
     for i, n in enumerate(b.ctx_lens_host.tolist()):
         got = B.debug_gather(b.v_pages, b.page_table, b.ctx_lens, i, 1, n)
         assert np.array_equal(W.raw_numpy(got), O.gather_tokens(W.raw_numpy(b.v_pages), W.raw_numpy(b.page_table), i, 1, n, "int8_head", raw=True))
+
+
+SHORT = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 160, 161, 255, 256, 257, 479, 480, 481, 511, 512]
+
+
+@pytest.mark.parametrize("heads,d", [((8, 2), 64), ((8, 2), 128), ((16, 1), 128), ((5, 1), 64), ((40, 2), 128), ((17, 1), 64)])
+@pytest.mark.parametrize("kv", KV)
+def test_rows_that_one_workgroup_takes(kv, heads, d):
+    """Tables of 32 pages, few rows: every length around the ends of pages, blocks and the waves' shares; one launch, no plan."""
+    b = lengths(build(kv, heads, d, ("const", 512), batch=len(SHORT), seed=21), SHORT)
+    assert b.page_table.shape[1] == 32
+    desc = B.make_desc(b.q, b.k_pages, b.page_table, sm_scale=1.0, k_scale=b.k_scale, v_scale=b.v_scale)
+    ws = B.alloc_workspace(desc, len(SHORT), DEV).fill_(255)
+    out, lse = call(b, "decode_lse", workspace=ws)
+    check(out, b)
+    assert B.read_plan(desc, ws)[1] == 0
+    a = oracle_args(b)
+    want = O.attn_lse(W.raw_numpy(b.q), None, a["k_pages"], a["page_table"], a["ctx_lens"], sm_scale=a["sm_scale"], q_dtype="bf16", kv_dtype=kv, k_scale=a["k_scale"])
+    seen, got = np.isfinite(want), lse.double().cpu().numpy()
+    assert np.array_equal(seen, np.isfinite(got)) and np.abs(got[seen] - want[seen]).max() < 1e-4
+    static = torch.empty_like(b.q)
+    call(b, "decode_static", out=static)
+    assert torch.equal(static, out) and torch.equal(call(b, workspace=ws), out)
+    # what comes out depends on the row alone
+    for i in (1, 9, 20, 27):
+        one = B.attn_decode(b.q[i:i + 1].contiguous(), b.k_pages, b.v_pages, b.page_table[i:i + 1].contiguous(), b.ctx_lens[i:i + 1].clone(), sm_scale=b.workload.sm_scale,
+                            k_scale=b.k_scale, v_scale=b.v_scale)
+        assert torch.equal(one[0], out[i])
+
+
+@pytest.mark.parametrize("batch", [128, 129])
+@pytest.mark.parametrize("kv", KV)
+def test_either_side_of_what_workgroups_take(kv, batch):
+    """512 rows are taken as they are, 516 are planned; a table of 33 pages is, too."""
+    b = build(kv, (8, 4), 64, ("uniform", 0, 500), batch=batch, seed=22)
+    check(call(b), b)
+    c = build(kv, (8, 4), 64, ("const", 528), batch=7, seed=23)
+    check(call(c), c)
+
+
+@pytest.mark.parametrize("kv", KV)
+def test_a_mixed_step_of_short_contexts(kv):
+    b = build(kv, (16, 4), 128, ("uniform", 1, 300), qlen=("uniform", 2, 60), batch=80, seed=24, prefix=True, append_rows=20)
+    assert b.page_table.shape[1] <= 32
+    out = call(b, "step")
+    check(out, b, "append")
+    dec, app = b.select(b.decode_rows()), b.select(b.append_rows())
+    row = lambda part: torch.from_numpy(np.concatenate([np.arange(o, o + n) for o, n in
+                                        zip(np.cumsum(b.q_lens_host) - b.q_lens_host, b.q_lens_host) if (n == 1) == part])).to(DEV)
+    assert torch.equal(out[row(True)], call(dec)) and torch.equal(out[row(False)], call(app, "append"))
+
+
+@pytest.mark.parametrize("kv", KV)
+def test_undefined_queries_of_short_contexts_concern_their_rows_alone(kv):
+    b = lengths(build(kv, (8, 2), 64, ("const", 300), batch=6, seed=25), [300, 40, 1, 170, 33, 290])
+    clean = call(b).clone()
+    b.q[1, 3, 5], b.q[3, 0, 0], b.q[5, 7, 63] = float("nan"), float("inf"), -float("inf")
+    out = call(b)
+    hurt = torch.zeros(6, 8, dtype=torch.bool, device=DEV)
+    hurt[1, 3] = hurt[3, 0] = hurt[5, 7] = True
+    assert torch.equal(out[~hurt], clean[~hurt]) and not torch.isfinite(out[hurt]).any()
