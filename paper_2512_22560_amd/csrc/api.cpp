@@ -337,12 +337,12 @@ static int decode_prepare(const rollattn_desc* desc, const void* q, const void* 
   return ROLLATTN_OK;
 }
 
-// Whether a call's rows are a workgroup's each, without plan, partials and merge: short contexts whose rows are resident at once, two
-// workgroups to a CU.  us a call, planned and so (int8): 37 contexts of up to 300 tokens (8/2/64) 9.3 -> 6.2, 24 of 100 .. 300
-// (32/8/128) 12.5 -> 8.9, 64 of 30 .. 500 (32/8/128) 20.3 -> 15.7, 128 of 100 .. 500 (64/1/128) 26.4 -> 16.3; but with more rows 211 of
-// 7 .. 25 (32/8/128) 15.1 -> 17.3, 256 of 256 .. 500 49.7 -> 58.7.
+// Whether a call's rows are taken as they are, without plan, partials and merge: where the table says that contexts are short.  us a call,
+// planned and so (int8): 37 contexts of up to 300 tokens (8/2/64) 9.3 -> 6.2, 64 of 30 .. 500 (32/8/128) 20.3 -> 15.7, 211 of 7 .. 25
+// 14.7 -> 7.1, 512 of 0 .. 500 (8/2/64) 25.3 -> 16.2, 512 of 256 .. 500 (64/4/128) 53.5 -> 50.9, 468 of 1 .. 134 32.7 -> 25.8; at worst 512 of
+// 100 .. 500 (8/8/128) 70.6 -> 72.1 and 500 of 1 .. 500 66.5 -> 67.6.
 static bool decode_direct(const rollattn_desc* desc, const DecodeArgs& a) {
-  return kv_has_head_scales(kv_kind(*desc)) && desc->max_pages_per_seq <= kDirectPages && (int64_t)desc->batch * a.rows_per_b <= 2 * kNumCUs &&
+  return kv_has_head_scales(kv_kind(*desc)) && desc->max_pages_per_seq <= kDirectPages && (int64_t)desc->batch * a.rows_per_b < (1 << 24) &&
          a.whole_rows && !a.shared.result;         // (whole_rows: not where the number of workers is forced)
 }
 

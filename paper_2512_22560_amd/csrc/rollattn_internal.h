@@ -212,7 +212,7 @@ hipError_t launch_decode_f32(const DecodeArgs& a, int head_dim, int grid, hipStr
 // float32, one launch for plan, attention and output: a workgroup per row, for tables of at most kDirectPages pages and no more rows than CUs
 hipError_t launch_decode_f32_direct(const DecodeArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_decode_mfma(const DecodeArgs& a, int head_dim, KvKind kv, int grid, hipStream_t s);
-// decode over pools with a scale for each page and head in one launch, without a plan or a merge: a workgroup per row
+// decode over pools with a scale for each page and head in one launch, without a plan or a merge: a workgroup or a wave per row
 hipError_t launch_decode_direct(const DecodeArgs& a, int head_dim, KvKind kv, hipStream_t s);
 hipError_t launch_combine(const DecodeArgs& a, int head_dim, bool out_bf16, hipStream_t s);
 // the same for bf16 rows of which a.shared holds another part of the context: every row is written, to a.shared.result

@@ -354,7 +354,7 @@ def test_rows_that_one_workgroup_takes(kv, heads, d):
 @pytest.mark.parametrize("batch", [128, 129])
 @pytest.mark.parametrize("kv", KV)
 def test_either_side_of_what_workgroups_take(kv, batch):
-    """512 rows are taken as they are, 516 are planned; a table of 33 pages is, too."""
+    """512 rows are a workgroup's each, 516 a wave's; a table of 33 pages is planned."""
     b = build(kv, (8, 4), 64, ("uniform", 0, 500), batch=batch, seed=22)
     check(call(b), b)
     c = build(kv, (8, 4), 64, ("const", 528), batch=7, seed=23)
@@ -382,3 +382,31 @@ def test_undefined_queries_of_short_contexts_concern_their_rows_alone(kv):
     hurt = torch.zeros(6, 8, dtype=torch.bool, device=DEV)
     hurt[1, 3] = hurt[3, 0] = hurt[5, 7] = True
     assert torch.equal(out[~hurt], clean[~hurt]) and not torch.isfinite(out[hurt]).any()
+
+
+@pytest.mark.parametrize("heads,d", [((8, 2), 64), ((6, 2), 128), ((34, 2), 128), ((3, 3), 64)])
+@pytest.mark.parametrize("kv", KV)
+def test_rows_that_one_wave_takes(kv, heads, d):
+    """Tables of 32 pages, more than 512 rows; the last workgroup is not full."""
+    ctx = np.random.default_rng(26).permutation(np.tile(SHORT, 10))[:271]
+    b = lengths(build(kv, heads, d, ("const", 512), batch=len(ctx), seed=26), ctx)
+    out, lse = call(b, "decode_lse")
+    check(out, b)
+    a = oracle_args(b)
+    want = O.attn_lse(W.raw_numpy(b.q), None, a["k_pages"], a["page_table"], a["ctx_lens"], sm_scale=a["sm_scale"], q_dtype="bf16", kv_dtype=kv, k_scale=a["k_scale"])
+    seen, got = np.isfinite(want), lse.double().cpu().numpy()
+    assert np.array_equal(seen, np.isfinite(got)) and np.abs(got[seen] - want[seen]).max() < 1e-4
+    assert torch.equal(call(b), out)
+    order = torch.randperm(len(ctx), generator=torch.Generator().manual_seed(1)).to(DEV)       # each row depends on itself alone
+    again = B.attn_decode(b.q[order].contiguous(), b.k_pages, b.v_pages, b.page_table[order].contiguous(), b.ctx_lens[order].contiguous(), sm_scale=b.workload.sm_scale,
+                          k_scale=b.k_scale, v_scale=b.v_scale)
+    assert torch.equal(again, out[order])
+
+
+@pytest.mark.parametrize("kv", KV)
+def test_a_mixed_step_of_many_short_contexts(kv):
+    b = build(kv, (16, 4), 128, ("uniform", 1, 300), qlen=("uniform", 2, 20), batch=200, seed=27, prefix=True, append_rows=40)
+    out = call(b, "step")
+    check(out, b, "append")
+    row = torch.from_numpy(np.concatenate([np.arange(o, o + n) for o, n in zip(np.cumsum(b.q_lens_host) - b.q_lens_host, b.q_lens_host) if n == 1])).to(DEV)
+    assert torch.equal(out[row], call(b.select(b.decode_rows())))
