@@ -176,8 +176,8 @@ int attn_merge(const rollattn_desc *desc, int64_t rows, const void *o1, const fl
  * decode path (planned over those trajectories only), one with q_lens[b] > 1 through the append path, one with
  * q_lens[b] == 0 contributes nothing.  The result is that of attn_append on the same arguments, and row for row
  * bit-identical to what attn_decode and attn_append give on the two sub-batches (within rounding, over pools with a scale
- * for each page and head, where the table is at most 32 pages wide and B * Hkv * ceil(Hq / Hkv / 16) at most 512 for the sub-batch
- * and more for the batch: a row is then the work of four waves in the one and of one wave in the other).  The partition into the two
+ * for each page and head, where the table is at most 64 pages wide and B * Hkv * ceil(Hq / Hkv / 16) at most 512 for the sub-batch
+ * and more for the batch: a row is then one workgroup's in the one and not in the other).  The partition into the two
  * kinds is made on the device from q_lens; nothing is copied to the host, so the call can be captured in a HIP
  * graph.  workspace of at least rollattn_step_workspace_bytes(desc, total_q) bytes. */
 int attn_step(const rollattn_desc *desc, const void *q, const int32_t *q_lens, const int32_t *q_offsets,
@@ -328,7 +328,7 @@ int32_t rollattn_debug_set_decode_workers(int32_t workers);
  * in its run) for the first block of its run, or (-1, 0, 0, 0) for a worker without blocks.  For BF16 queries and
  * more than 64 contexts the call may have given every row whole to one worker instead, where that ends sooner; the records
  * then tell what the equal runs would have been.  Over pools with a scale for each page and head, calls with tables of at most
- * 32 pages are not planned: T is 0 and there are no records.
+ * 32 pages (64, where B * Hkv * ceil(Hq / Hkv / 16) is at most 512) are not planned: T is 0 and there are no records.
  * starts_out must hold 4 * rollattn_plan_workers(desc) int32. */
 int rollattn_debug_read_plan(const rollattn_desc *desc, const void *workspace, int32_t *per_out,
                              int32_t *total_out, int32_t *starts_out, void *hip_stream);

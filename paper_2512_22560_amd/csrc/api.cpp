@@ -341,8 +341,11 @@ static int decode_prepare(const rollattn_desc* desc, const void* q, const void* 
 // planned and so (int8): 37 contexts of up to 300 tokens (8/2/64) 9.3 -> 6.2, 64 of 30 .. 500 (32/8/128) 20.3 -> 15.7, 211 of 7 .. 25
 // 14.7 -> 7.1, 512 of 0 .. 500 (8/2/64) 25.3 -> 16.2, 512 of 256 .. 500 (64/4/128) 53.5 -> 50.9, 468 of 1 .. 134 32.7 -> 25.8; at worst 512 of
 // 100 .. 500 (8/8/128) 70.6 -> 72.1 and 500 of 1 .. 500 66.5 -> 67.6.
+// Twice the pages where the rows are resident at once: 24 of 300 .. 800 (32/8/128) 15.9 -> 13.2, 64 of 100 .. 1000 27.7 -> 25.3, 100 of 500 .. 1000
+// (64/1/128) 35.0 -> 23.9, and 5 of them (32/8/128) 10.9 -> 11.9; with more rows, 320 of 4 .. 1117 (8/2/64), 20.8 -> 28.0.
 static bool decode_direct(const rollattn_desc* desc, const DecodeArgs& a) {
-  return kv_has_head_scales(kv_kind(*desc)) && desc->max_pages_per_seq <= kDirectPages && (int64_t)desc->batch * a.rows_per_b < (1 << 24) &&
+  const int64_t rows = (int64_t)desc->batch * a.rows_per_b;
+  return kv_has_head_scales(kv_kind(*desc)) && desc->max_pages_per_seq <= (rows <= kDirectRowsFew ? kDirectPagesFew : kDirectPages) && rows < (1 << 24) &&
          a.whole_rows && !a.shared.result;         // (whole_rows: not where the number of workers is forced)
 }
 

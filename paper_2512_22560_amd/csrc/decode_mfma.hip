@@ -628,6 +628,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_direct_kernel(const Decode
 
 // The same with a wave per row, for more rows than are resident at once with a workgroup each, two to a CU: 512 of 30 .. 500 tokens
 // (32/8/128, int8) 15.7 us with a workgroup each, 520 of them 21.2 with a wave; 1688 of 7 .. 25 17.3 and 7.1, 2048 of 256 .. 500 58.7 and 47.1.
+// (Eight waves to a row while there are no more rows than CUs: 40 of 30 .. 500 tokens 7.8 -> 8.9, 80 of 500 .. 1000 (8/2/64) 10.5 -> 9.5; not built.)
 template <int D, int KV>
 __global__ __launch_bounds__(kThreads, 2) void decode_rows_kernel(const DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves][2 * Geo<D, true>::kTileBytes];
@@ -650,7 +651,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_rows_kernel(const DecodeAr
 
 hipError_t launch_decode_direct(const DecodeArgs& a, int head_dim, KvKind kv, hipStream_t s) {
   const unsigned rows = (unsigned)a.batch * a.rows_per_b;
-  const bool few = rows <= 2 * kNumCUs;
+  const bool few = rows <= kDirectRowsFew;
   const dim3 grid(few ? rows : (rows + kWaves - 1) / kWaves);
   auto of_dim = [&](auto d, auto kind) {
     constexpr int D = decltype(d)::value, KV = decltype(kind)::value;

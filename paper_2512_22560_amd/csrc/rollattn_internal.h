@@ -20,6 +20,8 @@ constexpr int kWavePlanBatch = 64;      // batches up to this size are planned b
 constexpr float kWholeBusyFp8 = 900.f, kWholeBusy = 450.f, kWholeGain = 1.f / 130;   // MFMA decode: what rows that stay whole are priced with (plan_whole)
 constexpr int kMfmaDecodeWgsD64 = 3 * kNumCUs;   // MFMA decode, D = 64: workgroups that run at once, all of them where rows stay whole
 constexpr int kDirectPages = 32;        // contexts of at most this many pages are not cut (float32, and 8-bit pools with a scale per head)
+constexpr int kDirectPagesFew = 64;     // the latter where their rows are resident at once, a workgroup each
+constexpr int kDirectRowsFew = 512;     // ... two to a CU
 constexpr int kAppendTileRows = 256;    // query rows (token, head-in-group pairs) per append workgroup
 constexpr int kXcds = 8;                // accelerator dies, each with its own L2; workgroups are dealt to them round-robin
 constexpr int kAppendBlockTokens = 64;  // KV tokens staged per step of the append kernel

@@ -354,11 +354,15 @@ def test_rows_that_one_workgroup_takes(kv, heads, d):
 @pytest.mark.parametrize("batch", [128, 129])
 @pytest.mark.parametrize("kv", KV)
 def test_either_side_of_what_workgroups_take(kv, batch):
-    """512 rows are a workgroup's each, 516 a wave's; a table of 33 pages is planned."""
+    """512 rows are a workgroup's each, 516 a wave's; 65 pages are planned for few rows, 33 for many."""
     b = build(kv, (8, 4), 64, ("uniform", 0, 500), batch=batch, seed=22)
     check(call(b), b)
-    c = build(kv, (8, 4), 64, ("const", 528), batch=7, seed=23)
-    check(call(c), c)
+    for tokens, n in ((528, batch), (1024, 7), (1040, 7)):
+        c = lengths(build(kv, (8, 4), 64, ("const", tokens), batch=n, seed=23), tokens - np.arange(n) * 4)
+        desc = B.make_desc(c.q, c.k_pages, c.page_table, sm_scale=1.0, k_scale=c.k_scale, v_scale=c.v_scale)
+        ws = B.alloc_workspace(desc, n, DEV).fill_(255)
+        check(call(c, workspace=ws), c)
+        assert (B.read_plan(desc, ws)[1] > 0) == (tokens == 1040 or n == 129)
 
 
 @pytest.mark.parametrize("kv", KV)
