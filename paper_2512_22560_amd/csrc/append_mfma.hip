@@ -748,6 +748,12 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     }
     const int tok0 = blk * kStepTokens + tok_wave;     // first token of this wave's share of the block
     if (tok0 + kSubs * 32 - 1 > wave_min_pos) {        // causal edge or ragged end inside this block
+      // (faint queries over faint keys: a unit that has gone to zero would make a masked token's exponent undefined.  The scores of such
+      // a row are below 2^-90 with either.)
+      if constexpr (HEAD) {
+#pragma unroll
+        for (int p = 0; p < kPg; ++p) sc[p] = fmaxf(sc[p], 0x1p-126f);
+      }
 #pragma unroll
       for (int sub = 0; sub < kSubs; ++sub)
 #pragma unroll
