@@ -48,12 +48,12 @@
 // Pools with a scale for each page and KV head (E4M3 or int8 codes) take the FP8 path with f16 operands in the second product: a code
 // is exact in either, and probabilities keep 11 bits instead of 8.  So are those of the first over int8 codes, which are cheaper to
 // widen that way.  E4M3 keys are not widened at all (RAW_K): a bf16 number has 8 bits and an E4M3 one 4, so the query is the sum of
-// two E4M3 numbers, its nearest one and the rest (exact for elements down to 2^-10 of the wave's largest; below that the error is at
-// most 2^-18 of the largest, where bf16 itself leaves 2^-9 of each element), and the scores are two products with the codes as they
+// two E4M3 numbers, its nearest one and the rest (exact for elements down to 2^-9 of the row's largest; below that the error is at
+// most 2^-17 of the largest, where bf16 itself leaves 2^-9 of each element), and the scores are two products with the codes as they
 // lie in the pool, at twice the depth per instruction and half the bytes in LDS:
 //   64 chunks of 64 .. 1024 tokens behind 2k .. 16k (32/8/128) 2741 -> 2573 us, 32 of 256 behind 8k (64/4/128) 1695 -> 1585, the
 //   shared half of 64 groups of 8 behind 8192 tokens (64/4/128) 138 -> 130; 64 chunks of 8 behind 4k (half tiles) 124.6 -> 126.3.
-// For the ranges of f16 and E4M3 these queries are multiplied by a power of two per wave (exact; taken back with
+// For the ranges of f16 and E4M3 these queries are multiplied by a power of two per row (exact; taken back with
 // the page's K scale); for that of f16 a row's reference is that of the weights p * vs,
 // 2^kWeightBits below the largest when it moves; it moves when a lane's weights of a page add up to more than kHalfSumLimit, so none
 // is ever too large for f16, and one 2^-22 of the largest still is a normal number.
@@ -95,7 +95,7 @@ constexpr float kSumLimit = 16384.f;               // a lane's 32 probabilities 
 
 constexpr float kHalfSumLimit = 65000.f;           // the same for f16 weights, none of which may pass 65504
 constexpr float kWeightBits = 8.f;                 // f16: log2 of a row's largest weight when its reference moves
-constexpr int kDigitBits = 8;                      // E4M3 parts of a query: a wave's largest element is below two to this
+constexpr int kDigitBits = 8;                      // E4M3 parts of a query: a row's largest element is below two to this
 constexpr int kQueryBits = 15;                     // f16: a row's largest query element is below two to this
 
 // Row t of an S^T tile holds this token of its 16-token group: the middle two quads are
@@ -109,18 +109,6 @@ __device__ __forceinline__ float xor32_max(float x) {
 __device__ __forceinline__ float xor32_add(float x) {
   uintx2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Largest of a whole number per lane, in all lanes.
-__device__ __forceinline__ int wave_max(int x) {
-  x = max(x, __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true));    // the neighbour, the other two of four, ...
-  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true));
-  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));
-  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));
-  uintx2 r = __builtin_amdgcn_permlane16_swap((unsigned int)x, (unsigned int)x, false, false);
-  x = max((int)r[0], (int)r[1]);
-  r = __builtin_amdgcn_permlane32_swap((unsigned int)x, (unsigned int)x, false, false);
-  return max((int)r[0], (int)r[1]);
 }
 
 // Pair PAIR of sixteen E4M3 codes to bf16, exactly (every E4M3 value is a bf16 value): the hardware's scaled
@@ -457,7 +445,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
     for (int kk = 0; kk < kKK; ++kk) qop[kk] = *(const kx8*)(qrow + (RAW_K ? kk / 4 * 64 + h2 * 32 + kk % 4 * 8 : kk * 16 + h2 * 8));   // bf16 pools: scaled further down; int8: so far only moved
   }
-  float q_unit = 1.f;                            // int8, RAW_K: what a unit of this wave's rows is worth
+  float q_unit = 1.f;                            // HEAD: what a unit of this lane's row is worth
   intx8 q_digit[RAW_K ? 2 : 1][kDigitSteps];     // RAW_K: the query's leading and trailing parts
 
   floatx16 acc[kDT];
@@ -914,9 +902,9 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       for (int j = 0; j < kLoads; ++j)
         if (kAllThreadsLoad || (j * kThreads + tid) / kSrcChunks < kStepTokens) put(wptr[j][0], wptr[j][1], 0, k0[j]);
       if constexpr (HEAD) {
-        // the wave's largest element, so that the power stays in a scalar register: two magnitudes at a time, as whole numbers, which order
-        // the same (f16: exact for all above 2^-32 of it); raised so far that infinite and undefined ones, which concern their own
-        // rows alone, wrap round to below zero
+        // the row's largest element: two magnitudes at a time, as whole numbers, which order the same; raised so far that infinite and
+        // undefined ones, which concern their own rows alone, wrap round to below zero.  A power for each row, not for the wave's 32: a
+        // loud row would take its neighbours' bits away.
         typedef short shortx2 __attribute__((ext_vector_type(2)));
         typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
         shortx2 tops = {0x80, 0x80};
@@ -926,8 +914,10 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
           for (int w = 0; w < 4; ++w) tops = __builtin_elementwise_max(tops, __builtin_bit_cast(shortx2, __builtin_bit_cast(ushortx2, v[w] & 0x7fff7fffu) + ushortx2{0x80, 0x80}));
         }
-        const float top = __int_as_float((wave_max(max((int)tops[0], (int)tops[1])) - 0x80) << 16);
-        const int up = (RAW_K ? kDigitBits : kQueryBits) - __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top));
+        const unsigned int half_top = (unsigned int)max((int)tops[0], (int)tops[1]);
+        const uintx2 both = __builtin_amdgcn_permlane32_swap(half_top, half_top, false, false);   // the row's two lanes
+        const float top = __uint_as_float((max(both[0], both[1]) - 0x80) << 16);
+        const int up = (RAW_K ? kDigitBits : kQueryBits) - __builtin_amdgcn_frexp_expf(top);
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
           const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
@@ -950,7 +940,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
             }
           }
         }
-        q_unit = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(__builtin_amdgcn_ldexpf(1.f, -up))));
+        q_unit = __builtin_amdgcn_ldexpf(1.f, -up);
       }
     } else {
       // The query rows have been under way as long as the page ids; their scaling (bf16 pools: the scores then leave the
