@@ -95,6 +95,7 @@ constexpr float kSumLimit = 16384.f;               // a lane's 32 probabilities 
 
 constexpr float kHalfSumLimit = 65000.f;           // the same for f16 weights, none of which may pass 65504
 constexpr float kWeightBits = 8.f;                 // f16: log2 of a row's largest weight when its reference moves
+constexpr float kMostBits = 15.f;                  // ... and the most that rounding may make of it
 constexpr int kDigitBits = 8;                      // E4M3 parts of a query: a row's largest element is below two to this
 constexpr int kQueryBits = 15;                     // f16: a row's largest query element is below two to this
 
@@ -752,7 +753,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
     }
     const float m_old = m_ref;                         // what the exponents in s (bf16 pools) are relative to
     float p[kSubs][16];
-    // exponentials of the block against reference m_old + shift, and this lane's share of the row sums
+    // exponentials of the block against reference m_old + shift (HEAD, the second time: against shift), and this lane's share of the row sums
     float weights = 0.f;                               // f16: what says whether the reference has to move
     auto exponentials = [&](auto first_c, float shift) __attribute__((always_inline)) -> float {
       float ad[kPg], psum[kPg];
@@ -766,7 +767,8 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
         for (int i = 0; i < 16; ++i) {
           const int pg = sub * 2 + (i >> 3);
           float x;
-          if constexpr (FP8) x = __builtin_fmaf(s[sub][i], sc[pg], ad[pg]);
+          if constexpr (HEAD && !decltype(first_c)::value) x = __builtin_fmaf(s[sub][i], sc[pg], lvs[pg]) - shift;
+          else if constexpr (FP8) x = __builtin_fmaf(s[sub][i], sc[pg], ad[pg]);
           else if constexpr (decltype(first_c)::value) x = s[sub][i];
           else x = s[sub][i] - shift;
           p[sub][i] = __builtin_amdgcn_exp2f(x);
@@ -795,14 +797,21 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       float mloc;
       if constexpr (HEAD) {
 #pragma unroll
-        for (int q = 0; q < kPg; ++q) pm[q] = __builtin_fmaf(pm[q], sc[q], lvs[q] - kWeightBits);
+        for (int q = 0; q < kPg; ++q) pm[q] = __builtin_fmaf(pm[q], sc[q], lvs[q]);
         mloc = fmaxf(pm[0], pm[1]);
         if constexpr (kPg == 4) mloc = fmaxf(mloc, fmaxf(pm[kPg - 2], pm[kPg - 1]));
       } else if constexpr (kPg == 2) mloc = FP8 ? fmaxf(pm[0] * sc[0], pm[1] * sc[1]) : fmaxf(pm[0], pm[1]) + m_old;
       else if constexpr (FP8) mloc = fmaxf(fmaxf(pm[0] * sc[0], pm[1] * sc[1]), fmaxf(pm[2] * sc[2], pm[3] * sc[3]));
       else mloc = fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])) + m_old;
       const float m_run = seen_max();
-      const float m_new = fmaxf(m_run, xor32_max(mloc));           // the same in both lanes of a row
+      mloc = xor32_max(mloc);                                      // the same in both lanes of a row
+      if constexpr (HEAD) {
+        // (of a score past 2^25 the difference may come out larger, more than f16 holds; exponents below are differences of numbers
+        // that were rounded like this one, so none is larger)
+        const float below = mloc - kWeightBits;
+        mloc = mloc - below > kMostBits ? mloc : below;
+      }
+      const float m_new = fmaxf(m_run, mloc);
       const float m_safe = (m_new == -INFINITY) ? 0.f : m_new;     // rows that see nothing yet
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_safe);
       l_run *= alpha;
@@ -816,7 +825,7 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
 #pragma unroll
         for (int i = 0; i < 16; ++i) negm[i] = -m_safe;
       }
-      lane_sum = exponentials(std::false_type{}, m_safe - m_old);
+      lane_sum = exponentials(std::false_type{}, HEAD ? m_safe : m_safe - m_old);
     }
     l_run += lane_sum;
 #pragma unroll

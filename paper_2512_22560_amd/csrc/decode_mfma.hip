@@ -49,7 +49,8 @@ typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
-constexpr float kWeightBits = 14.f;   // f16 weights: log2 of the largest
+constexpr float kWeightBits = 14.f;   // f16 weights: log2 of the largest,
+constexpr float kMostBits = 15.f;     // ... and the most that rounding may make of it
 constexpr int kQueryBits = 15;        // f16 queries: the largest is below two to this
 
 template <int D, bool FP8>
@@ -419,7 +420,11 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
     }
     float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     mx = xor32_max(xor16_max(mx));
-    if constexpr (HEAD) mx -= kWeightBits;
+    if constexpr (HEAD) {
+      // (of a score past 2^25 the difference may come out larger, more than f16 holds)
+      const float below = mx - kWeightBits;
+      mx = mx - below > kMostBits ? mx : below;
+    }
     const float m_new = fmaxf(m_run, mx);       // finite: the first token of a block is always live
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
     float psum = 0.f;

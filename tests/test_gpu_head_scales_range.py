@@ -1,5 +1,5 @@
 """Queries of any magnitude over 8-bit pools with a scale for each page and KV head: faint ones over faint keys, rows of very
-different magnitudes side by side.
+different magnitudes side by side, scores past what float32 resolves.
 
 The bound is that of tests/test_gpu_head_scales.py, with one more term where appended queries meet E4M3 keys.  There a query is
 the sum of two E4M3 numbers, under a power of two that puts its row's largest element between 2^7 and 2^8.  The nearest E4M3 number
@@ -64,3 +64,16 @@ def test_ordinary_rows_next_to_loud_ones(kv, which, qlen):
     assert np.isfinite(got[ordinary]).all()
     worst = float((np.abs(got - ref) / bound)[ordinary].max())
     assert worst <= 1.0, f"{worst:.2f} times the bound"
+
+
+@pytest.mark.parametrize("power", [22, 23, 24, 25, 26, 27, 28, 40, 96])
+@pytest.mark.parametrize("which,qlen", SHAPES)
+@pytest.mark.parametrize("kv", KV)
+def test_scores_past_what_float32_resolves(kv, which, qlen, power):
+    """Which of the largest scores' tokens win is a matter of rounding there, but an output stays a mean of values."""
+    b = batch(kv, which, qlen, seed=44)
+    b.q = (b.q.float() * 2.0 ** power).to(torch.bfloat16)
+    got = call(b, which).float()
+    a = oracle_args(b)
+    most = max(np.abs(O.gather_tokens(a["v_pages"], a["page_table"], i, g, int(n), kv, a["v_scale"])).max() for i, n in enumerate(b.ctx_lens_host) for g in range(2))
+    assert torch.isfinite(got).all() and float(got.abs().max()) <= most * (1 + 2.0 ** -7)
