@@ -352,11 +352,12 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
       }
     };
     const int round = kRound * side;               // heads of a round
-    // the largest magnitude of a row, in all of its lanes
+    // the largest magnitude of a row, in all of its lanes; undefined elements count for nothing (the maximum passes over quiet ones
+    // only: of a signalling one and what came before it, it forgets the latter, so they are quieted)
     auto largest = [&](const float (&x)[8]) {
       float m = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = fmaxf(m, __builtin_fabsf(x[i]));
+      for (int i = 0; i < 8; ++i) m = fmaxf(m, __builtin_canonicalizef(__builtin_fabsf(x[i])));
       int t = __float_as_int(m);                  // (as integers they order the same)
       t = max(t, __builtin_amdgcn_mov_dpp(t, 0xb1, 0xf, 0xf, true));      // the neighbour,
       t = max(t, __builtin_amdgcn_mov_dpp(t, 0x4e, 0xf, 0xf, true));      // ... the other two of four,
