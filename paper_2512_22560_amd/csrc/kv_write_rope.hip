@@ -175,7 +175,11 @@ __device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, 
 // token belongs to is the last one that starts at or before it: for the first by looking at 64 starts at a time, from there on by
 // steps that double, then halve.
 __device__ __forceinline__ int place_of(const RopeWriteArgs& a, int first, int token) {
-  if (a.one_each) return a.ctx_lens[token] - 1;
+  if (a.one_each) {
+    // (only where the lengths on the device still say so: a captured launch may be replayed with trajectories that have ended)
+    const int place = a.ctx_lens[token] - 1;
+    if (((const __attribute__((address_space(4))) int32_t*)a.q_offsets)[a.batch] == a.total_q) return place;
+  }
   const int lane = threadIdx.x & 63;
   int lo = 0, n = a.batch;                            // among trajectories [lo, lo + n), starts in order
   while (n > 1) {
@@ -485,7 +489,7 @@ hipError_t launch_as(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid,
 
 hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s) {
   RopeWriteArgs a = args;
-  a.one_each = max_q_len == 1 && a.total_q == a.batch;   // (no trajectory has more, so each has one)
+  a.one_each = max_q_len == 1 && a.total_q == a.batch;   // (no trajectory has more, so each has one where so many rows are theirs)
   // a run of n tokens touches at most this many pages, wherever it starts
   const int64_t longest = std::min(max_q_len, a.total_q);
   a.pages = longest > 0 ? (int32_t)std::min<int64_t>((longest + kPageSize - 2) / kPageSize + 1, kMostPages) : 1;

@@ -1,0 +1,71 @@
+"""The rotating KV write where fewer rows are in use than the call was made for.  Bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_write_rope as R
+from paper_2512_22560_amd import binding as B
+from paper_2512_22560_amd import workloads as W
+from tests.test_gpu_kv_write_rope import DEV, batch_of, both, rows_of, same, table_of
+
+pytestmark = pytest.mark.gpu
+ints = lambda x: torch.from_numpy(np.asarray(x).astype(np.int32)).to(DEV)
+
+
+def shorter(b, new):
+    """The batch with other new tokens, at the ends of the contexts that it has."""
+    ctx = b.ctx_lens_host - b.q_lens_host + new
+    b.ctx_lens_host, b.q_lens_host, b.ctx_lens, b.q_lens = ctx, new, ints(ctx), ints(new)
+    b.q_offsets = ints(np.concatenate([[0], np.cumsum(new)]))
+    return b
+
+
+@pytest.mark.parametrize("heads,d", [((8, 4), 128), ((4, 1), 64)])
+@pytest.mark.parametrize("kv", ["int8_head", "bf16"])
+def test_single_tokens_of_trajectories_that_have_ended(kv, heads, d):
+    """As many rows as trajectories, as when all generate, but some have no new token and the last rows belong to nobody."""
+    b = batch_of("t", heads, d, "bf16", kv, ("uniform", 0, 60), ("const", 1), 51, batch=70)
+    new = (np.arange(70) % 7 != 2).astype(np.int64)
+    new[:1] = new[-3:] = 0
+    b = shorter(b, new)
+    used = int(new.sum())
+    gen = torch.Generator().manual_seed(52)
+    q, k, v = (rows_of(gen, 70, h, d, "bf16") for h in (heads[0], heads[1], heads[1]))
+    table = table_of(64, d)
+    pools = [None if t is None else t.clone() for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale)]
+    before = [W.raw_numpy(t) for t in pools]
+    got = B.kv_write_rope(q, k, v, b.q_lens, b.q_offsets, pools[0], pools[1], b.page_table, b.ctx_lens, cos_sin=table, max_q_len=1, k_scale=pools[2], v_scale=pools[3])
+    want = R.kv_write_rope(*(W.raw_numpy(x[:used]) for x in (q, k, v)), new, b.ctx_lens_host, W.raw_numpy(b.page_table), *before[:2], src_dtype="bf16", kv_dtype=kv,
+                           cos_sin=W.raw_numpy(table), k_scale=before[2], v_scale=before[3])
+    same((got[:used], *pools), want)
+
+
+def test_a_captured_write_is_replayed_with_trajectories_that_have_ended():
+    b = batch_of("t", (8, 4), 128, "bf16", "int8_head", ("uniform", 0, 60), ("const", 1), 53, batch=20)
+    gen = torch.Generator().manual_seed(54)
+    q, k, v = (rows_of(gen, 20, h, 128, "bf16") for h in (8, 4, 4))
+    table, out = table_of(80, 128), torch.empty((20, 8, 128), dtype=torch.bfloat16, device=DEV)
+    pools = [t.clone() for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale)]
+    call = lambda p, o: B.kv_write_rope(q, k, v, b.q_lens, b.q_offsets, p[0], p[1], b.page_table, b.ctx_lens, cos_sin=table, max_q_len=1, k_scale=p[2], v_scale=p[3], q_out=o)
+    call([t.clone() for t in pools], torch.empty_like(out))
+    torch.cuda.synchronize()
+    lens, offsets, ctx = b.q_lens, b.q_offsets, b.ctx_lens
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(pools, out)
+    for ended in ([], [3], [0, 3, 4], [0, 3, 4, 19], list(range(19))):
+        new = np.ones(20, dtype=np.int64)
+        new[ended] = 0
+        b.q_lens_host = np.ones(20, dtype=np.int64)
+        b.ctx_lens_host = W.raw_numpy(ctx).astype(np.int64)
+        now = b.ctx_lens_host - (new == 0)
+        for t, x in ((lens, new), (offsets, np.concatenate([[0], np.cumsum(new)]))):
+            t.copy_(ints(x))
+        before, used = [W.raw_numpy(t) for t in pools], int(new.sum())
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        # (a trajectory without a new token keeps its length: nothing of it is looked at)
+        want = R.kv_write_rope(*(W.raw_numpy(x[:used]) for x in (q, k, v)), new, np.where(new > 0, b.ctx_lens_host, now), W.raw_numpy(b.page_table), *before[:2],
+                               src_dtype="bf16", kv_dtype="int8_head", cos_sin=W.raw_numpy(table), k_scale=before[2], v_scale=before[3])
+        same((out[:used], *pools), want, f"{ended}")
