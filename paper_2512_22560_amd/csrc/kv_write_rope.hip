@@ -6,13 +6,14 @@
 // absmax / 448 or / 127 of the head's new rows in the page, never below kLeastHeadScale and, where the page already holds tokens,
 // never below the old one; if it grew, the codes already there are quantised again.
 //
-// Two kinds of workgroups share a launch.  Keys and values: one workgroup per (page that receives new tokens, pool); the page
+// Two kinds of workgroups share a launch.  Keys and values: a workgroup per (page that receives new tokens, pool); the page
 // belongs to one trajectory alone, so nothing here needs a global atomic.  Queries: one wave per token and some of its heads, which
 // lie side by side, so that a wave reads and writes kilobytes in a row, and what the token's position takes is looked up once.
 // A row of D elements is the work of D / 8 lanes, eight elements to a lane: two runs of four whose elements are each other's
 // partners, so that a rotation needs no exchange between lanes.  In a page's workgroup the groups of lanes are dealt to the new
 // slots first and the rest of them to heads, so that a lane keeps its slot over all heads it walks.
 #include <algorithm>
+#include <type_traits>
 
 #include "codes_device.h"
 
@@ -30,7 +31,7 @@ constexpr int kQueryWaves = 2048; // queries: waves wanted where there are few t
 // them 139 -> 133 and 117 -> 112 us alone, 719 -> 719 and 376 -> 375 with attn_append behind; 41 MB of them 244 -> 246 with it.
 constexpr int64_t kStreamQueries = 128 << 20;
 constexpr int kSmallPage = 256;   // elements of a token's keys up to which pages are small
-constexpr int kMostPages = 4096;  // pages of a trajectory with a workgroup of their own
+constexpr int kUneven = 5;        // times the mean chunk's pages that the longest one may have before pages are dealt out by a search
 
 template <int SRC_BYTES>
 struct Raw {                      // a lane's eight elements as they come
@@ -171,6 +172,21 @@ __device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, 
   }
 }
 
+// The last of `count` things that starts at or before `place`, starts in order and the first at 0: 64 at a time.  The same in all lanes.
+template <class Start>
+__device__ __forceinline__ int last_from(int count, int place, Start&& start) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = count;                              // among [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const bool before = at < n && start(lo + at) <= place;
+    const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1, 0);
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
 // The place in its context of new token `token`; `first` is the smallest token of the wave and the same in all lanes.  The trajectory a
 // token belongs to is the last one that starts at or before it: for the first by looking at 64 starts at a time, from there on by
 // steps that double, then halve.
@@ -180,15 +196,7 @@ __device__ __forceinline__ int place_of(const RopeWriteArgs& a, int first, int t
     const int place = a.ctx_lens[token] - 1;
     if (((const __attribute__((address_space(4))) int32_t*)a.q_offsets)[a.batch] == a.total_q) return place;
   }
-  const int lane = threadIdx.x & 63;
-  int lo = 0, n = a.batch;                            // among trajectories [lo, lo + n), starts in order
-  while (n > 1) {
-    const int step = (n + 63) / 64, at = lane * step;
-    const bool before = at < n && a.q_offsets[lo + at] <= first;
-    const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1, 0);
-    lo += k * step;
-    n = min(step, n - k * step);
-  }
+  int lo = last_from(a.batch, first, [&](int i) { return a.q_offsets[i]; });
   if (a.wave_tokens > 1) {
     int ahead = 1;
     for (; lo + ahead < a.batch && a.q_offsets[lo + ahead] <= token; ahead *= 2) lo += ahead;
@@ -246,8 +254,8 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 // 133 with fewer workgroups for its small pages (below).
 // 512 single tokens (64/4/128, int8; between events around the launch): 11.4 us with a search for each token's trajectory and a wave per
 // four query heads, 10.2 without the search, 8.8 with a wave per sixteen.
-// POOL: -1 the source type, else a KvKind; STREAM: rotated queries are written with the streaming hint
-template <int D, int SRC_BYTES, int POOL, bool STREAM>
+// POOL: -1 the source type, else a KvKind; STREAM: rotated queries are written with the streaming hint; DEAL: pages are dealt out by a search
+template <int D, int SRC_BYTES, int POOL, bool STREAM, bool DEAL>
 __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWriteArgs a) {
   constexpr bool kCodes = POOL >= 0, kHeadScales = kCodes && kv_has_head_scales(POOL);
   constexpr bool kInt8 = POOL == kKvInt8Head;
@@ -266,8 +274,17 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   // eight pages' keys, then their values
   const int pool = pages_before & 1;
   const unsigned int page_unit = (pages_before / 2) * kXcds + at;
-  const int b = __builtin_amdgcn_readfirstlane((int)(page_unit / (unsigned int)a.pages)), page_x = (int)page_unit - b * a.pages;
-  if (b >= a.batch) return;
+  int b, page_x;
+  if constexpr (!DEAL) {
+    b = __builtin_amdgcn_readfirstlane((int)(page_unit / (unsigned int)a.pages));
+    page_x = (int)page_unit - b * a.pages;
+    if (b >= a.batch) return;
+  } else {
+    // n tokens lie in at most n / 16 + 2 pages, so trajectory i's begin behind what all before it have at most
+    auto start = [&](int i) { return a.q_offsets[i] / kPageSize + 2 * i; };
+    b = last_from(a.batch, (int)page_unit, start);
+    page_x = (int)page_unit - __builtin_amdgcn_readfirstlane(start(b));
+  }
   // (the constant address space: nobody writes lengths or the table during the call, and scalar loads stay out of the rows' way)
   typedef const __attribute__((address_space(4))) int32_t* const_i32_p;
   int n = ((const_i32_p)a.q_lens)[b], len = ((const_i32_p)a.ctx_lens)[b], q_off = ((const_i32_p)a.q_offsets)[b];
@@ -281,7 +298,8 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   const Lane lane(a, col, rotate);
   const bool turns = lane.turns;
   const int e0 = lane.e0, e1 = lane.e1;
-  for (int page_i = first / kPageSize + page_x; page_i * kPageSize < len; page_i += a.pages) {
+  const int turn_pages = DEAL ? len / kPageSize + 1 : a.pages;   // (one page each where they were searched for)
+  for (int page_i = first / kPageSize + page_x; page_i * kPageSize < len; page_i += turn_pages) {
   const bool another = page_i != first / kPageSize + page_x;
   const int lo = max(first, page_i * kPageSize), hi = min(len, (page_i + 1) * kPageSize);
   const int s0 = lo - page_i * kPageSize, slots = hi - lo;
@@ -468,17 +486,17 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   }
 }
 
-template <int D, bool STREAM>
+template <int D, bool STREAM, bool DEAL>
 hipError_t launch_as(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid, hipStream_t s) {
   if (src_bytes == 4) {
     if (pool != -1) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((kv_write_rope_kernel<D, 4, -1, STREAM>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((kv_write_rope_kernel<D, 4, -1, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a);
   } else {
     switch (pool) {
-      case -1: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, -1, STREAM>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvFp8: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8, STREAM>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvFp8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8Head, STREAM>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvInt8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvInt8Head, STREAM>), grid, dim3(kThreads), 0, s, a); break;
+      case -1: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, -1, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvFp8: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvFp8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8Head, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvInt8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvInt8Head, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
       default: return hipErrorInvalidValue;
     }
   }
@@ -490,15 +508,20 @@ hipError_t launch_as(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid,
 hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s) {
   RopeWriteArgs a = args;
   a.one_each = max_q_len == 1 && a.total_q == a.batch;   // (no trajectory has more, so each has one where so many rows are theirs)
-  // a run of n tokens touches at most this many pages, wherever it starts
+  // A run of n tokens touches at most (n + 14) / 16 + 1 pages, wherever it starts: as many workgroups per trajectory as the longest chunk
+  // has pages, found by a division.  Small pages: a workgroup costs about as much to start as one's rows do, and most of those for the
+  // longest chunk's pages would have nothing to do, so there are as many as the mean chunk has pages, and they take turns.
+  // 512 chunks of 64 .. 1024 tokens (8/2/64, int8) 136 -> 123 us, 256 of them with 8/1/128 91.6 -> 89.6, with 8/4/64 78.2 -> 77.6; with 512
+  // elements of a token's keys 148 -> 144 or 134 -> 138 (128 chunks of 32 .. 512, 64/4/128), 137 -> 140 (16/8/64), with 1024 109 -> 118 (32/8/128).
+  // Where the longest chunk stands out neither will do (511 single tokens and one chunk of 30000, int8: 902 us with the few workgroups of
+  // 8/2/64, 819 with the many of 32/8/128; 63 and one of 2000: 21.6), and each workgroup takes the one page that is its own by a search over
+  // the chunks: 32, 128 and 13.1 us.  The search costs what two trips to memory do: 300 chunks of 1 .. 512 (bf16) 103.8 -> 105.8, 512 of 2 .. 64
+  // (8/2/64) 13.0 -> 14.1, so it is kept for these.
   const int64_t longest = std::min(max_q_len, a.total_q);
-  a.pages = longest > 0 ? (int32_t)std::min<int64_t>((longest + kPageSize - 2) / kPageSize + 1, kMostPages) : 1;
-  // Small pages: a workgroup costs about as much to start as one's rows do, and most of those for the longest chunk's pages would
-  // have nothing to do, so there are as many as the mean chunk has pages, and they take turns.  512 chunks of 64 .. 1024 tokens
-  // (8/2/64, int8) 143 -> 133 us, 256 of them with 8/1/128 101 -> 100, with 8/4/64 the same; with 512 elements of a token's keys
-  // 148 -> 144 or 134 -> 138 (128 chunks of 32 .. 512, 64/4/128), 137 -> 140 (16/8/64), with 1024 109 -> 118 (32/8/128).
-  if ((int64_t)a.hkv * head_dim <= kSmallPage) a.pages = (int32_t)std::min<int64_t>(a.pages, a.total_q / ((int64_t)kPageSize * a.batch) + 2);
-  const int64_t page_groups = ((int64_t)a.pages * a.batch + kXcds - 1) / kXcds * 2;
+  const int64_t pages = longest > 0 ? (longest + kPageSize - 2) / kPageSize + 1 : 1, mean = a.total_q / ((int64_t)kPageSize * a.batch) + 2;
+  const bool divided = pages <= kUneven * mean;
+  a.pages = !divided ? 0 : (int32_t)((int64_t)a.hkv * head_dim <= kSmallPage ? std::min(pages, mean) : pages);
+  const int64_t page_groups = ((divided ? (int64_t)a.pages * a.batch : a.total_q / kPageSize + 2 * (int64_t)a.batch) + kXcds - 1) / kXcds * 2;
   int64_t groups = page_groups;
   bool stream = false;
   if (a.q) {
@@ -513,11 +536,17 @@ hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, in
     stream = (int64_t)a.total_q * a.hq * head_dim * src_bytes > kStreamQueries;
     groups += ((((int64_t)a.total_q + a.wave_tokens - 1) / a.wave_tokens) * a.head_parts + kWaves * kXcds - 1) / (kWaves * kXcds);
   }
-  if (groups * kXcds > INT32_MAX || (int64_t)a.total_q * a.head_parts > INT32_MAX) return hipErrorInvalidValue;
+  // (a grid of 2^32 threads or more is cut short without an error)
+  if (groups * kXcds * kThreads > UINT32_MAX || (int64_t)a.total_q * a.head_parts > INT32_MAX) return hipErrorInvalidValue;
   a.page_share = (((uint64_t)page_groups << 32) + groups - 1) / groups;   // (rounded up: behind the last group there have been them all)
   const dim3 grid((unsigned)(groups * kXcds));
-  if (head_dim == 128) return stream ? launch_as<128, true>(a, src_bytes, pool, grid, s) : launch_as<128, false>(a, src_bytes, pool, grid, s);
-  if (head_dim == 64) return stream ? launch_as<64, true>(a, src_bytes, pool, grid, s) : launch_as<64, false>(a, src_bytes, pool, grid, s);
+  auto of_dim = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    if (divided) return stream ? launch_as<D, true, false>(a, src_bytes, pool, grid, s) : launch_as<D, false, false>(a, src_bytes, pool, grid, s);
+    return stream ? launch_as<D, true, true>(a, src_bytes, pool, grid, s) : launch_as<D, false, true>(a, src_bytes, pool, grid, s);
+  };
+  if (head_dim == 128) return of_dim(std::integral_constant<int, 128>{});
+  if (head_dim == 64) return of_dim(std::integral_constant<int, 64>{});
   return hipErrorInvalidValue;
 }
 

@@ -196,8 +196,8 @@ struct RopeWriteArgs {
   int32_t hq, hkv, max_pages, total_q;
   int32_t rot_dim, num_positions;
   int32_t batch;
-  // set at launch: pages of a trajectory with a workgroup of their own, the share of workgroups that take pages (in 2^-32), and into
-  // how many parts of how many heads a token's queries are cut
+  // set at launch: workgroups for the pages of each trajectory (0: for each page one, dealt out by a search), the share of workgroups
+  // that take pages (in 2^-32), and into how many parts of how many heads a token's queries are cut
   int32_t pages, head_parts, part_heads, wave_tokens, one_each;   // wave_tokens: tokens of a wave; one_each: token t is trajectory t's, if q_offsets say so
   uint64_t page_share;
   uint32_t pair_axes[4];           // two bits per pair

@@ -1,4 +1,4 @@
-"""The rotating KV write where fewer rows are in use than the call was made for.  Bit for bit."""
+"""The rotating KV write where chunks differ a lot, and where fewer rows are in use than the call was made for.  Bit for bit."""
 import numpy as np
 import pytest
 import torch
@@ -69,3 +69,70 @@ def test_a_captured_write_is_replayed_with_trajectories_that_have_ended():
         want = R.kv_write_rope(*(W.raw_numpy(x[:used]) for x in (q, k, v)), new, np.where(new > 0, b.ctx_lens_host, now), W.raw_numpy(b.page_table), *before[:2],
                                src_dtype="bf16", kv_dtype="int8_head", cos_sin=W.raw_numpy(table), k_scale=before[2], v_scale=before[3])
         same((out[:used], *pools), want, f"{ended}")
+
+
+def skewed(kv, heads, d, new, seed):
+    """A batch whose chunks are `new` behind short prefixes, pages in any order."""
+    new = np.asarray(new)
+    rng = np.random.default_rng(seed)
+    b = batch_of("t", heads, d, "f32" if kv == "f32" else "bf16", kv, ("const", 1), ("const", 0), seed, batch=len(new))
+    prefix = rng.integers(0, 40, len(new))
+    ctx = prefix + new
+    pages = -(-ctx // 16)
+    perm, at = rng.permutation(int(pages.sum())), 0
+    table = np.full((len(new), max(1, int(pages.max()))), -1, dtype=np.int32)
+    for i, n in enumerate(pages):
+        table[i, :n] = perm[at:at + n]
+        at += n
+    b.ctx_lens_host, b.q_lens_host, b.ctx_lens, b.q_lens = ctx, new, ints(ctx), ints(new)
+    b.q_offsets, b.page_table = ints(np.concatenate([[0], np.cumsum(new)])), ints(table)
+    grow = lambda t: None if t is None else torch.zeros((at, *t.shape[1:]), dtype=t.dtype, device=DEV) + (1 if t.dtype == torch.float32 else 0)
+    b.k_pages, b.v_pages, b.k_scale, b.v_scale = (grow(t) for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale))
+    return b
+
+
+def chunks(kind, rng):
+    if kind == "one long among single tokens":
+        new = np.ones(300, dtype=np.int64)
+        new[111] = 5000
+    elif kind == "the first":
+        new = rng.integers(0, 2, 65)
+        new[0] = 3000
+    elif kind == "the last":
+        new = rng.integers(0, 2, 4100)
+        new[-1] = 2000
+    elif kind == "alone":
+        new = np.zeros(500, dtype=np.int64)
+        new[250] = 4000
+    else:
+        new = np.exp(rng.uniform(0, np.log(700), 130)).astype(np.int64) * rng.integers(0, 2, 130)
+    return new
+
+
+@pytest.mark.parametrize("kind", ["one long among single tokens", "the first", "the last", "alone", "uneven"])
+@pytest.mark.parametrize("kv,heads,d", [("int8_head", (8, 2), 64), ("int8_head", (4, 4), 128), ("fp8_e4m3_head", (8, 2), 64), ("fp8_e4m3", (6, 2), 64), ("bf16", (8, 2), 64), ("f32", (2, 2), 64)])
+def test_chunks_that_differ_a_lot(kv, heads, d, kind):
+    new = chunks(kind, np.random.default_rng(55))
+    b = skewed(kv, heads, d, new, 56)
+    gen = torch.Generator().manual_seed(57)
+    src = b.workload.q_dtype
+    q, k, v = (rows_of(gen, int(new.sum()), h, d, src) for h in (heads[0], heads[1], heads[1]))
+    table = table_of(int(b.ctx_lens_host.max()), d)
+    got, want = both(b, q, k, v, table)
+    same(got, want)
+    got, want = both(b, None, k, v, table, max_q=100_000)                 # (more than the longest is allowed)
+    same(got, want)
+
+
+def test_more_page_places_than_a_launch_has():
+    """A batch of 4200 with one chunk of 33000 tokens: the longest chunk's pages for every trajectory would be 17 million workgroups."""
+    new = np.ones(4200, dtype=np.int64)
+    new[1234] = 33_000
+    b = skewed("int8_head", (8, 8), 64, new, 58)
+    gen = torch.Generator().manual_seed(59)
+    k, v = (rows_of(gen, int(new.sum()), 8, 64, "bf16") for _ in range(2))
+    got, want = both(b, None, k, v, table_of(4096, 64))
+    same(got, want)
+    kept = [t.clone() for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale)]
+    B.kv_write(k, v, b.q_lens, b.q_offsets, kept[0], kept[1], b.page_table, b.ctx_lens, max_q_len=33_000, k_scale=kept[2], v_scale=kept[3])
+    assert torch.equal(kept[1], got[2]) and torch.equal(kept[3], got[4])
