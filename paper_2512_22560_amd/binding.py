@@ -168,7 +168,8 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 def _kv_code(pages: torch.Tensor, k_scale, v_scale) -> int:
     """The pools' type: E4M3 codes have a scale for each page, or with scales [num_pages, Hkv] one for each page and KV head,
-    as int8 ones always do."""
+    as int8 ones always do.  [num_pages, 1] with one KV head is the latter: the same numbers, whose attention keeps more of its weights'
+    bits (kv_write alone takes them for the former)."""
     code = _dtype_code(pages)
     if code < FP8_E4M3 or k_scale is None or v_scale is None:
         return code
@@ -356,9 +357,12 @@ def attn_decode_shared(q, k_pages, v_pages, page_table, ctx_lens, *, group_size,
 def kv_write(k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, max_q_len,
              k_scale=None, v_scale=None, stream=None) -> None:
     """Puts the new tokens' K / V rows (packed by trajectory, [total_q, Hkv, D]) into the pools in place;
-    FP8 pools also get their page scales updated in place."""
+    8-bit pools also get their scales updated in place.  E4M3 pools of one KV head follow the rule of one scale for a page
+    whether their scales are [num_pages] or [num_pages, 1]."""
     _check_contig(k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, k_scale, v_scale)
     desc = make_desc(k_new, k_pages, page_table, sm_scale=1.0, k_scale=k_scale, v_scale=v_scale)
+    if desc.kv_dtype == FP8_E4M3_HEAD and desc.num_kv_heads == 1:
+        desc.kv_dtype = FP8_E4M3         # scales [num_pages, 1]: a page and its one head are the same, and the rule is the page's
     rc = lib().kv_write(ctypes.byref(desc), _ptr(k_new), _ptr(v_new), _ptr(q_lens), _ptr(q_offsets), int(k_new.shape[0]),
                         int(max_q_len), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(ctx_lens), _ptr(k_scale),
                         _ptr(v_scale), _stream(stream))
