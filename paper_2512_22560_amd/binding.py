@@ -173,15 +173,17 @@ def _kv_code(pages: torch.Tensor, k_scale, v_scale) -> int:
     code = _dtype_code(pages)
     if code < FP8_E4M3 or k_scale is None or v_scale is None:
         return code
-    if code == FP8_E4M3 and k_scale.dim() == 1:
-        return code
+    if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+        raise TypeError("scales are float32")
     pool = pages.shape
-    held = (pool[0], pool[1])
-    if k_scale.shape != held or v_scale.shape != held:
-        if code == FP8_E4M3 and k_scale.numel() == v_scale.numel() == pool[0]:
-            return code
+    held, n = (pool[0], pool[1]), pool[0]
+    if k_scale.shape == held and v_scale.shape == held:
+        return INT8_HEAD if code == INT8_HEAD else FP8_E4M3_HEAD
+    if code == INT8_HEAD:
         raise ValueError("scales of each page and KV head are [num_pages, Hkv]")
-    return INT8_HEAD if code == INT8_HEAD else FP8_E4M3_HEAD
+    if not (k_scale.dim() == v_scale.dim() == 1 and k_scale.numel() >= n and v_scale.numel() >= n) and not k_scale.numel() == v_scale.numel() == n:
+        raise ValueError("scales of both pools are [num_pages], or of each page and KV head [num_pages, Hkv]")
+    return code
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:

@@ -76,13 +76,15 @@ int dtype_code(const at::Tensor& t) {
 int kv_code(const at::Tensor& pages, const at::Tensor* k_scale, const at::Tensor* v_scale) {
   const int code = dtype_code(pages);
   if (code < ROLLATTN_FP8_E4M3 || !k_scale || !v_scale) return code;
-  if (code == ROLLATTN_FP8_E4M3 && k_scale->dim() == 1) return code;
-  const int64_t held[] = {pages.size(0), pages.size(1)};
-  if (k_scale->sizes() != at::IntArrayRef(held, 2) || v_scale->sizes() != at::IntArrayRef(held, 2)) {
-    if (code == ROLLATTN_FP8_E4M3 && k_scale->numel() == held[0] && v_scale->numel() == held[0]) return code;
-    throw Refusal{PyExc_ValueError, "scales of each page and KV head are [num_pages, Hkv]"};
-  }
-  return code == ROLLATTN_INT8_HEAD ? ROLLATTN_INT8_HEAD : ROLLATTN_FP8_E4M3_HEAD;
+  if (k_scale->scalar_type() != at::kFloat || v_scale->scalar_type() != at::kFloat) throw Refusal{PyExc_TypeError, "scales are float32"};
+  const int64_t held[] = {pages.size(0), pages.size(1)}, n = held[0];
+  if (k_scale->sizes() == at::IntArrayRef(held, 2) && v_scale->sizes() == at::IntArrayRef(held, 2))
+    return code == ROLLATTN_INT8_HEAD ? ROLLATTN_INT8_HEAD : ROLLATTN_FP8_E4M3_HEAD;
+  if (code == ROLLATTN_INT8_HEAD) throw Refusal{PyExc_ValueError, "scales of each page and KV head are [num_pages, Hkv]"};
+  const int64_t nk = k_scale->numel(), nv = v_scale->numel();
+  if (!(k_scale->dim() == 1 && v_scale->dim() == 1 && nk >= n && nv >= n) && !(nk == n && nv == n))
+    throw Refusal{PyExc_ValueError, "scales of both pools are [num_pages], or of each page and KV head [num_pages, Hkv]"};
+  return code;
 }
 
 void dims(const at::Tensor& t, int n, const char* what) {
