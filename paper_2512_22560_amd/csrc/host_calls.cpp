@@ -91,6 +91,12 @@ void dims(const at::Tensor& t, int n, const char* what) {
   if (t.dim() != n) throw Refusal{PyExc_ValueError, what};
 }
 
+// int32 arrays of at least so many entries
+void ints(const at::Tensor& t, int64_t least, const char* what) {
+  if (t.scalar_type() != at::kInt) throw Refusal{PyExc_TypeError, what};
+  if (t.numel() < least) throw Refusal{PyExc_ValueError, what};
+}
+
 // Elements between the rows of consecutive tokens; a token's heads lie side by side.
 int64_t row_stride(const at::Tensor& t) {
   const int64_t heads = t.size(1), d = t.size(2);
@@ -104,10 +110,17 @@ int64_t row_stride(const at::Tensor& t) {
   return heads * d;
 }
 
+// the chunks of B trajectories
+void chunks(const at::Tensor& q_lens, const at::Tensor& q_offsets, const at::Tensor& table) {
+  ints(q_lens, table.size(0), "q_lens is [B] int32");
+  ints(q_offsets, table.size(0) + 1, "q_offsets is [B + 1] int32");
+}
+
 rollattn_desc descriptor(const at::Tensor& rows, int64_t hq, const at::Tensor& k_pages, const at::Tensor& table, float sm_scale, const at::Tensor* k_scale,
                          const at::Tensor* v_scale) {
   dims(k_pages, 4, "pools are [num_pages, Hkv, page_size, D]");
-  dims(table, 2, "page_table is [B, max_pages]");
+  dims(table, 2, "page_table is [B, max_pages] int32");
+  ints(table, 0, "page_table is [B, max_pages] int32");
   rollattn_desc d{};
   d.batch = whole(table.size(0));
   d.num_q_heads = whole(hq);
@@ -195,6 +208,8 @@ PyObject* host_kv_write_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     rope.k_stride = row_stride(k_new);
     rope.v_stride = row_stride(v_new);
     const rollattn_desc desc = descriptor(k_new, hq, k_pages, page_table, 1.f, k_scale, v_scale);
+    ints(ctx_lens, page_table.size(0), "ctx_lens is [B] int32");
+    chunks(q_lens, q_offsets, page_table);
     const int32_t total = whole(total_q), longest = whole(number(args[10]));
     void* const stream = (void*)(uintptr_t)number(args[17]);
     void *const p_q = address(q), *const p_k = address(k_new), *const p_v = address(v_new), *const p_out = address(q_out), *const p_kp = address(k_pages), *const p_vp = address(v_pages);
@@ -210,11 +225,16 @@ PyObject* host_kv_write_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 }
 
 // The descriptor of an attention call.
-rollattn_desc attention(const at::Tensor& q, const at::Tensor& k_pages, const at::Tensor& table, PyObject* scale, const at::Tensor* k_scale, const at::Tensor* v_scale) {
+rollattn_desc attention(const at::Tensor& q, const at::Tensor& out, const at::Tensor& k_pages, const at::Tensor& v_pages, const at::Tensor& table, const at::Tensor& ctx_lens,
+                        PyObject* scale, const at::Tensor* k_scale, const at::Tensor* v_scale) {
   if (q.dim() < 2) throw Refusal{PyExc_ValueError, "query rows are [rows, Hq, D]"};
+  if (v_pages.sizes() != k_pages.sizes() || dtype_code(v_pages) != dtype_code(k_pages)) throw Refusal{PyExc_ValueError, "both pools are of one size and type"};
+  if (out.numel() < q.numel() || out.scalar_type() != q.scalar_type()) throw Refusal{PyExc_ValueError, "out takes a row for each of q's, of its type"};
   const double sm_scale = PyFloat_AsDouble(scale);
   if (sm_scale == -1. && PyErr_Occurred()) throw Raised{};
   rollattn_desc desc = descriptor(q, q.size(1), k_pages, table, (float)sm_scale, k_scale, v_scale);
+  if (q.numel() != q.size(0) * q.size(1) * k_pages.size(3)) throw Refusal{PyExc_ValueError, "query rows are [rows, Hq, D]"};
+  ints(ctx_lens, table.size(0), "ctx_lens is [B] int32");
   desc.k_scale = (const float*)address(k_scale);
   desc.v_scale = (const float*)address(v_scale);
   return desc;
@@ -226,11 +246,12 @@ PyObject* host_attn_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const at::Tensor &q = dense(tensor(args[0])), &k_pages = dense(tensor(args[1])), &v_pages = dense(tensor(args[2])), &page_table = dense(tensor(args[3]));
     const at::Tensor &ctx_lens = dense(tensor(args[4])), *k_scale = dense(maybe(args[6])), *v_scale = dense(maybe(args[7])), &out = dense(tensor(args[8]));
     const at::Tensor& workspace = tensor(args[9]);
-    const rollattn_desc desc = attention(q, k_pages, page_table, args[5], k_scale, v_scale);
+    const rollattn_desc desc = attention(q, out, k_pages, v_pages, page_table, ctx_lens, args[5], k_scale, v_scale);
+    if (q.size(0) < page_table.size(0)) throw Refusal{PyExc_ValueError, "a decode step has a query row for each trajectory"};
     void* const stream = (void*)(uintptr_t)number(args[10]);
     void *const p_q = address(q), *const p_kp = address(k_pages), *const p_vp = address(v_pages), *const p_out = address(out), *const p_ws = address(workspace);
     const int32_t *const p_table = (int32_t*)address(page_table), *const p_ctx = (int32_t*)address(ctx_lens);
-    const size_t room = (size_t)workspace.numel();
+    const size_t room = (size_t)workspace.nbytes();
     int rc;
     {
       const Unlocked other_threads_run;
@@ -246,12 +267,13 @@ PyObject* host_attn_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const at::Tensor &q = dense(tensor(args[0])), &q_lens = dense(tensor(args[1])), &q_offsets = dense(tensor(args[2])), &k_pages = dense(tensor(args[3]));
     const at::Tensor &v_pages = dense(tensor(args[4])), &page_table = dense(tensor(args[5])), &ctx_lens = dense(tensor(args[6]));
     const at::Tensor *k_scale = dense(maybe(args[9])), *v_scale = dense(maybe(args[10])), &out = dense(tensor(args[11])), &workspace = tensor(args[12]);
-    const rollattn_desc desc = attention(q, k_pages, page_table, args[7], k_scale, v_scale);
+    const rollattn_desc desc = attention(q, out, k_pages, v_pages, page_table, ctx_lens, args[7], k_scale, v_scale);
+    chunks(q_lens, q_offsets, page_table);
     const int32_t total = whole(q.size(0)), longest = whole(number(args[8]));
     void* const stream = (void*)(uintptr_t)number(args[13]);
     void *const p_q = address(q), *const p_kp = address(k_pages), *const p_vp = address(v_pages), *const p_out = address(out), *const p_ws = address(workspace);
     const int32_t *const p_lens = (int32_t*)address(q_lens), *const p_off = (int32_t*)address(q_offsets), *const p_table = (int32_t*)address(page_table), *const p_ctx = (int32_t*)address(ctx_lens);
-    const size_t room = (size_t)workspace.numel();
+    const size_t room = (size_t)workspace.nbytes();
     int rc;
     {
       const Unlocked other_threads_run;

@@ -57,3 +57,43 @@ def test_scales_that_are_taken():
         assert kind(dtype, 2, one(5, 2), one(5, 2)) == kind(dtype, 1, one(5, 1), one(5, 1)) == B.FP8_E4M3_HEAD
         assert kind(dtype, 2, None, None) == B.FP8_E4M3
     assert kind(torch.int8, 2, one(5, 2), one(5, 2)) == kind(torch.int8, 1, one(5, 1), one(5, 1)) == B.INT8_HEAD
+
+
+@pytest.mark.parametrize("dtype", CODES)
+def test_lengths_tables_and_rows_are_looked_at(dtype):
+    long = lambda *s: torch.zeros(s, dtype=torch.int64)
+    for name, least, n in (("ctx_lens", 3, 3), ("q_lens", 3, 2), ("q_offsets", 4, 2)):
+        for bad in (long(least), ints(least - 1), torch.zeros(least), torch.zeros(least, dtype=torch.int16)):
+            assert refused(dtype, **{name: bad}) == n
+    for bad in (long(3, 4), torch.zeros(3, 4), ints(12)):
+        assert refused(dtype, page_table=bad) == 3
+    assert refused(dtype, page_table=ints(4, 4)) == 3                                          # more trajectories than lengths, offsets and rows
+    other = torch.bfloat16
+    for bad in (pool(dtype, 4), pool(dtype)[:4], pool(dtype, 4).view(5, 2, 32, 64), torch.zeros(5, 2, 16, 64, dtype=other)):
+        assert refused(dtype, v_pages=bad) == 3
+    for name, shape in (("attn_decode", (3, 4, 64)), ("attn_append", (6, 4, 64))):
+        rows = "q" if name == "attn_decode" else "q_chunk"
+        for bad in ({"out": torch.zeros(shape)}, {"out": torch.zeros(shape, dtype=bf)[:-1]}, {"out": torch.zeros(shape, dtype=torch.int16)},
+                    {rows: torch.zeros(shape[0], 4, 32, dtype=bf), "out": torch.zeros(shape[0], 4, 32, dtype=bf)}):
+            (_, args), = ((n, a) for n, a in calls(dtype) if n == name)
+            with pytest.raises((ValueError, TypeError)):
+                getattr(B, name)(**dict(args, **bad))
+    for _, args in calls(dtype, q=torch.zeros(2, 4, 64, dtype=bf), out=torch.zeros(2, 4, 64, dtype=bf)):
+        with pytest.raises(ValueError):
+            B.attn_decode(**args)
+
+
+@pytest.mark.parametrize("dtype", CODES)
+def test_buffers_that_are_larger_are_taken(dtype):
+    """Lengths and offsets of a longer batch, more rows of output, a workspace of any type: what the library says of that is all that is wrong."""
+    for name, args in calls(dtype, ctx_lens=ints(9)):
+        if "out" in args:
+            args.update(out=torch.zeros(9, 4, 64, dtype=bf))
+        if "q_lens" in args:
+            args.update(q_lens=ints(8), q_offsets=ints(9))
+        if name == "kv_write_rope":
+            continue
+        for room, status in ((torch.zeros(16, dtype=torch.uint8), -5), (torch.zeros(4), -5)):
+            with pytest.raises(B.RollattnError) as e:
+                getattr(B, name)(**dict(args, workspace=room))
+            assert e.value.status == status
