@@ -41,7 +41,9 @@
  * Supported element types: q/out F32 with kv F32 (D = 64 or 128); q/out BF16 with kv
  * BF16, FP8_E4M3 or FP8_E4M3_HEAD (OCP E4M3, no infinities, max 448) or INT8_HEAD (two's
  * complement; D = 64 or 128).  Page scales must be positive and finite, as absmax / 448 is; those of the
- * _HEAD types between 2^-64, the least that is written here, and 2^100.
+ * _HEAD types between 2^-64, the least that is written here, and 2^100, and V scales of one KV head in one
+ * trajectory at most 2^100 apart (softmax weights are taken times the page's V scale in float32: further apart
+ * the tokens of the faint pages would drop out of the denominator).
  * Accumulation is float.  Hq / Hkv may be any positive integer (at most 256 for BF16 attn_append).
  *
  * Execution.  Calls enqueue kernels on `hip_stream` (a hipStream_t passed as void*,

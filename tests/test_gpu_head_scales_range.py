@@ -77,3 +77,19 @@ def test_scores_past_what_float32_resolves(kv, which, qlen, power):
     a = oracle_args(b)
     most = max(np.abs(O.gather_tokens(a["v_pages"], a["page_table"], i, g, int(n), kv, a["v_scale"])).max() for i, n in enumerate(b.ctx_lens_host) for g in range(2))
     assert torch.isfinite(got).all() and float(got.abs().max()) <= most * (1 + 2.0 ** -7)
+
+
+@pytest.mark.parametrize("ends", [("v", 36), ("v", 20), ("k", 100)])
+@pytest.mark.parametrize("which,qlen", SHAPES)
+@pytest.mark.parametrize("kv", KV)
+def test_scales_at_both_ends_of_their_range(kv, which, qlen, ends):
+    """Every other page has the least scale that a write leaves, as a page of zeros does.  Its values are next to nothing beside the other
+    pages', but its tokens take their part of the weights; its keys leave the scores at nothing."""
+    b = batch(kv, which, qlen, seed=45)
+    least = (torch.arange(b.k_scale.shape[0], device=DEV) % 2 == 0)[:, None]
+    name, top = ends
+    scale = getattr(b, name + "_scale")
+    scale.copy_(torch.where(least, torch.full_like(scale, 2.0 ** -64), torch.full_like(scale, 2.0 ** top)))
+    if name == "k":
+        b.q = (b.q.float() * 2.0 ** -110).to(torch.bfloat16)
+    check(call(b, which), b, which)
