@@ -45,6 +45,8 @@
  * trajectory at most 2^100 apart (softmax weights are taken times the page's V scale in float32: further apart
  * the tokens of the faint pages would drop out of the denominator).
  * Accumulation is float.  Hq / Hkv may be any positive integer (at most 256 for BF16 attn_append).
+ * Where attn_append, or the shared part of attn_decode_shared, meets FP8_E4M3_HEAD keys, a query element is the
+ * sum of two E4M3 numbers: off by at most 2^-17 of the largest of its row and head, exact from 2^-9 of that on.
  *
  * Execution.  Calls enqueue kernels on `hip_stream` (a hipStream_t passed as void*,
  * NULL = the default stream) and return without synchronising; nothing is copied to
@@ -264,8 +266,9 @@ typedef struct {
  *   keys and values alone.  q_out may be q where q is dense.  k_new, v_new, lengths, pools and scales as in kv_write; keys
  *   go into the pools from the float32 results of the rotation, rounded once (pools of the source type) or quantised by the
  *   rule of kv_write.
- * max_q_len sizes the launch as in kv_write: it must not understate the longest chunk.  No workspace; total_q == 0
- * succeeds without a launch. */
+ * max_q_len sizes the launch as in kv_write: it must not understate the longest chunk.  total_q may be more than
+ * q_offsets[B], as where a captured call is replayed after trajectories have ended: the rows behind belong to nobody, and
+ * what is written to their q_out means nothing.  No workspace; total_q == 0 succeeds without a launch. */
 int kv_write_rope(const rollattn_desc *desc, const rollattn_rope *rope, const void *q, const void *k_new, const void *v_new,
                   const int32_t *q_lens, const int32_t *q_offsets, int32_t total_q, int32_t max_q_len, void *q_out, void *k_pages,
                   void *v_pages, const int32_t *page_table, const int32_t *ctx_lens, float *k_scale, float *v_scale,

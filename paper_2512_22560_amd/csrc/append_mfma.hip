@@ -781,7 +781,8 @@ __device__ __forceinline__ void append_tile(const AppendArgs& kernel_args, Appen
       else return (psum[0] + psum[1]) + (psum[2] + psum[3]);
     };
     float lane_sum = exponentials(std::true_type{}, 0.f);
-    // (an infinite or undefined sum also fails the comparison and takes the slow path)
+    // (an infinite sum also fails the comparison and takes the slow path, and an undefined one does; HEAD: an undefined one need not, since the
+    // maximum passes over it: the row is undefined with either)
     if (__builtin_amdgcn_ballot_w64(!((HEAD ? weights : lane_sum) <= sum_limit))) {
       // largest exponent of the block: FP8 page scales and the softmax scale are positive here, so the maximum
       // can be taken on the raw products of each page
