@@ -136,3 +136,16 @@ def test_more_page_places_than_a_launch_has():
     kept = [t.clone() for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale)]
     B.kv_write(k, v, b.q_lens, b.q_offsets, kept[0], kept[1], b.page_table, b.ctx_lens, max_q_len=33_000, k_scale=kept[2], v_scale=kept[3])
     assert torch.equal(kept[1], got[2]) and torch.equal(kept[3], got[4])
+
+
+@pytest.mark.parametrize("heads,d", [((96, 2), 128), ((128, 4), 64)])
+def test_chunks_that_differ_a_lot_with_more_queries_than_the_caches_hold(heads, d):
+    """More than 128 MB of rotated queries are written with another kind of store."""
+    new = np.ones(200, dtype=np.int64)
+    new[77] = (130 << 20) // (heads[0] * d * 2)
+    b = skewed("int8_head", heads, d, new, 60)
+    gen = torch.Generator().manual_seed(61)
+    q, k, v = (rows_of(gen, int(new.sum()), h, d, "bf16") for h in (heads[0], heads[1], heads[1]))
+    assert q.numel() * 2 > 128 << 20
+    got, want = both(b, q, k, v, table_of(int(b.ctx_lens_host.max()), d))
+    same(got, want)
