@@ -9,7 +9,7 @@ are the operator's input, parents to the seed that `prepare` is given.  Head sha
 workloads that the repository states, and smaller ones of the same kind.
 
 Kinds of case:
-  draft    draft_tree: parents to visibility bits and positions
+  draft    attn_tree_mask: parents to visibility bits and positions
   write    kv_write_norm_rope: q and k of the new tokens, as one projection leaves them, are normalised by head and rotated, q is
            handed back, k and v go into the pages
   tree     attn_tree: a draft attends to its context
@@ -384,7 +384,7 @@ def _run_own(s):
         if "mask" not in s:                        # a program keeps its outputs and workspace from step to step
             s["mask"] = torch.empty((len(s["parents"]), s["words"]), dtype=torch.int64, device=s["parents"].device)
             s["positions"] = torch.empty_like(s["parents"])
-        B.draft_tree(s["parents"], *chunk, s["ctx"], max_q_len=s["max_q"], tree_mask=s["mask"], positions=s["positions"])
+        B.attn_tree_mask(s["parents"], *chunk, s["ctx"], max_q_len=s["max_q"], tree_mask=s["mask"], positions=s["positions"])
         return {"mask": s["mask"], "positions": s["positions"]}
     pools, where, scales = (s["k"], s["v"]), (s["table"], s["ctx"]), {"k_scale": s["k_scale"], "v_scale": s["v_scale"]}
     if s["kind"] == "write":
