@@ -274,6 +274,66 @@ int kv_write_rope(const rollattn_desc *desc, const rollattn_rope *rope, const vo
                   void *v_pages, const int32_t *page_table, const int32_t *ctx_lens, float *k_scale, float *v_scale,
                   void *hip_stream);
 
+/* Norms of queries and keys in front of the rotation: a head's row x of D elements becomes
+ *   (x * r) * weight      with r = 1 / sqrt(mean(x^2) + eps),
+ * each product, the sum, the root and the quotient one float32 operation.  Squares are float32, (x0^2 + x1^2) + (x2^2 + x3^2) of every
+ * four neighbours in float32 and the sum of these in double; the mean is rounded to float32 once.  (The double sum is exact, so that
+ * everything is defined bit for bit, unless sums of four neighbours lie 2^24 apart.) */
+typedef struct {
+  const float *q_weight, *k_weight;   /* device [head_dim], the same for all heads */
+  float eps;                          /* > 0, finite                               */
+} rollattn_norm;
+
+/* kv_write_rope for models that normalise every head of q and k before they turn it: arguments and rules as there, values as they
+ * are.  norm->q_weight is not looked at where q is NULL. */
+int kv_write_norm_rope(const rollattn_desc *desc, const rollattn_rope *rope, const rollattn_norm *norm, const void *q, const void *k_new,
+                       const void *v_new, const int32_t *q_lens, const int32_t *q_offsets, int32_t total_q, int32_t max_q_len, void *q_out,
+                       void *k_pages, void *v_pages, const int32_t *page_table, const int32_t *ctx_lens, float *k_scale, float *v_scale,
+                       void *hip_stream);
+
+/* Drafted tokens.  A step may score a whole tree of guessed tokens behind every trajectory's context at once: attn_tree_mask makes what
+ * the other calls need to know of the trees, kv_write_rope or kv_write_norm_rope puts the nodes' rows into the pages (one place
+ * each, rotated to the positions that attn_tree_mask gives), attn_tree attends, and kv_accept moves the rows of the path that was
+ * accepted to where the trajectory goes on.  Lengths and offsets as in attn_append: ctx_lens includes the n_b nodes of a draft, node i
+ * is at place L_b - n_b + i of the context.
+ *
+ * What a node sees of its draft is one bit for each of the draft's nodes: node j of the draft is bit j % 64 of word j / 64 of
+ * tree_mask [total_q][mask_words] (device), 1 <= mask_words <= ROLLATTN_MAX_MASK_WORDS.  Bits of nodes that do not exist are ignored;
+ * nodes past 64 * mask_words are seen by nobody. */
+#define ROLLATTN_MAX_MASK_WORDS 16
+
+/* The masks of trees: parents [total_q] int32 (device), a node's parent among the nodes of its own draft, of a lower number than its
+ * own; -1, and whatever else is no lower number, for a node right behind the context.  A node sees itself and its ancestors.
+ * positions [total_q] int32 (device; NULL: not wanted): L_b - n_b plus the number of ancestors, as kv_write_rope takes them.  Rows
+ * behind q_offsets[B] are left as they are.  max_q_len >= max n_b.  No workspace. */
+int attn_tree_mask(const int32_t *parents, const int32_t *q_lens, const int32_t *q_offsets, const int32_t *ctx_lens, int32_t batch,
+               int32_t total_q, int32_t max_q_len, uint64_t *tree_mask, int32_t mask_words, int32_t *positions, void *hip_stream);
+
+/* Attention of drafts: query row i of trajectory b sees tokens [0, L_b - n_b) and the nodes of its draft whose bits its mask has.  The
+ * mask need not be a tree's: rows may see later nodes, or nothing at all (a row that sees no token is zero, its lse -inf).  What a row
+ * does not see, undefined values included, does not reach it.  lse [total_q][Hq] float (device) as in attn_append_lse, or NULL.  Element
+ * types, pools and scales as in attn_append.  Queries over INT8_HEAD pools are scaled by a power of two per row and head as there.
+ * max_q_len must not understate the longest draft: rows past it would stay unwritten.  Rows behind q_offsets[B] are left as they are.
+ * Requires n_b <= L_b.  workspace of at least rollattn_tree_workspace_bytes(desc, total_q, max_q_len) bytes. */
+int attn_tree(const rollattn_desc *desc, const void *q, const int32_t *q_lens, const int32_t *q_offsets, int32_t total_q, int32_t max_q_len,
+              const uint64_t *tree_mask, int32_t mask_words, const void *k_pages, const void *v_pages, const int32_t *page_table,
+              const int32_t *ctx_lens, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t rollattn_tree_workspace_bytes(const rollattn_desc *desc, int32_t total_q, int32_t max_q_len);
+
+/* The accepted rows of drafts: accepted [total_q] int32 (device), packed like the drafts' rows, holds in its first m_b =
+ * accept_lens[b] <= n_b entries of trajectory b the numbers of the nodes that were accepted, strictly ascending.  The K and V rows of the
+ * i-th of them go from place L_b - n_b + accepted[i] to L_b - n_b + i; the caller's context is L_b - n_b + m_b long from there on.
+ * Pools of the source type: rows move bit for bit.  8-bit pools (k_scale, v_scale read and written as in kv_write): per page (and KV head
+ * for the _HEAD types) that rows go to, need = the largest |code * scale| of the rows that come from other pages / 448 (INT8: 127),
+ * scale' = max(scale, need), and every row of the page that is alive then, those in front of the draft included, becomes
+ * enc(code * scale of its page / scale'), which leaves codes alone where neither page nor scale is another.  Every product and quotient
+ * is one float32 operation: the result is defined bit for bit.  What is behind the accepted rows means nothing afterwards; pages in which
+ * no row moves are left as they are.  A page written here must belong to exactly one trajectory of the batch.  max_q_len >= max n_b only
+ * shapes the launch: one that understates costs speed, not correctness.  total_q == 0 succeeds without a launch.  No workspace. */
+int kv_accept(const rollattn_desc *desc, const int32_t *accepted, const int32_t *accept_lens, const int32_t *q_lens, const int32_t *q_offsets,
+              int32_t total_q, int32_t max_q_len, void *k_pages, void *v_pages, const int32_t *page_table, const int32_t *ctx_lens, float *k_scale,
+              float *v_scale, void *hip_stream);
+
 /* Bytes of workspace either call needs for this descriptor; total_q is the number of
  * query rows (B for decode).  Depends on the descriptor only, never on device data, and
  * not on max_pages_per_seq.  Nearly all of it holds partial results: for BF16 at D = 128

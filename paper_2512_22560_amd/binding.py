@@ -21,7 +21,7 @@ HOST_PATH = os.path.join(_HERE, "_host_calls.so")
 F32, BF16, FP8_E4M3, FP8_E4M3_HEAD, INT8_HEAD = 0, 1, 2, 3, 4
 EXPORTS = (
     "attn_decode", "attn_decode_static", "rollattn_static_scratch_bytes", "rollattn_static_init", "attn_append", "attn_decode_lse", "attn_append_lse", "attn_merge", "attn_step", "attn_decode_shared",
-    "kv_write", "kv_write_rope", "rollattn_workspace_bytes",
+    "kv_write", "kv_write_rope", "kv_write_norm_rope", "attn_tree_mask", "attn_tree", "kv_accept", "rollattn_tree_workspace_bytes", "rollattn_workspace_bytes",
     "rollattn_step_workspace_bytes", "rollattn_shared_workspace_bytes", "rollattn_debug_gather",
     "rollattn_debug_check_inputs",
     "rollattn_debug_plan", "rollattn_plan_capacity", "rollattn_plan_workers", "rollattn_debug_read_plan", "rollattn_debug_set_decode_workers", "rollattn_debug_read_append_plan", "rollattn_append_plan_capacity", "rollattn_step_append_offset",
@@ -45,6 +45,13 @@ class Rope(ctypes.Structure):
         ("num_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32),
         ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
     ]
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+MAX_MASK_WORDS = 16
 
 
 class RollattnError(RuntimeError):
@@ -98,6 +105,16 @@ def lib() -> ctypes.CDLL:
         l.kv_write.restype = ctypes.c_int
         l.kv_write_rope.argtypes = [dp, ctypes.POINTER(Rope), vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         l.kv_write_rope.restype = ctypes.c_int
+        l.kv_write_norm_rope.argtypes = [dp, ctypes.POINTER(Rope), ctypes.POINTER(Norm), vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        l.kv_write_norm_rope.restype = ctypes.c_int
+        l.attn_tree_mask.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp]
+        l.attn_tree_mask.restype = ctypes.c_int
+        l.attn_tree.argtypes = [dp, vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        l.attn_tree.restype = ctypes.c_int
+        l.rollattn_tree_workspace_bytes.argtypes = [dp, i32, i32]
+        l.rollattn_tree_workspace_bytes.restype = ctypes.c_size_t
+        l.kv_accept.argtypes = [dp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        l.kv_accept.restype = ctypes.c_int
         l.rollattn_workspace_bytes.argtypes = [dp, i32]
         l.rollattn_workspace_bytes.restype = ctypes.c_size_t
         l.rollattn_debug_gather.argtypes = [dp, vp, vp, vp, i32, i32, vp, vp]
@@ -140,7 +157,7 @@ _host = None
 
 
 def _load_host():
-    """The checks and the unpacking of attn_decode, attn_append and kv_write_rope as a module of its own (csrc/host_calls.cpp), which is
+    """The checks and the unpacking of the calls of every step as a module of its own (csrc/host_calls.cpp), which is
     told the library's addresses."""
     global _host
     l = lib()
@@ -148,7 +165,8 @@ def _load_host():
         from . import _host_calls
     except ImportError as e:
         raise RuntimeError("the _host_calls module is missing: build it with `python -m paper_2512_22560_amd.build`") from e
-    _host_calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (l.kv_write_rope, l.attn_decode, l.attn_append)))
+    _host_calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        l.kv_write_rope, l.attn_decode, l.attn_append, l.kv_write_norm_rope, l.attn_tree_mask, l.attn_tree, l.kv_accept)))
     _host = _host_calls
     return _host
 
@@ -194,6 +212,13 @@ def _stream(stream) -> int:
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _stream_of(t, stream) -> int:
+    """The current stream, which has to be one of the tensors' GPU, or the one that is given."""
+    if stream is None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"tensors are on cuda:{t.get_device()}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream(stream)
 
 
 def make_desc(q, k_pages, page_table, *, sm_scale, k_scale=None, v_scale=None, batch=None) -> Desc:
@@ -388,6 +413,70 @@ def kv_write_rope(q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_tab
     if rc:
         raise RollattnError(rc, "kv_write_rope")
     return q_out
+
+
+def kv_write_norm_rope(q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, q_weight, k_weight, eps, cos_sin, max_q_len,
+                       positions=None, pair_axes=None, interleaved=False, k_scale=None, v_scale=None, q_out=None, stream=None):
+    """kv_write_rope with a norm of every head of q and k in front of the rotation: x / sqrt(mean(x^2) + eps) * weight.
+
+    q_weight (None where q is None), k_weight: [D] float32, the same for all heads.  The other arguments as in kv_write_rope."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    rc = (_host or _load_host()).kv_write_norm_rope(
+        q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, cos_sin, max_q_len, positions,
+        None if pair_axes is None else bytes(pair_axes), interleaved, k_scale, v_scale, q_out, _stream_of(k_new, stream), q_weight, k_weight, eps)
+    if rc:
+        raise RollattnError(rc, "kv_write_norm_rope")
+    return q_out
+
+
+def attn_tree_mask(parents, q_lens, q_offsets, ctx_lens, *, max_q_len, tree_mask=None, positions=None, stream=None):
+    """What attn_tree and the writes need to know of drafts: (tree_mask [total_q, words] int64, positions [total_q] int32).
+
+    parents [total_q] int32: each node's parent among the nodes of its own draft, of a lower number; -1 right behind the context.
+    Bit j % 64 of word j / 64 of a node's mask says that it sees node j of its draft: itself and its ancestors.  positions: behind
+    the cached tokens and the ancestors.  ctx_lens includes the drafts."""
+    if tree_mask is None:
+        tree_mask = torch.empty((parents.shape[0], max(1, (int(max_q_len) + 63) // 64)), dtype=torch.int64, device=parents.device)
+    if positions is None:
+        positions = torch.empty_like(parents)
+    rc = (_host or _load_host()).attn_tree_mask(parents, q_lens, q_offsets, ctx_lens, max_q_len, tree_mask, positions, _stream_of(parents, stream))
+    if rc:
+        raise RollattnError(rc, "attn_tree_mask")
+    return tree_mask, positions
+
+
+def alloc_tree_workspace(q, k_pages, v_pages, page_table, ctx_lens, *, max_q_len, k_scale=None, v_scale=None) -> torch.Tensor:
+    desc = make_desc(q, k_pages, page_table, sm_scale=1.0, k_scale=k_scale, v_scale=v_scale)
+    n = int(lib().rollattn_tree_workspace_bytes(ctypes.byref(desc), int(q.shape[0]), int(max_q_len)))
+    if n == 0:
+        raise RollattnError(-2, "rollattn_tree_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def attn_tree(q, q_lens, q_offsets, tree_mask, k_pages, v_pages, page_table, ctx_lens, *, sm_scale, max_q_len,
+              k_scale=None, v_scale=None, out=None, lse=None, workspace=None, stream=None) -> torch.Tensor:
+    """Rows of q (the nodes of drafts, packed by trajectory) attend to their trajectory's cached tokens and to the nodes of their draft
+    whose bits tree_mask [total_q, words] int64 has (see attn_tree_mask).  ctx_lens includes the drafts, whose rows are in the pages.
+    lse [total_q, Hq] float32, where given, takes log2 of every row's softmax denominator."""
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if workspace is None:
+        workspace = alloc_tree_workspace(q, k_pages, v_pages, page_table, ctx_lens, max_q_len=max_q_len, k_scale=k_scale, v_scale=v_scale)
+    rc = (_host or _load_host()).attn_tree(q, q_lens, q_offsets, tree_mask, k_pages, v_pages, page_table, ctx_lens, sm_scale, max_q_len, k_scale, v_scale, out,
+                                           lse, workspace, _stream_of(q, stream))
+    if rc:
+        raise RollattnError(rc, "attn_tree")
+    return out
+
+
+def kv_accept(accepted, accept_lens, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, max_q_len, k_scale=None, v_scale=None, stream=None) -> None:
+    """Moves the K and V rows of the accepted nodes of every draft together, in place: node accepted[q_offsets[b] + i], i below
+    accept_lens[b], goes to place i of the draft.  accepted [total_q] int32 ascends within a trajectory.  ctx_lens includes the
+    drafts; afterwards a trajectory has ctx_lens - q_lens + accept_lens tokens.  8-bit pools get their scales updated in place."""
+    rc = (_host or _load_host()).kv_accept(accepted, accept_lens, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, max_q_len, k_scale, v_scale, _stream_of(accepted, stream))
+    if rc:
+        raise RollattnError(rc, "kv_accept")
 
 
 def debug_gather(pages, page_table, ctx_lens, b, kv_head, length, stream=None) -> torch.Tensor:

@@ -15,7 +15,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librollattn.so")
 PEAKS_LIB = os.path.join(HERE, "libbench_peaks.so")      # the benchmark's two peak microbenchmarks, not part of the library
 HOST_CALLS = os.path.join(HERE, "_host_calls.so")        # host_calls.cpp, a Python module: torch's headers, no GPU code
-SOURCES = ["append_mfma.hip", "append_mfma.hip:head", "decode_mfma.hip", "api.cpp", "plan.hip", "attn_f32.hip", "combine.hip", "kv_write.hip", "kv_write_rope.hip", "shared_prefix.hip"]
+SOURCES = ["append_mfma.hip", "append_mfma.hip:head", "decode_mfma.hip", "api.cpp", "plan.hip", "attn_f32.hip", "combine.hip", "kv_write.hip", "kv_write_rope.hip", "kv_write_rope.hip:norm", "shared_prefix.hip", "tree_mfma.hip", "draft.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wall", "-Wno-unused-function"]
@@ -25,7 +25,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
 # counter behind the compiler's back, so their build fails if the compiler reports any scratch.
 NO_SCRATCH = {"append_mfma.hip"}
 # A source that makes several objects: what the part of its name behind the colon sets.
-PARTS = {"head": ["-DROLLATTN_HEAD_SCALES"]}
+PARTS = {"head": ["-DROLLATTN_HEAD_SCALES"], "norm": ["-DROLLATTN_NORM"]}
 
 
 def _compile(src: str, extra) -> str:

@@ -828,10 +828,11 @@ int kv_write(const rollattn_desc* desc, const void* k_new, const void* v_new, co
   return ROLLATTN_OK;
 }
 
-int kv_write_rope(const rollattn_desc* desc, const rollattn_rope* rope, const void* q, const void* k_new, const void* v_new,
-                  const int32_t* q_lens, const int32_t* q_offsets, int32_t total_q, int32_t max_q_len, void* q_out, void* k_pages,
-                  void* v_pages, const int32_t* page_table, const int32_t* ctx_lens, float* k_scale, float* v_scale,
-                  void* hip_stream) {
+// norm: null where rows are only rotated.
+static int write_rope_impl(const rollattn_desc* desc, const rollattn_rope* rope, const rollattn_norm* norm, const void* q, const void* k_new, const void* v_new,
+                           const int32_t* q_lens, const int32_t* q_offsets, int32_t total_q, int32_t max_q_len, void* q_out, void* k_pages,
+                           void* v_pages, const int32_t* page_table, const int32_t* ctx_lens, float* k_scale, float* v_scale,
+                           void* hip_stream) {
   int rc = check_desc(desc, /*need_scales=*/false);
   if (rc) return rc;
   if (!rope || total_q < 0 || max_q_len < 0 || rope->num_positions < 1) return ROLLATTN_EINVAL;
@@ -856,11 +857,12 @@ int kv_write_rope(const rollattn_desc* desc, const rollattn_rope* rope, const vo
   const bool codes = has_codes(*desc);
   if (!k_new || !v_new || !q_lens || !q_offsets || !k_pages || !v_pages || !page_table || !ctx_lens || !rope->cos_sin) return ROLLATTN_EINVAL;
   if (!q != !q_out) return ROLLATTN_EINVAL;
+  if (norm && (!norm->k_weight || (q && !norm->q_weight))) return ROLLATTN_EINVAL;
   if (q && q == q_out && a.q_stride != q_row) return ROLLATTN_EINVAL;      // (in place: rows must lie where they are read)
   if (codes && (!k_scale || !v_scale)) return ROLLATTN_EDTYPE;
   if (!aligned16(q) || !aligned16(q_out) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_lens) || !aligned16(q_offsets) ||
       !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(page_table) || !aligned16(ctx_lens) || !aligned16(rope->cos_sin) ||
-      !aligned16(rope->positions) || (codes && (!aligned16(k_scale) || !aligned16(v_scale))))
+      !aligned16(rope->positions) || (norm && (!aligned16(norm->k_weight) || (q && !aligned16(norm->q_weight)))) || (codes && (!aligned16(k_scale) || !aligned16(v_scale))))
     return ROLLATTN_EALIGN;
   if (desc->batch > 65535) return ROLLATTN_ESHAPE;     // as kv_write, whose grid has a row per trajectory
   a.q = q; a.k_new = k_new; a.v_new = v_new; a.q_out = q_out; a.k_pages = k_pages; a.v_pages = v_pages;
@@ -871,10 +873,109 @@ int kv_write_rope(const rollattn_desc* desc, const rollattn_rope* rope, const vo
   a.rot_dim = rope->rot_dim; a.num_positions = rope->num_positions; a.interleaved = rope->interleaved != 0;
   hipStream_t s = (hipStream_t)hip_stream;
   ProfileScope prof(s);
-  const hipError_t e = launch_kv_write_rope(a, max_q_len, desc->head_dim, src_bytes, codes ? (int)kv_kind(*desc) : -1, s);
+  const int pool = codes ? (int)kv_kind(*desc) : -1;
+  hipError_t e;
+  if (norm) {
+    a.q_weight = norm->q_weight; a.k_weight = norm->k_weight; a.eps = norm->eps;
+    e = launch_kv_write_norm_rope(a, max_q_len, desc->head_dim, src_bytes, pool, s);
+  } else {
+    e = launch_kv_write_rope(a, max_q_len, desc->head_dim, src_bytes, pool, s);
+  }
   prof.stop();
   if (e != hipSuccess) return fail_hip(e);
   return ROLLATTN_OK;
+}
+
+int kv_write_rope(const rollattn_desc* desc, const rollattn_rope* rope, const void* q, const void* k_new, const void* v_new,
+                  const int32_t* q_lens, const int32_t* q_offsets, int32_t total_q, int32_t max_q_len, void* q_out, void* k_pages,
+                  void* v_pages, const int32_t* page_table, const int32_t* ctx_lens, float* k_scale, float* v_scale,
+                  void* hip_stream) {
+  return write_rope_impl(desc, rope, nullptr, q, k_new, v_new, q_lens, q_offsets, total_q, max_q_len, q_out, k_pages, v_pages, page_table, ctx_lens, k_scale,
+                         v_scale, hip_stream);
+}
+
+int kv_write_norm_rope(const rollattn_desc* desc, const rollattn_rope* rope, const rollattn_norm* norm, const void* q, const void* k_new,
+                       const void* v_new, const int32_t* q_lens, const int32_t* q_offsets, int32_t total_q, int32_t max_q_len, void* q_out,
+                       void* k_pages, void* v_pages, const int32_t* page_table, const int32_t* ctx_lens, float* k_scale, float* v_scale,
+                       void* hip_stream) {
+  if (!norm || !(norm->eps > 0.f) || std::isinf(norm->eps)) return ROLLATTN_EINVAL;
+  return write_rope_impl(desc, rope, norm, q, k_new, v_new, q_lens, q_offsets, total_q, max_q_len, q_out, k_pages, v_pages, page_table, ctx_lens, k_scale,
+                         v_scale, hip_stream);
+}
+
+int attn_tree_mask(const int32_t* parents, const int32_t* q_lens, const int32_t* q_offsets, const int32_t* ctx_lens, int32_t batch,
+               int32_t total_q, int32_t max_q_len, uint64_t* tree_mask, int32_t mask_words, int32_t* positions, void* hip_stream) {
+  if (batch < 0 || total_q < 0 || max_q_len < 0) return ROLLATTN_EINVAL;
+  if (mask_words < 1 || mask_words > ROLLATTN_MAX_MASK_WORDS) return ROLLATTN_ESHAPE;
+  if (batch == 0 || total_q == 0) return ROLLATTN_OK;
+  if (!parents || !q_lens || !q_offsets || !ctx_lens || !tree_mask) return ROLLATTN_EINVAL;
+  if (!aligned16(parents) || !aligned16(q_lens) || !aligned16(q_offsets) || !aligned16(ctx_lens) || !aligned16(tree_mask) || !aligned16(positions))
+    return ROLLATTN_EALIGN;
+  if (batch > 65535) return ROLLATTN_ESHAPE;
+  TreeMaskArgs a{};
+  a.parents = parents; a.q_lens = q_lens; a.q_offsets = q_offsets; a.ctx_lens = ctx_lens;
+  a.mask = tree_mask; a.positions = positions; a.batch = batch; a.mask_words = mask_words;
+  const hipError_t e = launch_tree_mask(a, max_q_len, (hipStream_t)hip_stream);
+  return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
+}
+
+size_t rollattn_tree_workspace_bytes(const rollattn_desc* desc, int32_t total_q, int32_t max_q_len) {
+  if (check_desc(desc) != ROLLATTN_OK || total_q < 0 || max_q_len < 0) return 0;
+  return 256;
+}
+
+int attn_tree(const rollattn_desc* desc, const void* q, const int32_t* q_lens, const int32_t* q_offsets, int32_t total_q, int32_t max_q_len,
+              const uint64_t* tree_mask, int32_t mask_words, const void* k_pages, const void* v_pages, const int32_t* page_table,
+              const int32_t* ctx_lens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_desc(desc);
+  if (rc) return rc;
+  if (total_q < 0 || max_q_len < 0) return ROLLATTN_EINVAL;
+  if (mask_words < 1 || mask_words > ROLLATTN_MAX_MASK_WORDS) return ROLLATTN_ESHAPE;
+  rc = append_limits(*desc);
+  if (rc) return rc;
+  if (desc->batch == 0 || total_q == 0) return ROLLATTN_OK;
+  if (max_q_len == 0) return ROLLATTN_EINVAL;      // (rows, and none of them anybody's)
+  if (!q || !q_lens || !q_offsets || !tree_mask || !k_pages || !v_pages || !page_table || !ctx_lens || !out || !workspace) return ROLLATTN_EINVAL;
+  if (!aligned16(q) || !aligned16(q_lens) || !aligned16(q_offsets) || !aligned16(tree_mask) || !aligned16(k_pages) || !aligned16(v_pages) ||
+      !aligned16(page_table) || !aligned16(ctx_lens) || !aligned16(out) || !aligned16(lse) || !aligned16(workspace))
+    return ROLLATTN_EALIGN;
+  if (workspace_bytes < rollattn_tree_workspace_bytes(desc, total_q, max_q_len)) return ROLLATTN_EWORKSPACE;
+  if (desc->batch > 65535) return ROLLATTN_ESHAPE;
+  TreeArgs a{};
+  a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.page_table = page_table; a.ctx_lens = ctx_lens;
+  a.q_lens = q_lens; a.q_offsets = q_offsets; a.mask = tree_mask; a.out = out; a.lse = lse;
+  a.k_scale = desc->k_scale; a.v_scale = desc->v_scale;
+  a.batch = desc->batch; a.hq = desc->num_q_heads; a.hkv = desc->num_kv_heads; a.group = a.hq / a.hkv;
+  a.max_pages = desc->max_pages_per_seq; a.mask_words = mask_words; a.total_q = total_q;
+  a.scale_log2 = desc->sm_scale * 1.4426950408889634f;
+  hipStream_t s = (hipStream_t)hip_stream;
+  ProfileScope prof(s);
+  const hipError_t e = desc->q_dtype == ROLLATTN_F32 ? launch_tree_f32(a, desc->head_dim, s)
+                                                     : launch_tree_mfma(a, desc->head_dim, kv_kind(*desc), std::min(max_q_len, total_q), s);
+  prof.stop();
+  return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
+}
+
+int kv_accept(const rollattn_desc* desc, const int32_t* accepted, const int32_t* accept_lens, const int32_t* q_lens, const int32_t* q_offsets,
+              int32_t total_q, int32_t max_q_len, void* k_pages, void* v_pages, const int32_t* page_table, const int32_t* ctx_lens, float* k_scale,
+              float* v_scale, void* hip_stream) {
+  int rc = check_desc(desc, /*need_scales=*/false);
+  if (rc) return rc;
+  if (total_q < 0 || max_q_len < 0) return ROLLATTN_EINVAL;
+  if (desc->batch == 0 || total_q == 0) return ROLLATTN_OK;
+  const bool codes = has_codes(*desc);
+  if (!accepted || !accept_lens || !q_lens || !q_offsets || !k_pages || !v_pages || !page_table || !ctx_lens) return ROLLATTN_EINVAL;
+  if (codes && (!k_scale || !v_scale)) return ROLLATTN_EDTYPE;
+  if (!aligned16(accepted) || !aligned16(accept_lens) || !aligned16(q_lens) || !aligned16(q_offsets) || !aligned16(k_pages) || !aligned16(v_pages) ||
+      !aligned16(page_table) || !aligned16(ctx_lens) || (codes && (!aligned16(k_scale) || !aligned16(v_scale))))
+    return ROLLATTN_EALIGN;
+  if (desc->batch > 65535) return ROLLATTN_ESHAPE;
+  AcceptArgs a{};
+  a.accepted = accepted; a.accept_lens = accept_lens; a.q_lens = q_lens; a.q_offsets = q_offsets; a.page_table = page_table; a.ctx_lens = ctx_lens;
+  a.k_pages = k_pages; a.v_pages = v_pages; a.k_scale = k_scale; a.v_scale = v_scale;
+  a.batch = desc->batch; a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq;
+  const hipError_t e = launch_kv_accept(a, max_q_len, desc->head_dim, desc->head_dim * dtype_bytes(desc->kv_dtype), codes ? (int)kv_kind(*desc) : -1, (hipStream_t)hip_stream);
+  return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
 }
 
 int rollattn_debug_gather(const rollattn_desc* desc, const void* pages, const int32_t* page_table,
@@ -1004,6 +1105,6 @@ const char* rollattn_last_hip_error(void) {
   return copy.c_str();
 }
 
-int rollattn_version(void) { return 102; }
+int rollattn_version(void) { return 103; }
 
 }  // extern "C"

@@ -6,6 +6,9 @@
 // the groups are merged with the log-sum-exp rule at the end, across the wave in registers, across waves through LDS.
 // Bound by latency (the calls are small): page id, then K and V, then the softmax chain.  Four tokens per lane group are
 // under way at a time and share one step of that chain.
+#include <algorithm>
+#include <type_traits>
+
 #include "plan_device.h"
 
 namespace rollattn {
@@ -55,12 +58,17 @@ __device__ __forceinline__ float across_groups(float x, bool add) {
 
 // Attention of up to HT query rows (same KV head) over tokens [0, len), len > 0, of a paged range whose
 // page ids start at table[0].  Leaves un-normalised o in o_out[h][D] (LDS), and max (log2
-// units) / sum in ml_out[h][2].  All THREADS threads must call it.
-template <int D, int THREADS, int HT>
+// units) / sum in ml_out[h][2].  All THREADS threads must call it.  sees(t): whether the rows see token t (All: every one;
+// else there may be none, the maximum is then -inf and everything else zero).
+struct All {
+  __device__ __forceinline__ bool operator()(int) const { return true; }
+};
+template <int D, int THREADS, int HT, class Sees = All>
 __device__ void attend_f32(const float* const* qrows, int n_heads, const float* k_pages, const float* v_pages,
                            const int32_t* table, int len, int hkv, int g, float scale_log2,
                            float (*o_part)[HT][D], float (*ml_part)[HT][2], float (*o_out)[D],
-                           float (*ml_out)[2]) {
+                           float (*ml_out)[2], Sees sees = Sees{}) {
+  constexpr bool kAll = std::is_same_v<Sees, All>;
   using G_ = F32Geo<D>;
   constexpr int kWaves = THREADS / 64, kGroups = kWaves * G_::kTokPerWave, kUnroll = 4;
   const int tid = threadIdx.x;
@@ -82,8 +90,11 @@ __device__ void attend_f32(const float* const* qrows, int n_heads, const float* 
   }
   for (int t0 = grp; t0 - grp < len; t0 += kUnroll * kGroups) {    // (the same trips for every lane)
     float4 kv[kUnroll], vv[kUnroll];
+    bool seen[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
+      seen[u] = t0 + u * kGroups < len;
+      if constexpr (!kAll) seen[u] = seen[u] && sees(t0 + u * kGroups);
       const int t = min(t0 + u * kGroups, len - 1);                // past the end: the last token again, weight zero
       const size_t off = (((size_t)table[t / kPageSize] * hkv + g) * kPageSize + (t % kPageSize)) * D + dl * 4;
       kv[u] = *(const float4*)(k_pages + off);
@@ -91,14 +102,15 @@ __device__ void attend_f32(const float* const* qrows, int n_heads, const float* 
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)                              // (zero times an infinity would not be zero)
-      if (t0 + u * kGroups >= len) vv[u] = make_float4(0, 0, 0, 0);
+      if (!seen[u]) vv[u] = make_float4(0, 0, 0, 0);
 #pragma unroll
     for (int h = 0; h < HT; ++h) {
       float s[kUnroll], m_new = m[h];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         s[u] = q[h].x * kv[u].x + q[h].y * kv[u].y + q[h].z * kv[u].z + q[h].w * kv[u].w;
-        s[u] = t0 + u * kGroups < len ? token_sum<D>(s[u]) * scale_log2 : -INFINITY;
+        s[u] = token_sum<D>(s[u]);
+        s[u] = seen[u] ? s[u] * scale_log2 : -INFINITY;
         m_new = fmaxf(m_new, s[u]);
       }
       const float base = m_new == -INFINITY ? 0.f : m_new;         // a lane group that has seen no token yet
@@ -141,10 +153,11 @@ __device__ void attend_f32(const float* const* qrows, int n_heads, const float* 
     float mmax = ml_part[0][h][0];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) mmax = fmaxf(mmax, ml_part[w][h][0]);   // finite: some wave has the first token
+    const float base = !kAll && mmax == -INFINITY ? 0.f : mmax;
     float o = 0.f, ls = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(ml_part[w][h][0] - mmax);       // 2^-inf = 0
+      const float f = __builtin_amdgcn_exp2f(ml_part[w][h][0] - base);       // 2^-inf = 0
       o += f * o_part[w][h][d];
       ls += f * ml_part[w][h][1];
     }
@@ -299,7 +312,57 @@ __global__ __launch_bounds__(kThreads) void append_f32_kernel(const AppendArgs a
   }
 }
 
+// Drafted tokens in float32: one workgroup per (query row, KV head, head tile), as in append; what a row sees of the draft its mask says.
+template <int D>
+__global__ __launch_bounds__(kThreads) void tree_f32_kernel(const TreeArgs a) {
+  __shared__ __attribute__((aligned(16))) float o_part[kThreads / 64][kHT][D];
+  __shared__ float ml_part[kThreads / 64][kHT][2];
+  __shared__ __attribute__((aligned(16))) float o_out[kHT][D];
+  __shared__ float ml_out[kHT][2];
+  const int n_ht = (a.group + kHT - 1) / kHT;
+  const int rows = min(a.total_q, a.q_offsets[a.batch]);          // (rows behind the last draft are nobody's)
+  const long n_work = (long)rows * a.hkv * n_ht;
+  for (long work = blockIdx.x; work < n_work; work += gridDim.x) {
+    const int row = (int)(work / (a.hkv * n_ht));
+    const int g = (int)((work - (long)row * a.hkv * n_ht) / n_ht);
+    const int h0 = (int)(work % n_ht) * kHT;
+    const int n_heads = min(kHT, a.group - h0);
+    // trajectory of this packed row: largest b with q_offsets[b] <= row
+    int lo = 0, hi = a.batch;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.q_offsets[mid] <= row) lo = mid; else hi = mid;
+    }
+    const int b = lo, len = a.ctx_lens[b], prefix = len - a.q_lens[b];
+    const float* qrows[kHT];
+#pragma unroll
+    for (int h = 0; h < kHT; ++h) qrows[h] = (const float*)a.q + ((size_t)row * a.hq + (size_t)g * a.group + h0 + min(h, n_heads - 1)) * D;
+    const uint64_t* const words = a.mask + (size_t)row * a.mask_words;
+    const int n_words = a.mask_words;
+    attend_f32<D, kThreads, kHT>(qrows, n_heads, (const float*)a.k_pages, (const float*)a.v_pages, a.page_table + (size_t)b * a.max_pages, len, a.hkv, g, a.scale_log2,
+                                 o_part, ml_part, o_out, ml_out,
+                                 [=](int t) { return t < prefix || ((t - prefix) >> 6 < n_words && words[(t - prefix) >> 6] >> ((t - prefix) & 63) & 1); });
+    for (int e = threadIdx.x; e < n_heads * D; e += kThreads) {
+      const int h = e / D, d = e % D;
+      const size_t orow = (size_t)row * a.hq + (size_t)g * a.group + h0 + h;
+      const float l = ml_out[h][1];
+      ((float*)a.out)[orow * D + d] = l == 0.f ? 0.f : o_out[h][d] / l;       // (nothing seen: a row of zeros)
+      if (a.lse && d == 0) a.lse[orow] = ml_out[h][0] + __builtin_amdgcn_logf(l);
+    }
+    __syncthreads();
+  }
+}
+
 }  // namespace
+
+hipError_t launch_tree_f32(const TreeArgs& a, int head_dim, hipStream_t s) {
+  const int tiles = (a.group + kHT - 1) / kHT;
+  const dim3 grid((unsigned)std::min<int64_t>((int64_t)a.total_q * a.hkv * tiles, 1 << 20));
+  if (head_dim == 64) hipLaunchKernelGGL((tree_f32_kernel<64>), grid, dim3(kThreads), 0, s, a);
+  else if (head_dim == 128) hipLaunchKernelGGL((tree_f32_kernel<128>), grid, dim3(kThreads), 0, s, a);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
 
 hipError_t launch_decode_f32(const DecodeArgs& a, int head_dim, int grid, hipStream_t s) {
   if (head_dim == 64) {

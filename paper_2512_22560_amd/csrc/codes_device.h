@@ -69,4 +69,45 @@ struct Quotients {
   }
 };
 
+// Four codes -> four floats, exactly.
+template <bool INT8>
+__device__ __forceinline__ void decode4(unsigned int w, float* x) {
+  if constexpr (INT8) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)(w >> (8 * e));
+  } else {
+    const floatx2 f0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), f1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = f0[0]; x[1] = f0[1]; x[2] = f1[0]; x[3] = f1[1];
+  }
+}
+
+// Sixteen codes: the largest magnitude (undefined ones count for nothing), and the codes of the same values under another scale,
+// enc(dec(code) * before / now).
+template <bool INT8>
+__device__ __forceinline__ float largest16(uintx4 w) {
+  float m = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float x[4];
+    decode4<INT8>(w[k], x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m = fmaxf(m, __builtin_fabsf(x[e]));
+  }
+  return m;
+}
+template <bool INT8>
+__device__ __forceinline__ uintx4 again16(uintx4 w, float before, float now) {
+  const Quotients<false> by(now);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float x[4];
+    decode4<INT8>(w[k], x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= before;
+    by.divide(x);
+    w[k] = INT8 ? encode4_int8(x) : encode4_e4m3(x);
+  }
+  return w;
+}
+
 }  // namespace rollattn

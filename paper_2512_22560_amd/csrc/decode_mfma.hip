@@ -26,137 +26,14 @@
 //   2^kWeightBits, and one of 2^-28 of it is still a normal number; the row sum takes p = weight / vs.
 // Bound by memory like the rest: 64 contexts of 512 .. 8191 tokens (32/8/128, int8, 367 MB) 73 us a call, 5.0 TB/s, 256 of 1024 .. 32767
 // (64/4/128, 2.3 GB) 388 us, 5.8 TB/s.  The query as two int8 numbers and integer products: 0.7 % less, but no longer exact; not kept.
-#include <type_traits>
-
-#include "plan_device.h"
+#include "stream_tiles.h"
 
 namespace rollattn {
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef int intx2 __attribute__((ext_vector_type(2)));
-typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
-
-typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
-typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
-
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-
-constexpr float kWeightBits = 14.f;   // f16 weights: log2 of the largest,
-constexpr float kMostBits = 15.f;     // ... and the most that rounding may make of it
-constexpr int kQueryBits = 15;        // f16 queries: the largest is below two to this
-
-template <int D, bool FP8>
-struct Geo {
-  static constexpr int kRowBytes = D * (FP8 ? 1 : 2);
-  static constexpr int kChunks = kRowBytes / 16;          // 16-byte chunks per token row
-  static constexpr int kRowsPerLoad = 64 / kChunks;        // token rows one wave-wide load covers
-  static constexpr int kLoads = kBlockTokens / kRowsPerLoad;  // loads per block, per pool
-  static constexpr int kTileBytes = kBlockTokens * kRowBytes; // LDS bytes per block, per pool
-  static constexpr int kStages = FP8 ? 4 : 2;              // blocks in flight per wave
-  static constexpr int kDT = D / 16;                       // 16-wide output tiles along D
-  static constexpr int kKK = D / 32;                       // 32-deep steps of the QK product
-  static_assert(kRowsPerLoad <= 16 && 16 % kRowsPerLoad == 0, "a load must stay inside one page");
-};
-
-// Swizzle keys: which 16-byte column a logical chunk of token row t lands in.  K rows are
-// read 16 rows at a time (rows {0-3, 8-11, 16-19, 24-27} + 4*tile), V rows 4 or 8 at a time.
-__device__ __forceinline__ int key_k(int t) { return (t & 3) | (((t >> 3) & 3) << 2); }
-__device__ __forceinline__ int key_v16(int t) { return ((t & 3) << 1) | (((t >> 3) & 1) << 3); }
-__device__ __forceinline__ int key_v8(int t) { return t & 7; }
-
-__device__ __forceinline__ float xor16_max(float x) {
-  uintx2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float xor32_max(float x) {
-  uintx2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float xor16_add(float x) {
-  uintx2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float xor32_add(float x) {
-  uintx2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Eight E4M3 codes to bf16, exactly: the scaled conversion with a scale of one, two codes per instruction.
-__device__ __forceinline__ bf16x8 fp8x8_to_bf16(uint32_t lo, uint32_t hi) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
-  bf16x8 r;
-  r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
-  r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
-  return r;
-}
-
-__device__ __forceinline__ halfx8 fp8x8_to_f16(uint32_t lo, uint32_t hi) {
-  const halfx2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
-  const halfx2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
-  const halfx2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
-  const halfx2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
-  return halfx8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// Eight 8-bit integers to f16, exactly: with the sign turned round a byte counts from -128 up, as the low bits of 1024.0 it adds
-// itself to that, and 1152 less is the value.  (Left out for keys and taken off the scores instead: 73.0 -> 72.6 us, not worth it.)
-__device__ __forceinline__ halfx8 int8x8_to_f16(uint32_t lo, uint32_t hi) {
-  lo ^= 0x80808080u;
-  hi ^= 0x80808080u;
-  const halfx2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
-  const halfx2 a = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) + off;
-  const halfx2 b = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) + off;
-  const halfx2 c = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) + off;
-  const halfx2 d = __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) + off;
-  return halfx8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// Eight codes as an operand of the first or second product, and the product with another.
-template <int KV>
-__device__ __forceinline__ auto widen_k8(uint32_t lo, uint32_t hi) {
-  if constexpr (KV == kKvInt8Head) return int8x8_to_f16(lo, hi);
-  else return fp8x8_to_bf16(lo, hi);
-}
-template <int KV>
-__device__ __forceinline__ auto widen_v8(uint32_t lo, uint32_t hi) {
-  if constexpr (KV == kKvFp8Head) return fp8x8_to_f16(lo, hi);
-  else if constexpr (KV == kKvInt8Head) return int8x8_to_f16(lo, hi);
-  else return fp8x8_to_bf16(lo, hi);
-}
-__device__ __forceinline__ floatx4 mfma(bf16x8 x, bf16x8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
-__device__ __forceinline__ floatx4 mfma(halfx8 x, halfx8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, z, 0, 0, 0); }
-
-// (worked out where it is used: the thread's index would take a register over the whole of a worker's rows)
-__device__ __forceinline__ int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }
-
-struct Cursor {
-  int b, r, blk;   // trajectory, row within it, block within the row
-  int n, len;      // blocks in the row, context length of the trajectory
-};
-
-// 16 bytes of a K or V row.  Where every byte of a run is read once per call, by one wave (see all_read_again), it is read
-// with the streaming hint.  Over FP8 pools that keeps page scales, 32 pages' to a cache line, from being displaced (384
-// contexts: 4.73 -> 4.54 GB read); over bf16 pools as many bytes come faster.  Worth 8 to 11 % of a launch: 64 contexts of
-// 512 .. 8k (32/8/128, bf16) 154.0 -> 138.1 us with the merge, 256 long-tailed ones (64/8/128) 1440 -> 1323 us, 384 over
-// FP8 pools (64/4/128) 798 -> 713 us (6.3 TB/s, what a streaming read reaches).
-template <bool STREAM>
-__device__ __forceinline__ uint4 load16(const unsigned char* p) {
-  typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
-  const uintx4 x = STREAM ? __builtin_nontemporal_load((const uintx4*)p) : *(const uintx4*)p;
-  return make_uint4(x[0], x[1], x[2], x[3]);
-}
 
 // One run of blocks.  WHOLE: it is one row from its first block to its last; FOLD: whose other part, in attn_decode_shared, is there
 // and folded in.  PART: it lies in one row and its result stays in LDS, un-normalised, [heads][D] in the wave's tiles and (max, sum) of

@@ -8,6 +8,7 @@
 
 #include <cstdint>
 #include <exception>
+#include <initializer_list>
 
 #include "rollattn.h"
 
@@ -16,6 +17,10 @@ namespace {
 decltype(&kv_write_rope) call_kv_write_rope = nullptr;      // the library's, as `bind` was given them
 decltype(&attn_decode) call_attn_decode = nullptr;
 decltype(&attn_append) call_attn_append = nullptr;
+decltype(&kv_write_norm_rope) call_kv_write_norm_rope = nullptr;
+decltype(&attn_tree_mask) call_attn_tree_mask = nullptr;
+decltype(&attn_tree) call_attn_tree = nullptr;
+decltype(&kv_accept) call_kv_accept = nullptr;
 
 struct Refusal {
   PyObject* kind;
@@ -110,6 +115,16 @@ int64_t row_stride(const at::Tensor& t) {
   return heads * d;
 }
 
+// (the kernels would read host addresses, or another GPU's, as this one's)
+void one_gpu(std::initializer_list<const at::Tensor*> all) {
+  int64_t device = -1;
+  for (const at::Tensor* t : all) {
+    if (!t) continue;
+    if (!t->is_cuda() || (device >= 0 && t->get_device() != device)) throw Refusal{PyExc_ValueError, "tensors are on one GPU"};
+    device = t->get_device();
+  }
+}
+
 // the chunks of B trajectories
 void chunks(const at::Tensor& q_lens, const at::Tensor& q_offsets, const at::Tensor& table) {
   ints(q_lens, table.size(0), "q_lens is [B] int32");
@@ -155,9 +170,9 @@ PyObject* guarded(Py_ssize_t nargs, Py_ssize_t want, F&& f) {
 }
 
 // q, k_new, v_new, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, cos_sin, max_q_len, positions, pair_axes, interleaved, k_scale,
-// v_scale, q_out, stream
-PyObject* host_kv_write_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  return guarded(nargs, 18, [&]() -> PyObject* {
+// v_scale, q_out, stream; with norms: q_weight, k_weight, eps
+PyObject* write_rope(PyObject* const* args, Py_ssize_t nargs, bool norms) {
+  return guarded(nargs, norms ? 21 : 18, [&]() -> PyObject* {
     const at::Tensor *q = maybe(args[0]), &k_new = tensor(args[1]), &v_new = tensor(args[2]);
     const at::Tensor &q_lens = dense(tensor(args[3])), &q_offsets = dense(tensor(args[4])), &k_pages = dense(tensor(args[5])), &v_pages = dense(tensor(args[6]));
     const at::Tensor &page_table = dense(tensor(args[7])), &ctx_lens = dense(tensor(args[8])), &cos_sin = dense(tensor(args[9]));
@@ -207,9 +222,20 @@ PyObject* host_kv_write_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     rope.interleaved = turned;
     rope.k_stride = row_stride(k_new);
     rope.v_stride = row_stride(v_new);
+    rollattn_norm norm{};
+    if (norms) {
+      const at::Tensor *q_weight = dense(maybe(args[18])), &k_weight = dense(tensor(args[19]));
+      if (k_weight.scalar_type() != at::kFloat || (q_weight && q_weight->scalar_type() != at::kFloat)) throw Refusal{PyExc_TypeError, "weights of norms are [D] float32"};
+      if (k_weight.numel() != d || (q && !q_weight) || (q_weight && q_weight->numel() != d)) throw Refusal{PyExc_ValueError, "weights of norms are [D] float32"};
+      norm.q_weight = (const float*)address(q_weight);
+      norm.k_weight = (const float*)address(k_weight);
+      norm.eps = (float)PyFloat_AsDouble(args[20]);
+      if (PyErr_Occurred()) throw Raised{};
+    }
     const rollattn_desc desc = descriptor(k_new, hq, k_pages, page_table, 1.f, k_scale, v_scale);
     ints(ctx_lens, page_table.size(0), "ctx_lens is [B] int32");
     chunks(q_lens, q_offsets, page_table);
+    if (norms) one_gpu({q, &k_new, &v_new, &q_lens, &q_offsets, &k_pages, &v_pages, &page_table, &ctx_lens, &cos_sin, positions, k_scale, v_scale, q_out, maybe(args[18]), &tensor(args[19])});
     const int32_t total = whole(total_q), longest = whole(number(args[10]));
     void* const stream = (void*)(uintptr_t)number(args[17]);
     void *const p_q = address(q), *const p_k = address(k_new), *const p_v = address(v_new), *const p_out = address(q_out), *const p_kp = address(k_pages), *const p_vp = address(v_pages);
@@ -218,11 +244,15 @@ PyObject* host_kv_write_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     int rc;
     {
       const Unlocked other_threads_run;
-      rc = call_kv_write_rope(&desc, &rope, p_q, p_k, p_v, p_lens, p_off, total, longest, p_out, p_kp, p_vp, p_table, p_ctx, p_ks, p_vs, stream);
+      if (norms) rc = call_kv_write_norm_rope(&desc, &rope, &norm, p_q, p_k, p_v, p_lens, p_off, total, longest, p_out, p_kp, p_vp, p_table, p_ctx, p_ks, p_vs, stream);
+      else rc = call_kv_write_rope(&desc, &rope, p_q, p_k, p_v, p_lens, p_off, total, longest, p_out, p_kp, p_vp, p_table, p_ctx, p_ks, p_vs, stream);
     }
     return PyLong_FromLong(rc);
   });
 }
+
+PyObject* host_kv_write_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return write_rope(args, nargs, false); }
+PyObject* host_kv_write_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return write_rope(args, nargs, true); }
 
 // The descriptor of an attention call.
 rollattn_desc attention(const at::Tensor& q, const at::Tensor& out, const at::Tensor& k_pages, const at::Tensor& v_pages, const at::Tensor& table, const at::Tensor& ctx_lens,
@@ -283,12 +313,108 @@ PyObject* host_attn_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
-// addresses of the library's kv_write_rope, attn_decode and attn_append
+// parents, q_lens, q_offsets, ctx_lens, max_q_len, tree_mask, positions, stream
+PyObject* host_attn_tree_mask(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded(nargs, 8, [&]() -> PyObject* {
+    const at::Tensor &parents = dense(tensor(args[0])), &q_lens = dense(tensor(args[1])), &q_offsets = dense(tensor(args[2])), &ctx_lens = dense(tensor(args[3]));
+    const at::Tensor &mask = dense(tensor(args[5])), *positions = dense(maybe(args[6]));
+    dims(parents, 1, "parents is [total_q] int32");
+    ints(parents, 0, "parents is [total_q] int32");
+    dims(q_lens, 1, "q_lens is [B] int32");
+    const int64_t total_q = parents.size(0), batch = q_lens.size(0);
+    ints(q_lens, batch, "q_lens is [B] int32");
+    ints(q_offsets, batch + 1, "q_offsets is [B + 1] int32");
+    ints(ctx_lens, batch, "ctx_lens is [B] int32");
+    if (mask.scalar_type() != at::kLong) throw Refusal{PyExc_TypeError, "tree_mask is [total_q, mask_words] int64"};
+    if (mask.dim() != 2 || mask.size(0) != total_q) throw Refusal{PyExc_ValueError, "tree_mask is [total_q, mask_words] int64"};
+    if (positions) {
+      ints(*positions, 0, "positions is [total_q] int32");
+      if (positions->numel() != total_q) throw Refusal{PyExc_ValueError, "positions is [total_q] int32"};
+    }
+    one_gpu({&parents, &q_lens, &q_offsets, &ctx_lens, &mask, positions});
+    const int32_t b = whole(batch), total = whole(total_q), longest = whole(number(args[4])), words = whole(mask.size(1));
+    void* const stream = (void*)(uintptr_t)number(args[7]);
+    const int32_t *const p_par = (int32_t*)address(parents), *const p_lens = (int32_t*)address(q_lens), *const p_off = (int32_t*)address(q_offsets), *const p_ctx = (int32_t*)address(ctx_lens);
+    uint64_t* const p_mask = (uint64_t*)address(mask);
+    int32_t* const p_pos = (int32_t*)address(positions);
+    int rc;
+    {
+      const Unlocked other_threads_run;
+      rc = call_attn_tree_mask(p_par, p_lens, p_off, p_ctx, b, total, longest, p_mask, words, p_pos, stream);
+    }
+    return PyLong_FromLong(rc);
+  });
+}
+
+// q, q_lens, q_offsets, tree_mask, k_pages, v_pages, page_table, ctx_lens, sm_scale, max_q_len, k_scale, v_scale, out, lse, workspace, stream
+PyObject* host_attn_tree(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded(nargs, 16, [&]() -> PyObject* {
+    const at::Tensor &q = dense(tensor(args[0])), &q_lens = dense(tensor(args[1])), &q_offsets = dense(tensor(args[2])), &mask = dense(tensor(args[3]));
+    const at::Tensor &k_pages = dense(tensor(args[4])), &v_pages = dense(tensor(args[5])), &page_table = dense(tensor(args[6])), &ctx_lens = dense(tensor(args[7]));
+    const at::Tensor *k_scale = dense(maybe(args[10])), *v_scale = dense(maybe(args[11])), &out = dense(tensor(args[12])), *lse = dense(maybe(args[13])), &workspace = dense(tensor(args[14]));
+    const rollattn_desc desc = attention(q, out, k_pages, v_pages, page_table, ctx_lens, args[8], k_scale, v_scale);
+    chunks(q_lens, q_offsets, page_table);
+    if (mask.scalar_type() != at::kLong) throw Refusal{PyExc_TypeError, "tree_mask is [total_q, mask_words] int64"};
+    if (mask.dim() != 2 || mask.size(0) != q.size(0)) throw Refusal{PyExc_ValueError, "tree_mask is [total_q, mask_words] int64"};
+    if (lse && (lse->scalar_type() != at::kFloat || lse->numel() != q.size(0) * q.size(1))) throw Refusal{PyExc_ValueError, "lse is [total_q, Hq] float32"};
+    one_gpu({&q, &q_lens, &q_offsets, &mask, &k_pages, &v_pages, &page_table, &ctx_lens, k_scale, v_scale, &out, lse, &workspace});
+    const int32_t total = whole(q.size(0)), longest = whole(number(args[9])), words = whole(mask.size(1));
+    void* const stream = (void*)(uintptr_t)number(args[15]);
+    void *const p_q = address(q), *const p_kp = address(k_pages), *const p_vp = address(v_pages), *const p_out = address(out), *const p_ws = address(workspace);
+    const int32_t *const p_lens = (int32_t*)address(q_lens), *const p_off = (int32_t*)address(q_offsets), *const p_table = (int32_t*)address(page_table), *const p_ctx = (int32_t*)address(ctx_lens);
+    const uint64_t* const p_mask = (uint64_t*)address(mask);
+    float* const p_lse = (float*)address(lse);
+    const size_t room = (size_t)workspace.nbytes();
+    int rc;
+    {
+      const Unlocked other_threads_run;
+      rc = call_attn_tree(&desc, p_q, p_lens, p_off, total, longest, p_mask, words, p_kp, p_vp, p_table, p_ctx, p_out, p_lse, p_ws, room, stream);
+    }
+    return PyLong_FromLong(rc);
+  });
+}
+
+// accepted, accept_lens, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, max_q_len, k_scale, v_scale, stream
+PyObject* host_kv_accept(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded(nargs, 12, [&]() -> PyObject* {
+    const at::Tensor &accepted = dense(tensor(args[0])), &accept_lens = dense(tensor(args[1])), &q_lens = dense(tensor(args[2])), &q_offsets = dense(tensor(args[3]));
+    const at::Tensor &k_pages = dense(tensor(args[4])), &v_pages = dense(tensor(args[5])), &page_table = dense(tensor(args[6])), &ctx_lens = dense(tensor(args[7]));
+    const at::Tensor *k_scale = dense(maybe(args[9])), *v_scale = dense(maybe(args[10]));
+    dims(k_pages, 4, "pools are [num_pages, Hkv, page_size, D]");
+    if (v_pages.sizes() != k_pages.sizes() || dtype_code(v_pages) != dtype_code(k_pages)) throw Refusal{PyExc_ValueError, "both pools are of one size and type"};
+    rollattn_desc desc = descriptor(k_pages, k_pages.size(1), k_pages, page_table, 1.f, k_scale, v_scale);
+    desc.q_dtype = desc.kv_dtype == ROLLATTN_F32 ? ROLLATTN_F32 : ROLLATTN_BF16;
+    dims(accepted, 1, "accepted is [total_q] int32");
+    ints(accepted, 0, "accepted is [total_q] int32");
+    ints(accept_lens, page_table.size(0), "accept_lens is [B] int32");
+    ints(ctx_lens, page_table.size(0), "ctx_lens is [B] int32");
+    chunks(q_lens, q_offsets, page_table);
+    one_gpu({&accepted, &accept_lens, &q_lens, &q_offsets, &k_pages, &v_pages, &page_table, &ctx_lens, k_scale, v_scale});
+    const int32_t total = whole(accepted.size(0)), longest = whole(number(args[8]));
+    void* const stream = (void*)(uintptr_t)number(args[11]);
+    void *const p_kp = address(k_pages), *const p_vp = address(v_pages);
+    const int32_t *const p_acc = (int32_t*)address(accepted), *const p_alen = (int32_t*)address(accept_lens), *const p_lens = (int32_t*)address(q_lens), *const p_off = (int32_t*)address(q_offsets);
+    const int32_t *const p_table = (int32_t*)address(page_table), *const p_ctx = (int32_t*)address(ctx_lens);
+    float *const p_ks = (float*)address(k_scale), *const p_vs = (float*)address(v_scale);
+    int rc;
+    {
+      const Unlocked other_threads_run;
+      rc = call_kv_accept(&desc, p_acc, p_alen, p_lens, p_off, total, longest, p_kp, p_vp, p_table, p_ctx, p_ks, p_vs, stream);
+    }
+    return PyLong_FromLong(rc);
+  });
+}
+
+// addresses of the library's calls
 PyObject* host_bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  return guarded(nargs, 3, [&]() -> PyObject* {
+  return guarded(nargs, 7, [&]() -> PyObject* {
     call_kv_write_rope = (decltype(call_kv_write_rope))(uintptr_t)number(args[0]);
     call_attn_decode = (decltype(call_attn_decode))(uintptr_t)number(args[1]);
     call_attn_append = (decltype(call_attn_append))(uintptr_t)number(args[2]);
+    call_kv_write_norm_rope = (decltype(call_kv_write_norm_rope))(uintptr_t)number(args[3]);
+    call_attn_tree_mask = (decltype(call_attn_tree_mask))(uintptr_t)number(args[4]);
+    call_attn_tree = (decltype(call_attn_tree))(uintptr_t)number(args[5]);
+    call_kv_accept = (decltype(call_kv_accept))(uintptr_t)number(args[6]);
     Py_RETURN_NONE;
   });
 }
@@ -298,6 +424,10 @@ PyMethodDef methods[] = {
     {"kv_write_rope", (PyCFunction)(void (*)(void))host_kv_write_rope, METH_FASTCALL, nullptr},
     {"attn_decode", (PyCFunction)(void (*)(void))host_attn_decode, METH_FASTCALL, nullptr},
     {"attn_append", (PyCFunction)(void (*)(void))host_attn_append, METH_FASTCALL, nullptr},
+    {"kv_write_norm_rope", (PyCFunction)(void (*)(void))host_kv_write_norm_rope, METH_FASTCALL, nullptr},
+    {"attn_tree_mask", (PyCFunction)(void (*)(void))host_attn_tree_mask, METH_FASTCALL, nullptr},
+    {"attn_tree", (PyCFunction)(void (*)(void))host_attn_tree, METH_FASTCALL, nullptr},
+    {"kv_accept", (PyCFunction)(void (*)(void))host_kv_accept, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

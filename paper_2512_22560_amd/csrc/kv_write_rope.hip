@@ -91,6 +91,28 @@ struct Turn {
   }
 };
 
+// The norm of a head's row, of which this lane has eight elements x in two runs of four and their weights w: by the root of the mean square,
+// in the order that the interface states (squares and runs in float32, the runs in double, which is exact, so that it does not matter
+// which lane has which).  Every lane of the row takes part.
+template <int D>
+__device__ __forceinline__ void normalise(float (&x)[8], const float (&w)[8], float eps) {
+#pragma clang fp contract(off)
+  const float lo = (x[0] * x[0] + x[1] * x[1]) + (x[2] * x[2] + x[3] * x[3]), hi = (x[4] * x[4] + x[5] * x[5]) + (x[6] * x[6] + x[7] * x[7]);
+  double sum = (double)lo + (double)hi;
+  auto add = [&](auto ctrl) __attribute__((always_inline)) {
+    const uintx2 v = __builtin_bit_cast(uintx2, sum);
+    const uintx2 o = {(unsigned int)__builtin_amdgcn_mov_dpp((int)v[0], decltype(ctrl)::value, 0xf, 0xf, true), (unsigned int)__builtin_amdgcn_mov_dpp((int)v[1], decltype(ctrl)::value, 0xf, 0xf, true)};
+    sum += __builtin_bit_cast(double, o);
+  };
+  add(std::integral_constant<int, 0xb1>{});      // the neighbour, the other two of four, the other four of eight, the other eight
+  add(std::integral_constant<int, 0x4e>{});
+  add(std::integral_constant<int, 0x141>{});
+  if constexpr (D == 128) add(std::integral_constant<int, 0x140>{});
+  const float r = 1.f / __builtin_sqrtf((float)(sum * (1.0 / D)) + eps);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (x[i] * r) * w[i];
+}
+
 // The cosines and sines of four pairs from j on; place: the token's place in its context, token: its number among the new ones.
 __device__ __forceinline__ void look_up(const RopeWriteArgs& a, int j, int place, int64_t token, Turn& turn) {
   const int half = a.rot_dim / 2;
@@ -134,6 +156,21 @@ struct Lane {
   }
 };
 
+// A lane's eight weights of a norm (none: nothing is done with them).
+template <bool NORM>
+struct Weights {
+  float w[8];
+  __device__ __forceinline__ void load(const float* weight, const Lane& lane) {
+    if constexpr (NORM) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i] = weight[lane.e0 + i];
+        w[4 + i] = weight[lane.e1 + i];
+      }
+    }
+  }
+};
+
 template <int SRC_BYTES>
 __device__ __forceinline__ Raw<SRC_BYTES> fetch(const Lane& lane, const void* rows, int64_t element) {
   const unsigned char* p = (const unsigned char*)rows + element * SRC_BYTES;
@@ -143,13 +180,18 @@ __device__ __forceinline__ Raw<SRC_BYTES> fetch(const Lane& lane, const void* ro
   return r;
 }
 
-// A row of the source type, turned where it has to be, at p; STREAM: past the caches' care.
-template <int SRC_BYTES, bool STREAM>
-__device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, const Turn& turn, void* p, Raw<SRC_BYTES> r) {
-  if (lane.turns) {
+// A row of the source type, normalised (NORM) and turned where it has to be, at p; STREAM: past the caches' care.
+template <int D, int SRC_BYTES, bool STREAM, bool NORM>
+__device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, const Turn& turn, const Weights<NORM>& weights, void* p, Raw<SRC_BYTES> r) {
+  if (NORM || lane.turns) {
     float x[8];
     to_float<SRC_BYTES>(r, x);
-    turn.apply(x, a.interleaved);
+    if constexpr (NORM) {
+      normalise<D>(x, weights.w, a.eps);
+      if (lane.turns) turn.apply(x, a.interleaved);
+    } else {
+      turn.apply(x, a.interleaved);
+    }
     if constexpr (SRC_BYTES == 4) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -206,7 +248,7 @@ __device__ __forceinline__ int place_of(const RopeWriteArgs& a, int first, int t
   return a.ctx_lens[lo] - a.q_lens[lo] + token - a.q_offsets[lo];
 }
 
-template <int D, int SRC_BYTES, bool STREAM>
+template <int D, int SRC_BYTES, bool STREAM, bool NORM>
 __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned int block) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;  // lanes of a row, heads under way at a time
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -222,6 +264,8 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
   const int h0 = part * a.part_heads, h1 = first + mine < a.total_q ? min(a.hq, h0 + a.part_heads) : 0;
   const Lane lane(a, col, true);
   Turn turn;
+  Weights<NORM> weights;
+  weights.load(a.q_weight, lane);
   const int heads = min(a.hq - h0, a.part_heads);     // (the same in all lanes)
   auto load = [&](Raw<SRC_BYTES> (&r)[kKeep], int h) {
 #pragma unroll
@@ -237,7 +281,7 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
       const int head = h0 + h + i * side + sub;
-      if (head < h1) store<SRC_BYTES, STREAM>(a, lane, turn, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
+      if (head < h1) store<D, SRC_BYTES, STREAM>(a, lane, turn, weights, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
     }
   }
 }
@@ -255,7 +299,7 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
 // 512 single tokens (64/4/128, int8; between events around the launch): 11.4 us with a search for each token's trajectory and a wave per
 // four query heads, 10.2 without the search, 8.8 with a wave per sixteen.
 // POOL: -1 the source type, else a KvKind; STREAM: rotated queries are written with the streaming hint; DEAL: pages are dealt out by a search
-template <int D, int SRC_BYTES, int POOL, bool STREAM, bool DEAL>
+template <int D, int SRC_BYTES, int POOL, bool STREAM, bool DEAL, bool NORM>
 __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWriteArgs a) {
   constexpr bool kCodes = POOL >= 0, kHeadScales = kCodes && kv_has_head_scales(POOL);
   constexpr bool kInt8 = POOL == kKvInt8Head;
@@ -268,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   const unsigned int pages_before = (unsigned int)((uint64_t)g * a.page_share >> 32), pages_then = (unsigned int)((uint64_t)(g + 1) * a.page_share >> 32);
   if (pages_before == pages_then) {
     const unsigned int unit = (g - pages_before) * kXcds + at;
-    turn_queries<D, SRC_BYTES, STREAM>(a, unit);
+    turn_queries<D, SRC_BYTES, STREAM, NORM>(a, unit);
     return;
   }
   // eight pages' keys, then their values
@@ -296,6 +340,8 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   const int group = (int)threadIdx.x / kLanes, col = (int)threadIdx.x % kLanes;
   const bool rotate = a.cos_sin != nullptr && pool == 0;
   const Lane lane(a, col, rotate);
+  Weights<NORM> weights;
+  if (pool == 0) weights.load(a.k_weight, lane);
   const bool turns = lane.turns;
   const int e0 = lane.e0, e1 = lane.e1;
   const int turn_pages = DEAL ? len / kPageSize + 1 : a.pages;   // (one page each where they were searched for)
@@ -322,7 +368,10 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
           if (h - head0 + i * side < hkv) r[i] = fetch_row(min(h + i * side, hkv - 1));
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
-          if (h + i * side < hkv) store<SRC_BYTES, false>(a, lane, turn, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
+          if (h + i * side < hkv) {
+            if (!NORM || pool == 0) store<D, SRC_BYTES, false>(a, lane, turn, weights, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
+            else store<D, SRC_BYTES, false>(a, lane, turn, Weights<false>{}, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
+          }
       }
   } else {
     static_assert(SRC_BYTES == 2, "codes are made of bf16 rows");
@@ -333,6 +382,9 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
     constexpr float kMax = kInt8 ? kInt8Max : kE4m3Max;
     auto rotated = [&](const Raw<SRC_BYTES>& r, float (&x)[8]) {
       to_float<2>(r, x);
+      if constexpr (NORM) {
+        if (pool == 0) normalise<D>(x, weights.w, a.eps);
+      }
       if (turns) turn.apply(x, a.interleaved);
     };
     auto encode4 = [&](const float* x) { return kInt8 ? encode4_int8(x) : encode4_e4m3(x); };
@@ -486,17 +538,24 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
   }
 }
 
+// This file makes two objects: the write without norms and, with the macro set, the one with them.
+#ifdef ROLLATTN_NORM
+constexpr bool kNorm = true;
+#else
+constexpr bool kNorm = false;
+#endif
+
 template <int D, bool STREAM, bool DEAL>
 hipError_t launch_as(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid, hipStream_t s) {
   if (src_bytes == 4) {
     if (pool != -1) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((kv_write_rope_kernel<D, 4, -1, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((kv_write_rope_kernel<D, 4, -1, STREAM, DEAL, kNorm>), grid, dim3(kThreads), 0, s, a);
   } else {
     switch (pool) {
-      case -1: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, -1, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvFp8: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvFp8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8Head, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
-      case kKvInt8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvInt8Head, STREAM, DEAL>), grid, dim3(kThreads), 0, s, a); break;
+      case -1: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, -1, STREAM, DEAL, kNorm>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvFp8: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8, STREAM, DEAL, kNorm>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvFp8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvFp8Head, STREAM, DEAL, kNorm>), grid, dim3(kThreads), 0, s, a); break;
+      case kKvInt8Head: hipLaunchKernelGGL((kv_write_rope_kernel<D, 2, kKvInt8Head, STREAM, DEAL, kNorm>), grid, dim3(kThreads), 0, s, a); break;
       default: return hipErrorInvalidValue;
     }
   }
@@ -505,7 +564,12 @@ hipError_t launch_as(const RopeWriteArgs& a, int src_bytes, int pool, dim3 grid,
 
 }  // namespace
 
-hipError_t launch_kv_write_rope(const RopeWriteArgs& args, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s) {
+#ifdef ROLLATTN_NORM
+hipError_t launch_kv_write_norm_rope(const RopeWriteArgs& args,
+#else
+hipError_t launch_kv_write_rope(const RopeWriteArgs& args,
+#endif
+                                int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s) {
   RopeWriteArgs a = args;
   a.one_each = max_q_len == 1 && a.total_q == a.batch;   // (no trajectory has more, so each has one where so many rows are theirs)
   // A run of n tokens touches at most (n + 14) / 16 + 1 pages, wherever it starts: as many workgroups per trajectory as the longest chunk

@@ -202,6 +202,44 @@ struct RopeWriteArgs {
   uint64_t page_share;
   uint32_t pair_axes[4];           // two bits per pair
   int32_t interleaved;
+  // norms in front of the rotation (both null: none)
+  const float *q_weight, *k_weight;
+  float eps;
+};
+
+// Attention of drafted tokens.
+struct TreeArgs {
+  const void* q;
+  const void* k_pages;
+  const void* v_pages;
+  const int32_t* page_table;
+  const int32_t* ctx_lens;
+  const int32_t* q_lens;
+  const int32_t* q_offsets;
+  const uint64_t* mask;            // [total_q][mask_words]
+  void* out;
+  float* lse;                      // optional [total_q][Hq], as in DecodeArgs
+  const float* k_scale;
+  const float* v_scale;
+  int32_t batch, hq, hkv, group, max_pages, mask_words, total_q;
+  float scale_log2;
+  int32_t row_tiles;               // set at launch: tiles of query rows per KV head that the longest draft has
+};
+
+// Parents to masks and positions.
+struct TreeMaskArgs {
+  const int32_t *parents, *q_lens, *q_offsets, *ctx_lens;
+  uint64_t* mask;
+  int32_t* positions;              // optional
+  int32_t batch, mask_words;
+};
+
+// The accepted rows of drafts to consecutive places.
+struct AcceptArgs {
+  const int32_t *accepted, *accept_lens, *q_lens, *q_offsets, *page_table, *ctx_lens;
+  void *k_pages, *v_pages;
+  float *k_scale, *v_scale;
+  int32_t batch, hkv, max_pages;
 };
 
 // Launchers (defined in the .hip files).  Each returns the hipError_t of its launch.
@@ -232,6 +270,12 @@ hipError_t launch_kv_write(const void* k_new, const void* v_new, const int32_t* 
                            int32_t max_q_len, int head_dim, int src_bytes, bool fp8, hipStream_t s);
 // pool: -1 for one of the source type, else what its codes are (bf16 sources)
 hipError_t launch_kv_write_rope(const RopeWriteArgs& a, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s);
+hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, int32_t max_q_len, hipStream_t s);
+hipError_t launch_tree_f32(const TreeArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_tree_mask(const TreeMaskArgs& a, int32_t max_q_len, hipStream_t s);
+// row_bytes: of a token and KV head in the pools; pool as in launch_kv_write_rope
+hipError_t launch_kv_accept(const AcceptArgs& a, int32_t max_q_len, int head_dim, int row_bytes, int pool, hipStream_t s);
+hipError_t launch_kv_write_norm_rope(const RopeWriteArgs& a, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s);   // (with norms)
 hipError_t launch_merge_states(const void* o1, const float* d1, const void* o2, const float* d2, void* out, float* d_out,
                                long rows, int head_dim, bool f32, hipStream_t s);
 hipError_t launch_check_inputs(const int32_t* page_table, const int32_t* ctx_lens, const int32_t* q_lens,
