@@ -919,9 +919,37 @@ int attn_tree_mask(const int32_t* parents, const int32_t* q_lens, const int32_t*
   return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
 }
 
+namespace {
+// Workspace of attn_tree: the plan and the partials of rows that were cut.
+struct TreeLayout {
+  int32_t parts, tiles, workers;
+  size_t header, prefix, wstart, partial_ml, partial_o, total;
+};
+TreeLayout tree_layout(const rollattn_desc& d, int64_t max_q_len) {
+  TreeLayout w{};
+  size_t off = 256;
+  if (d.q_dtype == ROLLATTN_F32) {
+    w.total = off;
+    return w;
+  }
+  const int64_t rows = std::max<int64_t>(1, max_q_len) * (d.num_q_heads / d.num_kv_heads);
+  w.parts = rows <= kTreeTileRows ? 1 : 2;
+  w.tiles = (int32_t)std::min<int64_t>((rows + kTreeTileRows * w.parts - 1) / (kTreeTileRows * w.parts), INT32_MAX);
+  w.workers = kNumCUs * 4 * (w.parts == 1 ? 2 : 1);
+  const size_t parts = 2 * (size_t)w.workers * w.parts * kTreeTileRows;
+  w.header = 0;
+  w.prefix = off;      off += align256(sizeof(int32_t) * ((size_t)d.batch + 1));
+  w.wstart = off;      off += align256(sizeof(int32_t) * 4 * (size_t)w.workers);
+  w.partial_ml = off;  off += align256(sizeof(float) * 2 * parts);
+  w.partial_o = off;   off += align256(sizeof(float) * d.head_dim * parts);
+  w.total = off;
+  return w;
+}
+}  // namespace
+
 size_t rollattn_tree_workspace_bytes(const rollattn_desc* desc, int32_t total_q, int32_t max_q_len) {
   if (check_desc(desc) != ROLLATTN_OK || total_q < 0 || max_q_len < 0) return 0;
-  return 256;
+  return tree_layout(*desc, std::min(max_q_len, total_q)).total;
 }
 
 int attn_tree(const rollattn_desc* desc, const void* q, const int32_t* q_lens, const int32_t* q_offsets, int32_t total_q, int32_t max_q_len,
@@ -939,9 +967,19 @@ int attn_tree(const rollattn_desc* desc, const void* q, const int32_t* q_lens, c
   if (!aligned16(q) || !aligned16(q_lens) || !aligned16(q_offsets) || !aligned16(tree_mask) || !aligned16(k_pages) || !aligned16(v_pages) ||
       !aligned16(page_table) || !aligned16(ctx_lens) || !aligned16(out) || !aligned16(lse) || !aligned16(workspace))
     return ROLLATTN_EALIGN;
-  if (workspace_bytes < rollattn_tree_workspace_bytes(desc, total_q, max_q_len)) return ROLLATTN_EWORKSPACE;
+  const TreeLayout w = tree_layout(*desc, std::min(max_q_len, total_q));
+  if (workspace_bytes < w.total) return ROLLATTN_EWORKSPACE;
   if (desc->batch > 65535) return ROLLATTN_ESHAPE;
+  if (desc->q_dtype != ROLLATTN_F32) {
+    // a worker's start packs the row into 11 bits and the block into 20; blocks are counted in 32 bits, as are the merge's waves
+    const int64_t rows = (int64_t)desc->num_kv_heads * w.tiles, blocks = (int64_t)desc->max_pages_per_seq / 2 + 1;
+    if (rows > 2047 || blocks > (1 << 20) || desc->batch * rows * blocks > INT32_MAX || desc->batch * rows * 8 > INT32_MAX) return ROLLATTN_ESHAPE;
+  }
   TreeArgs a{};
+  char* base = (char*)workspace;
+  a.tile_parts = w.parts; a.row_tiles = w.tiles; a.workers = w.workers;
+  a.header = (int32_t*)(base + w.header); a.prefix = (int32_t*)(base + w.prefix); a.wstart = (int32_t*)(base + w.wstart);
+  a.partial_ml = (float*)(base + w.partial_ml); a.partial_o = (float*)(base + w.partial_o);
   a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.page_table = page_table; a.ctx_lens = ctx_lens;
   a.q_lens = q_lens; a.q_offsets = q_offsets; a.mask = tree_mask; a.out = out; a.lse = lse;
   a.k_scale = desc->k_scale; a.v_scale = desc->v_scale;
@@ -951,7 +989,7 @@ int attn_tree(const rollattn_desc* desc, const void* q, const int32_t* q_lens, c
   hipStream_t s = (hipStream_t)hip_stream;
   ProfileScope prof(s);
   const hipError_t e = desc->q_dtype == ROLLATTN_F32 ? launch_tree_f32(a, desc->head_dim, s)
-                                                     : launch_tree_mfma(a, desc->head_dim, kv_kind(*desc), std::min(max_q_len, total_q), s);
+                                                     : launch_tree_mfma(a, desc->head_dim, kv_kind(*desc), s);
   prof.stop();
   return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
 }

@@ -23,6 +23,7 @@ constexpr int kDirectPages = 32;        // contexts of at most this many pages a
 constexpr int kDirectPagesFew = 64;     // the latter where their rows are resident at once, a workgroup each
 constexpr int kDirectRowsFew = 512;     // ... two to a CU
 constexpr int kAppendTileRows = 256;    // query rows (token, head-in-group pairs) per append workgroup
+constexpr int kTreeTileRows = 32;       // drafts: query rows of one product
 constexpr int kXcds = 8;                // accelerator dies, each with its own L2; workgroups are dealt to them round-robin
 constexpr int kAppendBlockTokens = 64;  // KV tokens staged per step of the append kernel
 constexpr int kTileRecWords = 8;       // append: int32 per tile record (32 bytes: one scalar load)
@@ -223,7 +224,10 @@ struct TreeArgs {
   const float* v_scale;
   int32_t batch, hq, hkv, group, max_pages, mask_words, total_q;
   float scale_log2;
-  int32_t row_tiles;               // set at launch: tiles of query rows per KV head that the longest draft has
+  // bf16 queries: products' worth of query rows in a tile (1 or 2), tiles per KV head that the longest draft has, workers, and the plan
+  int32_t tile_parts, row_tiles, workers;
+  int32_t *header, *prefix, *wstart;
+  float *partial_ml, *partial_o;   // float[2 workers][tile_parts][32][2] (max in log2 units, sum) and [..][D / 8][64][4], as the accumulators lie
 };
 
 // Parents to masks and positions.
@@ -270,7 +274,7 @@ hipError_t launch_kv_write(const void* k_new, const void* v_new, const int32_t* 
                            int32_t max_q_len, int head_dim, int src_bytes, bool fp8, hipStream_t s);
 // pool: -1 for one of the source type, else what its codes are (bf16 sources)
 hipError_t launch_kv_write_rope(const RopeWriteArgs& a, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s);
-hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, int32_t max_q_len, hipStream_t s);
+hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, hipStream_t s);
 hipError_t launch_tree_f32(const TreeArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_tree_mask(const TreeMaskArgs& a, int32_t max_q_len, hipStream_t s);
 // row_bytes: of a token and KV head in the pools; pool as in launch_kv_write_rope
