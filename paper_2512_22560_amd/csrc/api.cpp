@@ -933,9 +933,9 @@ TreeLayout tree_layout(const rollattn_desc& d, int64_t max_q_len) {
     return w;
   }
   const int64_t rows = std::max<int64_t>(1, max_q_len) * (d.num_q_heads / d.num_kv_heads);
-  w.parts = rows <= kTreeTileRows ? 1 : 2;
+  w.parts = rows <= kTreeTileRows ? 1 : rows <= 2 * kTreeTileRows ? 2 : rows <= 4 * kTreeTileRows ? 4 : 8;
   w.tiles = (int32_t)std::min<int64_t>((rows + kTreeTileRows * w.parts - 1) / (kTreeTileRows * w.parts), INT32_MAX);
-  w.workers = kNumCUs * 4 * (w.parts == 1 ? 2 : 1);
+  w.workers = kNumCUs * 8 / w.parts;       // two waves to a SIMD
   const size_t parts = 2 * (size_t)w.workers * w.parts * kTreeTileRows;
   w.header = 0;
   w.prefix = off;      off += align256(sizeof(int32_t) * ((size_t)d.batch + 1));

@@ -1,17 +1,17 @@
 // Attention of a tree of drafted tokens (bf16 queries) over bf16 or 8-bit (E4M3, int8) paged KV (gfx950).
 //
-// A row is (trajectory, KV head, tile of 32 or 64 query rows): a query row is a (drafted token, query head of the group) pair,
+// A row is (trajectory, KV head, tile of 32 W query rows): a query row is a (drafted token, query head of the group) pair,
 // token-major, so the heads that share the KV head and the tokens of a draft that fit one tile read K and V once.  As in decode, rows
-// are cut into 32-token blocks, laid end to end, and every wave is a worker with one equal run of that sequence; it streams its run
-// from memory straight into a private ring of LDS tiles, without any barrier, and consumes a block with
-//   S^T = K Q^T          (tokens x query rows, v_mfma_f32_32x32x16, K rows as A; one LDS read for all query rows)
-//   O^T += V^T P^T       (dims x query rows, V read back transposed with ds_read_b64_tr_*; one read for all query rows)
+// are cut into 32-token blocks, laid end to end, and every worker has one equal run of that sequence; a worker is W waves of 32 query rows
+// each.  It streams its run from memory straight into a ring of LDS tiles, and each of its waves consumes a block with
+//   S^T = K Q^T          (tokens x query rows, v_mfma_f32_32x32x16, K rows as A)
+//   O^T += V^T P^T       (dims x query rows, V read back transposed with ds_read_b64_tr_*)
 // A run that covers a whole row writes the row's output itself; one that starts or ends inside a row leaves an un-normalised partial
 // (max, sum, O) for the merge.
 // A block that lies in the cached prefix is seen whole by every row and knows no mask.  In the blocks behind it a row sees the tokens
 // whose bits are set in its mask words, eight tokens at a time.  What a row does not see must not reach it: a score is replaced before
-// the maximum, and where values of such a block are not finite (zero times infinity would not be zero) they are added apart to the rows
-// that see them, and leave the second product.
+// the maximum, and where values of such a block are not finite (zero times infinity would not be zero) zeros take their places in the
+// second product, and they are added apart to the rows that see them.
 // Codes become operands as in decode: see decode_mfma.hip for the range of f16 and the power of two per query row.
 #include "stream_tiles.h"
 
@@ -21,9 +21,9 @@ namespace {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;             // of the merge
 constexpr int kWaves = kThreads / 64;
-constexpr int kRows = kTreeTileRows;      // query rows of one product
+constexpr int kRows = kTreeTileRows;      // query rows of a wave
 
 __device__ __forceinline__ floatx16 mfma32(bf16x8 x, bf16x8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
 __device__ __forceinline__ floatx16 mfma32(halfx8 x, halfx8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
@@ -31,6 +31,12 @@ __device__ __forceinline__ floatx16 mfma32(halfx8 x, halfx8 y, floatx16 z) { ret
 // Row t of an S^T tile holds this token of its 16-token group: the middle two quads are swapped, so that the 8 scores a lane ends up with
 // are 8 consecutive tokens.
 __device__ __forceinline__ int tau(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+
+// Tiles of 32 W query rows that a draft of n tokens has per KV head (no more than the caller has said that the longest one has).
+__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int n) {
+  const int rows = kRows * a.tile_parts;
+  return n > 0 ? min((n * a.group + rows - 1) / rows, a.row_tiles) : 0;
+}
 
 // Which 16-byte column a logical chunk of token row t lands in.
 template <int D, bool FP8>
@@ -93,60 +99,66 @@ struct RowAt {
   }
 };
 
-// Blocks of a wave's ring, the one in work included.  A wave of 64 query rows has a SIMD to itself (accumulators alone are 128 registers of
-// 512) and a quarter of the LDS, waves of 32 are two to a SIMD.
-template <bool FP8, int RT>
-constexpr int kTreeSlots = RT == 2 ? (FP8 ? 4 : 2) : (FP8 ? 2 : 1);
-template <int D, bool FP8, int RT>
+// A worker's ring: its blocks, the one in work included, so that two waves to a SIMD find their LDS.
+template <int D, bool FP8, int W>
 struct TreeLds {
   typedef Geo<D, FP8> G_;
-  __attribute__((aligned(1024))) unsigned char k[kTreeSlots<FP8, RT>][G_::kTileBytes], v[kTreeSlots<FP8, RT>][G_::kTileBytes];
-  float scales[FP8 ? kTreeSlots<FP8, RT> : 1][FP8 ? 64 : 4];   // of a block's two pages: K's, V's (the other lanes' are copies)
+  static constexpr int kSlots = W == 1 ? (FP8 ? 2 : 1) : W == 2 ? (FP8 ? 4 : 2) : 4;
+  __attribute__((aligned(1024))) unsigned char k[kSlots][G_::kTileBytes], v[kSlots][G_::kTileBytes];
+  float scales[FP8 ? kSlots : 1][W][FP8 ? 64 : 4];   // of a block's two pages: K's, V's (the other lanes' are copies), for each wave
 };
 
 // One run of n_mine blocks from block blk of row (b, r) on.
-// Loads.  The tiles of block i + slots go into the places of block i, K's as soon as the first product has read them and V's behind the
-// second.  HBM -> LDS without a register stop: lane l's 16 bytes land at M0 + 16 l, so a row's chunks are swizzled by the address a lane
+// Loads.  W = 1: the tiles of block i + slots go into the places of block i, K's as soon as the first product has read them and V's behind
+// the second; no barriers.  Else each wave loads its share of a block, waits for its own loads and meets the others at one barrier per block:
+// behind it the block is there, and the place of the block before is free for the one that is slots - 1 ahead.
+// HBM -> LDS without a register stop: lane l's 16 bytes land at M0 + 16 l, so a row's chunks are swizzled by the address a lane
 // reads from.  The compiler does not see these loads as loads; they are awaited by count: vector-memory counts go down in order, so
 // with N of these loads sent after the ones that are waited for, no more than N outstanding operations of any kind means that those have
 // landed (others in between only make the wait longer).
-template <int D, int KV, int RT, bool STREAM>
-__device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, int blk0, int n_mine, int worker, TreeLds<D, kv_is_codes(KV), RT>& lds) {
+template <int D, int KV, int W, bool STREAM>
+__device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, int blk0, int n_mine, int worker, int wave, TreeLds<D, kv_is_codes(KV), W>& lds) {
   constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
   constexpr bool INT8 = KV == kKvInt8Head;
-  constexpr int kTile = kRows * RT, kSlots = kTreeSlots<FP8, RT>;
+  constexpr int kTile = kRows * W, kSlots = TreeLds<D, FP8, W>::kSlots;
   constexpr int kKK = D / 16, kDT = D / 32;
   using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
   using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;  // ... and of the second
   using op = std::conditional_t<HEAD, _Float16, __bf16>;
   using G_ = Geo<D, FP8>;
-  constexpr int kKLoads = G_::kLoads + (FP8 ? 1 : 0);      // loads of a block's K tile and scales
+  // this wave's loads of a block: of each pool's tile its share, or where there are more waves than a tile has loads, of one pool's tile one
+  // (where there are more than both have, some twice: the same bytes to the same place); its copy of the scales
+  constexpr int kShare = G_::kLoads >= W ? G_::kLoads / W : 1;
+  constexpr int kVLoads = G_::kLoads >= W ? kShare : 0, kKLoads = kShare + (FP8 ? 1 : 0);
   const int lane = lane_id();
   const int n32 = lane & 31;   // query row (B column) / K token row (A row) carried by this lane
   const int h2 = lane >> 5;    // half of the contraction this lane feeds
 
-  const int group = a.group, hkv = a.hkv, n_rt = a.row_tiles, rows_per_b = hkv * n_rt;
+  const int group = a.group, hkv = a.hkv;
   const size_t tile_stride = (size_t)kPageSize * G_::kRowBytes;   // bytes of one (page, head) tile
   const bool flip = a.scale_log2 < 0.f;                           // (queries the other way round, so that larger scores are larger exponents)
   const float scale_log2 = __builtin_fabsf(a.scale_log2);
 
-  struct Cursor { int b, r, blk, n, len; };   // trajectory, row within it, block within the row; blocks in the row, context length
-  auto blocks_of = [&](int len) { return (len + kBlockTokens - 1) / kBlockTokens; };
-  Cursor pc{b0, r0, blk0, 0, 0};              // producer: next block to request from HBM
-  pc.len = Draft(a, b0).len;
-  pc.n = blocks_of(pc.len);
+  struct Cursor { int b, r, blk, n, len, tiles; };   // trajectory, row within it, block within the row; blocks in the row, context length, tiles per KV head
+  auto enter = [&](Cursor& c) {
+    const Draft d(a, c.b);
+    c.tiles = tree_tiles(a, d.n);
+    c.len = c.tiles ? d.len : 0;
+    c.n = (c.len + kBlockTokens - 1) / kBlockTokens;
+  };
+  Cursor pc{b0, r0, blk0, 0, 0, 0};           // producer: next block to request from HBM
+  enter(pc);
   Cursor cc = pc;                             // consumer: block being computed
-  auto advance = [&](Cursor& c) {
-    if (++c.blk < c.n) return;
+  auto advance = [&](Cursor& c) {             // (whether it is another row now)
+    if (++c.blk < c.n) return false;
     c.blk = 0;
-    if (++c.r < rows_per_b) return;
+    if (++c.r < hkv * c.tiles) return true;
     c.r = 0;
-    for (;;) {
-      const Draft d(a, ++c.b);
-      c.len = d.n > 0 ? d.len : 0;
-      if (c.len) break;
-    }
-    c.n = blocks_of(c.len);
+    do {
+      ++c.b;
+      enter(c);
+    } while (c.len == 0);
+    return true;
   };
 
   // ---- producer: a window of 64 page ids (32 blocks) of the current row, one per lane
@@ -161,82 +173,105 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     if constexpr (STREAM) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(m0), "v"(off), "s"(base) : "memory");
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(base) : "memory");
   };
-  // a tile of one pool: row row0 + lane / chunks of the block per load; rows at or past L_b read its last one again
-  auto load_tile = [&](const void* pool, auto key_of, unsigned char* dst) __attribute__((always_inline)) {
-    const unsigned char* tile[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) tile[i] = (const unsigned char*)pool + (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(p_page[i] * hkv + p_g) * tile_stride;
+  // this wave's share of a tile of one pool: row row0 + lane / chunks of the block per load; rows at or past L_b read its last one again
+  auto load_tile = [&](const void* pool, int first, auto count_c, auto key_of, unsigned char* dst) __attribute__((always_inline)) {
     const int c = lane % G_::kChunks, sub = lane / G_::kChunks;
 #pragma unroll
-    for (int j = 0; j < G_::kLoads; ++j) {
-      const int row0 = j * G_::kRowsPerLoad, row = row0 + sub;
+    for (int i = 0; i < decltype(count_c)::value; ++i) {
+      const int j = first + i * W, row0 = j * G_::kRowsPerLoad, row = row0 + sub;
+      const int page = row0 < kPageSize ? p_page[0] : p_page[1];
+      const unsigned char* tile = (const unsigned char*)pool + (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(page * hkv + p_g) * tile_stride;
       int slot = row % kPageSize;
       if (p_lim < kBlockTokens) slot = min(row, p_lim - 1) % kPageSize;      // (the row's last block alone)
-      dma16(tile[row0 / kPageSize], slot * G_::kRowBytes + ((c ^ key_of(row)) & (G_::kChunks - 1)) * 16, dst + j * 1024);
+      dma16(tile, slot * G_::kRowBytes + ((c ^ key_of(row)) & (G_::kChunks - 1)) * 16, dst + j * 1024);
     }
   };
-  // what block pc of the run needs, then its K tile and scales; its V tile
-  auto issue_k = [&](int slot) __attribute__((always_inline)) {
+  constexpr std::integral_constant<int, kShare> share_c{};
+  auto load_k = [&](int slot, int first) __attribute__((always_inline)) {
+    load_tile(a.k_pages, first, share_c, [](int row) { return tree_key_k<D, FP8>(row); }, lds.k[slot]);
+  };
+  auto load_v = [&](int slot, int first) __attribute__((always_inline)) {
+    load_tile(a.v_pages, first, share_c, [](int row) { return tree_key_v<FP8>(row); }, lds.v[slot]);
+  };
+  // what block pc of the run needs
+  auto look_up = [&]() __attribute__((always_inline)) {
     const int k = pc.blk >> 5;
     if (k != pwin) {
       pid_vec = (pwin >= 0 && k == pwin + 1) ? pid_next : load_window(k);
       pid_next = load_window(k + 1);
       pwin = k;
     }
-    p_g = pc.r / n_rt;
+    p_g = pc.r / pc.tiles;
     p_lim = min(pc.len - pc.blk * kBlockTokens, kBlockTokens);
     p_page[0] = __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1));
     p_page[1] = p_lim > kPageSize ? __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1) + 1) : p_page[0];
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (what this overwrites has been read)
-    load_tile(a.k_pages, [](int row) { return tree_key_k<D, FP8>(row); }, lds.k[slot]);
+  };
+  auto load_scales = [&](int slot) __attribute__((always_inline)) {
     if constexpr (FP8) {
       const int page = lane & 1 ? p_page[1] : p_page[0];
       const float* from = (lane & 2 ? a.v_scale : a.k_scale) + (HEAD ? (size_t)page * hkv + p_g : (size_t)page);
-      const unsigned int m0 = __builtin_amdgcn_readfirstlane((unsigned int)(uintptr_t)lds.scales[slot]);
+      const unsigned int m0 = __builtin_amdgcn_readfirstlane((unsigned int)(uintptr_t)lds.scales[slot][wave]);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(from) : "memory");
     }
   };
-  auto issue_v = [&](int slot) __attribute__((always_inline)) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    load_tile(a.v_pages, [](int row) { return tree_key_v<FP8>(row); }, lds.v[slot]);
-    // step to the next block of the run (never past its end: the rows after the last block need not exist); a new row starts with a
-    // fresh page-id window
-    if (++issued < n_mine) {
-      const int row_before = pc.b * rows_per_b + pc.r;
-      advance(pc);
-      if (pc.b * rows_per_b + pc.r != row_before) pwin = -1;
-    }
+  // step to the next block of the run (never past its end: the rows after the last block need not exist); a new row starts with a
+  // fresh page-id window
+  auto step = [&]() __attribute__((always_inline)) {
+    if (++issued < n_mine && advance(pc)) pwin = -1;
   };
-  // until all but the loads of `pairs` blocks, and kMore others, have landed
-  auto await = [&](int pairs, auto more_c) __attribute__((always_inline)) {
-    constexpr int kMore = decltype(more_c)::value, kPair = G_::kLoads + kKLoads;
-    if (kSlots > 3 && pairs == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 3 ? 3 * kPair + kMore : 0) : "memory");
-    else if (kSlots > 2 && pairs == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 2 ? 2 * kPair + kMore : 0) : "memory");
-    else if (kSlots > 1 && pairs == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 1 ? kPair + kMore : 0) : "memory");
+  // (what the loads overwrite has been read)
+  auto all_read = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+  auto issue_k = [&](int slot) __attribute__((always_inline)) {      // W = 1: K and scales, then V
+    look_up();
+    load_k(slot, 0);
+    load_scales(slot);
+  };
+  auto issue_v = [&](int slot) __attribute__((always_inline)) {
+    load_v(slot, 0);
+    step();
+  };
+  auto issue = [&](int slot) __attribute__((always_inline)) {
+    look_up();
+    if constexpr (kVLoads > 0) {
+      load_k(slot, wave);
+      load_v(slot, wave);
+    } else if (wave % (2 * G_::kLoads) < G_::kLoads) {
+      load_k(slot, wave % G_::kLoads);
+    } else {
+      load_v(slot, wave % G_::kLoads);
+    }
+    load_scales(slot);
+    step();
+  };
+  // until all but this wave's loads of `blocks` blocks, and kMore others, have landed
+  auto await = [&](int blocks, auto more_c) __attribute__((always_inline)) {
+    constexpr int kMore = decltype(more_c)::value, kBlock = kVLoads + kKLoads;
+    if (kSlots > 3 && blocks == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 3 ? 3 * kBlock + kMore : 0) : "memory");
+    else if (kSlots > 2 && blocks == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 2 ? 2 * kBlock + kMore : 0) : "memory");
+    else if (kSlots > 1 && blocks == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 1 ? kBlock + kMore : 0) : "memory");
     else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMore) : "memory");
   };
 
   // ---- consumer state
-  kx8 qop[RT][kKK];          // Q^T as the B operand: lane (row n32, half h2), 8 dims per step
-  float q_unit[RT];          // int8: what a unit of this lane's row is worth
-  floatx16 acc[RT][kDT];     // O^T: lane (row n32, half h2) holds dims dt*32 + (i/4)*8 + h2*4 + i%4
-  float m_run[RT], l_run[RT];// running max (log2 units) of this lane's rows, its share of the running sums
+  kx8 qop[kKK];              // Q^T as the B operand: lane (row n32, half h2), 8 dims per step
+  float q_unit = 0.f;        // int8: what a unit of this lane's row is worth
+  floatx16 acc[kDT];        // O^T: lane (row n32, half h2) holds dims dt*32 + (i/4)*8 + h2*4 + i%4
+  float m_run = 0.f, l_run = 0.f;   // running max (log2 units) of this lane's rows, its share of the running sums
   int seg_first_blk = 0;     // block of the row at which the current segment started
   bool first_segment = true, dirty = false;   // dirty: values of the segment that are no numbers have been left out of its sums
   int rows_here = 0, prefix = 0, n_b = 0, q_off = 0, j0 = 0, g = 0;   // of the consumer's row
 
   auto begin_segment = [&]() __attribute__((always_inline)) {
     const Draft d(a, cc.b);
-    g = cc.r / n_rt;
-    j0 = (cc.r - g * n_rt) * kTile;
+    g = cc.r / cc.tiles;
+    j0 = (cc.r - g * cc.tiles) * kTile + wave * kRows;
     n_b = d.n;
     q_off = d.off;
     prefix = d.len - d.n;
-    rows_here = min(kTile, d.n * group - j0);        // (none: a tile that only longer drafts have)
-#pragma unroll
-    for (int c = 0; c < RT; ++c) {
+    rows_here = min(kRows, d.n * group - j0);        // (none: a wave past the last row helps with the loads)
+    {
       // (rows past the last read it again; what becomes of them is not stored)
-      const RowAt at(a, d, g, max(0, min(j0 + c * kRows + n32, d.n * group - 1)));
+      const RowAt at(a, d, g, max(0, min(j0 + n32, d.n * group - 1)));
       const __bf16* qrow = (const __bf16*)a.q + at.out * D;
 #pragma unroll
       for (int kk = 0; kk < kKK; ++kk) {
@@ -244,32 +279,32 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
         uint4 v = *(const uint4*)(qrow + (FP8 ? ((kk >> 1) * 2 + h2) * 16 + (kk & 1) * 8 : kk * 16 + h2 * 8));
         const uint32_t sign = flip ? 0x80008000u : 0u;
         v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign;
-        qop[c][kk] = __builtin_bit_cast(kx8, v);     // (int8: as it came, until all of the row is there)
+        qop[kk] = __builtin_bit_cast(kx8, v);     // (int8: as it came, until all of the row is there)
       }
-      q_unit[c] = scale_log2;
+      q_unit = scale_log2;
       if constexpr (INT8) {
         float top = 0.f;
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[c][kk]);
+          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) top = fmaxf(top, __builtin_fabsf((float)v[e]));
         }
         const int up = kQueryBits - __builtin_amdgcn_frexp_expf(xor32_max(top));
 #pragma unroll
         for (int kk = 0; kk < kKK; ++kk) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[c][kk]);
+          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) qop[c][kk][e] = (_Float16)__builtin_amdgcn_ldexpf((float)v[e], up);
+          for (int e = 0; e < 8; ++e) qop[kk][e] = (_Float16)__builtin_amdgcn_ldexpf((float)v[e], up);
         }
-        q_unit[c] = __builtin_amdgcn_ldexpf(scale_log2, -up);
+        q_unit = __builtin_amdgcn_ldexpf(scale_log2, -up);
       }
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[c][dt][i] = 0.f;
-      m_run[c] = -INFINITY;
-      l_run[c] = 0.f;
+        for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+      m_run = -INFINITY;
+      l_run = 0.f;
     }
     seg_first_blk = cc.blk;
     dirty = false;
@@ -278,16 +313,14 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     const bool whole = seg_first_blk == 0 && cc.blk == cc.n - 1;
     const size_t slot = (size_t)worker * 2 + (first_segment ? 0 : 1);
     const Draft d(a, cc.b);
-#pragma unroll
-    for (int c = 0; c < RT; ++c) {
-      if (c * kRows >= rows_here) break;
-      const float l_tot = xor32_add(l_run[c]);
+    if (rows_here > 0) {
+      const float l_tot = xor32_add(l_run);
       if (whole) {
         // the whole row was ours: normalise and store
-        const bool ok = c * kRows + n32 < rows_here;
-        const RowAt at(a, d, g, max(0, min(j0 + c * kRows + n32, d.n * group - 1)));
+        const bool ok = n32 < rows_here;
+        const RowAt at(a, d, g, max(0, min(j0 + n32, d.n * group - 1)));
         const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot;   // (nothing seen: a row of zeros)
-        if (a.lse && ok && h2 == 0) a.lse[at.out] = m_run[c] + __builtin_amdgcn_logf(l_tot);
+        if (a.lse && ok && h2 == 0) a.lse[at.out] = m_run + __builtin_amdgcn_logf(l_tot);
         __bf16* dst = (__bf16*)a.out + at.out * D + h2 * 4;
         if (ok) {
 #pragma unroll
@@ -296,25 +329,24 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
             for (int i4 = 0; i4 < 4; ++i4) {
               bf16x4 pk;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) pk[e] = (__bf16)(acc[c][dt][i4 * 4 + e] * inv);
+              for (int e = 0; e < 4; ++e) pk[e] = (__bf16)(acc[dt][i4 * 4 + e] * inv);
               *(bf16x4*)(dst + dt * 32 + i4 * 8) = pk;
             }
         }
       } else {
-        float* dst = a.partial_o + (slot * RT + c) * (kRows * D) + lane * 4;
+        float* dst = a.partial_o + (slot * W + wave) * (kRows * D) + lane * 4;
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
           for (int i4 = 0; i4 < 4; ++i4)
-            *(floatx4*)(dst + (dt * 4 + i4) * 256) = floatx4{acc[c][dt][i4 * 4], acc[c][dt][i4 * 4 + 1], acc[c][dt][i4 * 4 + 2], acc[c][dt][i4 * 4 + 3]};
-        if (h2 == 0) *(floatx2*)(a.partial_ml + ((slot * RT + c) * kRows + n32) * 2) = floatx2{m_run[c], l_tot};
+            *(floatx4*)(dst + (dt * 4 + i4) * 256) = floatx4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
+        if (h2 == 0) *(floatx2*)(a.partial_ml + ((slot * W + wave) * kRows + n32) * 2) = floatx2{m_run, l_tot};
       }
     }
     if (!INT8 && dirty) {
       // rare, and one token after the other: each lane adds to the values that it has just stored
-      for (int c = 0; c < RT; ++c) {
-        if (c * kRows + n32 >= rows_here) break;
-        const RowAt at(a, d, g, j0 + c * kRows + n32);
+      if (n32 < rows_here) {
+        const RowAt at(a, d, g, j0 + n32);
         const uint64_t* const words = a.mask + (size_t)(d.off + at.node) * a.mask_words;
         for (int t = max(prefix, seg_first_blk * kBlockTokens); t < min(d.len, (cc.blk + 1) * kBlockTokens); ++t) {
           const int rel = t - prefix;
@@ -341,7 +373,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
               for (int e = 0; e < 4; ++e) y[e] = (__bf16)((float)y[e] + x[e]);
               *o = y;
             } else {
-              floatx4* const o = (floatx4*)(a.partial_o + (slot * RT + c) * (kRows * D) + (dim / 8 * 64 + lane) * 4);
+              floatx4* const o = (floatx4*)(a.partial_o + (slot * W + wave) * (kRows * D) + (dim / 8 * 64 + lane) * 4);
               floatx4 y = *o;
 #pragma unroll
               for (int e = 0; e < 4; ++e) y[e] += x[e];
@@ -354,13 +386,11 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     first_segment = false;
   };
 
-  floatx16 s[RT];
+  floatx16 s;
   // ---- S^T = K Q^T
   auto scores = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < RT; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[c][i] = 0.f;
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
     const int t = (n32 & 16) + tau(n32 & 15);
     const unsigned char* rowp = lds.k[slot] + t * G_::kRowBytes;
     const int key = tree_key_k<D, FP8>(t);
@@ -369,23 +399,20 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       for (int p = 0; p < kKK / 2; ++p) {
         const uint4 raw = *(const uint4*)(rowp + ((p * 2 + h2) ^ key) * 16);
         const auto lo = widen_k8<KV>(raw.x, raw.y), hi = widen_k8<KV>(raw.z, raw.w);
-#pragma unroll
-        for (int c = 0; c < RT; ++c) s[c] = mfma32(lo, qop[c][2 * p], s[c]);
-#pragma unroll
-        for (int c = 0; c < RT; ++c) s[c] = mfma32(hi, qop[c][2 * p + 1], s[c]);
+s = mfma32(lo, qop[2 * p], s);
+s = mfma32(hi, qop[2 * p + 1], s);
       }
     } else {
 #pragma unroll
       for (int kk = 0; kk < kKK; ++kk) {
         const kx8 kop = *(const kx8*)(rowp + (((kk * 2 + h2) ^ key) & (G_::kChunks - 1)) * 16);
-#pragma unroll
-        for (int c = 0; c < RT; ++c) s[c] = mfma32(kop, qop[c][kk], s[c]);
+s = mfma32(kop, qop[kk], s);
       }
     }
   };
   // This lane then holds, for its rows, the scores of tokens tok0 + (i/8)*16 + h2*8 + i%8: eight of each page.
-  opx8 pop[RT][2];
-  unsigned int seen[RT];                             // bit i: of this lane's score i (set in the blocks behind the prefix alone)
+  opx8 pop[2];
+  unsigned int seen = 0;                             // bit i: of this lane's score i (set in the blocks behind the prefix alone)
   auto softmax = [&](bool edge, const float4& scales) __attribute__((always_inline)) {
     const int tok0 = cc.blk * kBlockTokens;
     float kscale[2] = {1.f, 1.f}, vscale[2] = {1.f, 1.f}, lvs[2] = {0.f, 0.f}, ivs[2] = {1.f, 1.f};
@@ -399,31 +426,30 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
         }
       }
     }
-#pragma unroll
-    for (int c = 0; c < RT; ++c) {
+    {
       float sc[2];
 #pragma unroll
-      for (int pg = 0; pg < 2; ++pg) sc[pg] = (INT8 ? q_unit[c] : scale_log2) * (FP8 ? kscale[pg] : 1.f);
+      for (int pg = 0; pg < 2; ++pg) sc[pg] = (INT8 ? q_unit : scale_log2) * (FP8 ? kscale[pg] : 1.f);
       if (edge) {
         // (faint queries over faint keys: a unit that has gone to zero would make a masked token's exponent undefined)
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) sc[pg] = fmaxf(sc[pg], 0x1p-126f);
-        const int j = max(0, min(j0 + c * kRows + n32, n_b * group - 1));
+        const int j = max(0, min(j0 + n32, n_b * group - 1));
         const uint64_t* words = a.mask + (size_t)(q_off + j / group) * a.mask_words;
-        seen[c] = 0;
+        seen = 0;
 #pragma unroll
-        for (int pg = 0; pg < 2; ++pg) seen[c] |= seen_bits(words, a.mask_words, tok0 + pg * kPageSize + h2 * 8 - prefix, n_b, 0xffu) << (8 * pg);
+        for (int pg = 0; pg < 2; ++pg) seen |= seen_bits(words, a.mask_words, tok0 + pg * kPageSize + h2 * 8 - prefix, n_b, 0xffu) << (8 * pg);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[c][i] = seen[c] >> i & 1 ? s[c][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[i] = seen >> i & 1 ? s[i] : -INFINITY;
       }
       float mx[2];
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
         const int o = pg * 8;
-        float x = fmaxf(fmaxf(s[c][o], s[c][o + 1]), s[c][o + 2]);
-        x = fmaxf(fmaxf(x, s[c][o + 3]), s[c][o + 4]);
-        x = fmaxf(fmaxf(x, s[c][o + 5]), s[c][o + 6]);
-        mx[pg] = fmaxf(x, s[c][o + 7]);
+        float x = fmaxf(fmaxf(s[o], s[o + 1]), s[o + 2]);
+        x = fmaxf(fmaxf(x, s[o + 3]), s[o + 4]);
+        x = fmaxf(fmaxf(x, s[o + 5]), s[o + 6]);
+        mx[pg] = fmaxf(x, s[o + 7]);
         mx[pg] = HEAD ? __builtin_fmaf(mx[pg], sc[pg], lvs[pg]) : mx[pg] * sc[pg];
       }
       float top = xor32_max(fmaxf(mx[0], mx[1]));
@@ -432,28 +458,28 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
         const float below = top - kWeightBits;
         top = top - below > kMostBits ? top : below;
       }
-      const float m_new = fmaxf(m_run[c], top);
+      const float m_new = fmaxf(m_run, top);
       const float base = m_new == -INFINITY ? 0.f : m_new;   // (a row that has seen nothing yet)
-      const float alpha = __builtin_amdgcn_exp2f(m_run[c] - base);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - base);
       float psum[2] = {0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int pg = i >> 3;
         float x;
-        if constexpr (HEAD) x = __builtin_fmaf(s[c][i], sc[pg], lvs[pg]) - base;
-        else x = __builtin_fmaf(s[c][i], sc[pg], -base);
+        if constexpr (HEAD) x = __builtin_fmaf(s[i], sc[pg], lvs[pg]) - base;
+        else x = __builtin_fmaf(s[i], sc[pg], -base);
         const float p = __builtin_amdgcn_exp2f(x);
         psum[pg] += p;
-        pop[c][pg][i & 7] = (op)(FP8 && !HEAD ? p * vscale[pg] : p);
+        pop[pg][i & 7] = (op)(FP8 && !HEAD ? p * vscale[pg] : p);
       }
-      l_run[c] = l_run[c] * alpha + (HEAD ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1]);
-      if (__builtin_amdgcn_ballot_w64(m_new > m_run[c])) {
+      l_run = l_run * alpha + (HEAD ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1]);
+      if (__builtin_amdgcn_ballot_w64(m_new > m_run)) {
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[c][dt][i] *= alpha;
+          for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
       }
-      m_run[c] = m_new;
+      m_run = m_new;
     }
   };
   // ---- O^T += V^T P^T : A = V^T tile (32 dims x 16 tokens) read transposed from LDS
@@ -484,8 +510,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) {
         const opx8 v = v_operand(slot, ks, dt);
-#pragma unroll
-        for (int c = 0; c < RT; ++c) acc[c][dt] = mfma32(v, pop[c][ks], acc[c][dt]);
+acc[dt] = mfma32(v, pop[ks], acc[dt]);
       }
   };
   // Whether the values of a block hold any that is no number: then zeros take their places in front of the second product, and those of
@@ -508,48 +533,92 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     }
   };
 
-  for (int i = 0; i < min(kSlots, n_mine); ++i) {
-    issue_k(i);
-    issue_v(i);
-  }
-  int slot = 0;
-  for (int i = 0; i < n_mine; ++i) {
-    if (i == 0 || cc.blk == 0) begin_segment();
-    const bool edge = (cc.blk + 1) * kBlockTokens > prefix, more = i + kSlots < n_mine;
-    const int behind = min(kSlots - 1, n_mine - 1 - i);      // blocks behind this one that are under way
-    await(behind, std::integral_constant<int, G_::kLoads>{});
-    scores(slot);
-    float4 kept_scales = {};
-    if constexpr (FP8) kept_scales = *(const float4*)lds.scales[slot];
-    if (more) {
-      issue_k(slot);
-      await(behind, std::integral_constant<int, kKLoads>{});
-    } else {
-      await(behind, std::integral_constant<int, 0>{});
-    }
-    softmax(edge, kept_scales);
-    if (!INT8 && edge && any_undefined(slot)) {
-      without_undefined(slot);
-      dirty = true;
+  // the block in `slot`, from its scores on
+  auto consume = [&](int i, int slot, bool edge, const float4& scales) __attribute__((always_inline)) {
+    softmax(edge, scales);
+    if constexpr (!INT8 && W == 1) {
+      if (edge && any_undefined(slot)) {
+        without_undefined(slot);
+        dirty = true;
+      }
     }
     values(slot);
-    if (more) issue_v(slot);
-    if (cc.blk == cc.n - 1 || i == n_mine - 1) end_segment();
-    if (i + 1 < n_mine) advance(cc);
-    slot = slot + 1 == kSlots ? 0 : slot + 1;
+  };
+  int slot = 0;
+  auto scales_of = [&](int slot) __attribute__((always_inline)) { return FP8 ? *(const float4*)lds.scales[slot][wave] : make_float4(1.f, 1.f, 1.f, 1.f); };
+  if constexpr (W == 1) {
+    for (int i = 0; i < min(kSlots, n_mine); ++i) {
+      issue_k(i);
+      issue_v(i);
+    }
+    for (int i = 0; i < n_mine; ++i) {
+      if (i == 0 || cc.blk == 0) begin_segment();
+      const bool edge = (cc.blk + 1) * kBlockTokens > prefix, more = i + kSlots < n_mine;
+      const int behind = min(kSlots - 1, n_mine - 1 - i);      // blocks behind this one that are under way
+      await(behind, std::integral_constant<int, kVLoads>{});
+      scores(slot);
+      const float4 scales = scales_of(slot);
+      if (more) {
+        all_read();
+        issue_k(slot);
+        await(behind, std::integral_constant<int, kKLoads>{});
+      } else {
+        await(behind, std::integral_constant<int, 0>{});
+      }
+      consume(i, slot, edge, scales);
+      if (more) {
+        all_read();
+        issue_v(slot);
+      }
+      if (cc.blk == cc.n - 1 || i == n_mine - 1) end_segment();
+      if (i + 1 < n_mine) advance(cc);
+      slot = slot + 1 == kSlots ? 0 : slot + 1;
+    }
+  } else {
+    for (int i = 0; i < min(kSlots - 1, n_mine); ++i) issue(i);
+    for (int i = 0; i < n_mine; ++i) {
+      if (i == 0 || cc.blk == 0) begin_segment();
+      const bool edge = (cc.blk + 1) * kBlockTokens > prefix;
+      await(min(kSlots - 2, n_mine - 1 - i), std::integral_constant<int, 0>{});
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (i + kSlots - 1 < n_mine) issue(slot == 0 ? kSlots - 1 : slot - 1);
+      if constexpr (!INT8) {
+        // (the ones that are told apart: every wave looks at all of the tile, and none reads it until all have put zeros into it)
+        if (edge && any_undefined(slot)) {
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          without_undefined(slot);
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          dirty = true;
+        }
+      }
+      if (rows_here > 0) {
+        scores(slot);
+        consume(i, slot, edge, scales_of(slot));
+      }
+      if (cc.blk == cc.n - 1 || i == n_mine - 1) end_segment();
+      if (i + 1 < n_mine) advance(cc);
+      slot = slot + 1 == kSlots ? 0 : slot + 1;
+    }
   }
 }
 
-// The start of a worker's run, for a batch of at most 64 trajectories: worked out by every wave for itself, a lane per trajectory (the rule
-// is plan_decode's).  The first worker writes the header and the scan, which the merge reads.
+// The partition: as plan_decode's, with hkv * tiles rows of a trajectory, of its own number of tiles.  Blocks of b before all heads:
+// prefix[b], in units of its KV heads.
+__device__ __forceinline__ int tree_blocks(const TreeArgs& a, int b, int& per_row) {
+  const int tiles = tree_tiles(a, a.q_lens[b]);
+  per_row = tiles ? (a.ctx_lens[b] + kBlockTokens - 1) / kBlockTokens : 0;
+  return tiles * per_row;
+}
+
+// The start of a worker's run, for a batch of at most 64 trajectories: worked out by every wave for itself, a lane per trajectory.  The first
+// worker writes the header and the scan, which the merge reads.
 __device__ __forceinline__ int4 tree_plan_in_wave(const TreeArgs& a, int worker) {
-  const int lane = lane_id(), rows_per_b = a.hkv * a.row_tiles;
-  int len = 0;
-  if (lane < a.batch) len = a.q_lens[lane] > 0 ? a.ctx_lens[lane] : 0;
-  const int count = (len + kBlockTokens - 1) / kBlockTokens;
+  const int lane = lane_id(), hkv = a.hkv;
+  int per_row = 0, count = 0;
+  if (lane < a.batch) count = tree_blocks(a, lane, per_row);
   const int upto = wave_inclusive_scan(count), first = upto - count;
   const int blocks = __builtin_amdgcn_readlane(upto, 63);
-  const int total = blocks * rows_per_b;
+  const int total = blocks * hkv;
   const int per = max(1, (total + a.workers - 1) / a.workers);
   const unsigned int x = (unsigned int)worker * (unsigned int)per;
   if (worker == 0) {
@@ -560,46 +629,90 @@ __device__ __forceinline__ int4 tree_plan_in_wave(const TreeArgs& a, int worker)
     }
   }
   if (x >= (unsigned int)total) return make_int4(-1, 0, 0, 0);
-  const unsigned long long before = __builtin_amdgcn_ballot_w64(lane < a.batch && (unsigned int)(rows_per_b * first) <= x);
+  const unsigned long long before = __builtin_amdgcn_ballot_w64(lane < a.batch && (unsigned int)(hkv * first) <= x);
   const int b = 63 - __builtin_clzll(before);
-  const int n = __builtin_amdgcn_readlane(count, b);
-  const int rem = (int)x - rows_per_b * __builtin_amdgcn_readlane(first, b);
+  const int n = __builtin_amdgcn_readlane(per_row, b);
+  const int rem = (int)x - hkv * __builtin_amdgcn_readlane(first, b);
   return make_int4(b, ((rem / n) << 20) | (rem % n), 0, min(per, total - (int)x));
 }
 
-template <int D, int KV, int RT>
-__global__ __launch_bounds__(kThreads, RT == 2 ? 1 : 2) void tree_mfma_kernel(const TreeArgs a) {
-  __shared__ TreeLds<D, kv_is_codes(KV), RT> lds[kWaves];
+// Workgroups go to the XCDs in turn; workers that follow each other, whose rows may read the same K and V, have one XCD's cache in common.
+template <int D, int KV, int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 2) void tree_mfma_kernel(const TreeArgs a) {
+  constexpr int kWorkers = W == 1 ? 4 : 1;       // of a workgroup
+  __shared__ TreeLds<D, kv_is_codes(KV), W> lds[kWorkers];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int worker = blockIdx.x * kWaves + wave;
+  const int group = (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds);
+  const int worker = group * kWorkers + (W == 1 ? wave : 0);
   int4 start;
   if (a.batch <= kWavePlanBatch) start = tree_plan_in_wave(a, worker);
   else start = *(const int4*)(a.wstart + 4 * worker);
   const int b = __builtin_amdgcn_readfirstlane(start.x), at = __builtin_amdgcn_readfirstlane(start.y), mine = __builtin_amdgcn_readfirstlane(start.w);
   if (b < 0) return;
-  tree_worker<D, KV, RT, false>(a, b, at >> 20, at & 0xFFFFF, mine, worker, lds[wave]);
+  tree_worker<D, KV, W, false>(a, b, at >> 20, at & 0xFFFFF, mine, worker, W == 1 ? 0 : wave, lds[W == 1 ? wave : 0]);
 }
 
-__global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(const DecodePlanArgs p) {
-  __shared__ DecodePlanLds lds;
-  plan_decode(p, lds, [&](int b) { return p.q_lens[b] > 0 ? p.ctx_lens[b] : 0; });
+__global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(const TreeArgs a) {
+  __shared__ int4 wave_tot[kPlanThreads / 256];
+  __shared__ int prefix_s[kLdsPrefix + 1];
+  const int tid = threadIdx.x, batch = a.batch, hkv = a.hkv;
+  const bool in_lds = batch <= kLdsPrefix;
+  int running = 0;
+  for (int b0 = 0; b0 < batch; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    int per_row, all;
+    const int count = b < batch ? tree_blocks(a, b, per_row) : 0;
+    const int first = running + block_exclusive_scan(count, wave_tot, &all);
+    if (b < batch) {
+      a.prefix[b] = first;
+      if (in_lds) prefix_s[b] = first;
+    }
+    running += all;
+  }
+  if (tid == 0) {
+    a.prefix[batch] = running;
+    if (in_lds) prefix_s[batch] = running;
+  }
+  const int total = running * hkv, per = max(1, (total + a.workers - 1) / a.workers);
+  if (tid == 0) a.header[kPlanPer] = per;
+  __threadfence_block();
+  __syncthreads();   // prefix[] written above is read below by other threads of this workgroup
+  for (int w = tid; w < a.workers; w += kPlanThreads) {
+    const long x = (long)w * per;
+    int4 st = make_int4(-1, 0, 0, 0);
+    if (x < total) {
+      // largest b whose rows start at or before x (trajectories without blocks can never be the answer: the next one starts at the same place)
+      const int* pf = in_lds ? prefix_s : a.prefix;
+      int lo = 0, hi = batch;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((long)hkv * pf[mid] <= x) lo = mid; else hi = mid;
+      }
+      int n;
+      tree_blocks(a, lo, n);
+      const int rem = (int)(x - (long)hkv * pf[lo]);
+      st = make_int4(lo, ((rem / n) << 20) | (rem % n), 0, (int)min((long)per, (long)total - x));
+    }
+    *(int4*)(a.wstart + 4 * w) = st;
+  }
 }
 
 // Merge of the partials that runs left of rows they did not cover alone, as in combine.hip: one wave per (row, 32 query rows, 32 dims),
 // lanes as in the accumulators, four pieces under way at a time.  A piece of which a query row saw nothing has weight zero.
-template <int D, int RT>
+template <int D>
 __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) {
   constexpr int kDT = D / 32;
-  const int lane = lane_id(), n32 = lane & 31, h2 = lane >> 5;
+  const int lane = lane_id(), n32 = lane & 31, h2 = lane >> 5, parts = a.tile_parts;
   const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + (threadIdx.x >> 6)));
-  const int dt = unit % kDT, c = unit / kDT % RT, row = unit / (kDT * RT), rows_per_b = a.hkv * a.row_tiles;
-  const int b = row / rows_per_b, r = row - b * rows_per_b;
+  const int dt = unit % kDT, part0 = unit / kDT, most = a.row_tiles * parts;   // (of the longest draft: 32 query rows each)
+  const int row = part0 / most, p = part0 - row * most, tile = p / parts, c = p - tile * parts, b = row / a.hkv, g = row - b * a.hkv;
   if (b >= a.batch) return;
-  const int per = a.header[kPlanPer], first = a.prefix[b], n = a.prefix[b + 1] - first;
+  const int per = a.header[kPlanPer], first = a.prefix[b], all = a.prefix[b + 1] - first;
   const Draft d(a, b);
-  const int g = r / a.row_tiles, j0 = (r - g * a.row_tiles) * (kRows * RT) + c * kRows;
-  if (n == 0 || j0 >= d.n * a.group) return;
-  const long r0 = (long)rows_per_b * first + (long)r * n;
+  const int j0 = p * kRows, tiles = tree_tiles(a, d.n);
+  if (all == 0 || j0 >= d.n * a.group) return;
+  const int n = all / tiles, r = g * tiles + tile;
+  const long r0 = (long)a.hkv * first + (long)r * n;
   const int wf = (int)(r0 / per), wl = (int)((r0 + n - 1) / per), pieces = wl - wf + 1;
   if (pieces == 1) return;                                  // one worker had the whole row
   const int first_slot = ((long)wf * per < r0) ? 1 : 0;
@@ -615,7 +728,7 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) 
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int s = min(s0 + i, pieces - 1);
-      const size_t part = ((size_t)(wf + s) * 2 + (s == 0 ? first_slot : 0)) * RT + c;
+      const size_t part = ((size_t)(wf + s) * 2 + (s == 0 ? first_slot : 0)) * parts + c;
       x[i] = *(const floatx2*)(a.partial_ml + (part * kRows + n32) * 2);
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = *(const floatx4*)(a.partial_o + part * (kRows * D) + ((dt * 4 + i4) * 64 + lane) * 4);
@@ -662,25 +775,29 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) 
 
 hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, hipStream_t s) {
   if (a.batch > kWavePlanBatch) {
-    DecodePlanArgs p{};
-    p.ctx_lens = a.ctx_lens; p.q_lens = a.q_lens; p.batch = a.batch; p.rows_per_b = a.hkv * a.row_tiles;
-    p.workers = p.slots = a.workers;
-    p.header = a.header; p.prefix = a.prefix; p.wstart = a.wstart;
-    hipLaunchKernelGGL(tree_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+    hipLaunchKernelGGL(tree_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const dim3 grid((unsigned)(a.workers / kWaves));
   const int64_t units = (int64_t)a.batch * a.hkv * a.row_tiles * a.tile_parts * (head_dim / 32);
   const dim3 merge_grid((unsigned)((units + kWaves - 1) / kWaves));
-  auto launch = [&](auto d, auto kind, auto c) {
-    hipLaunchKernelGGL((tree_mfma_kernel<decltype(d)::value, decltype(kind)::value, decltype(c)::value>), grid, dim3(kThreads), 0, s, a);
+  auto launch = [&](auto d, auto kind, auto w) {
+    constexpr int W = decltype(w)::value;
+    hipLaunchKernelGGL((tree_mfma_kernel<decltype(d)::value, decltype(kind)::value, W>), dim3(a.workers / (W == 1 ? 4 : 1)), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((tree_merge_kernel<decltype(d)::value, decltype(c)::value>), merge_grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((tree_merge_kernel<decltype(d)::value>), merge_grid, dim3(kThreads), 0, s, a);
     return hipGetLastError();
   };
-  auto of_tiles = [&](auto d, auto kind) { return a.tile_parts == 1 ? launch(d, kind, std::integral_constant<int, 1>{}) : launch(d, kind, std::integral_constant<int, 2>{}); };
+  auto of_tiles = [&](auto d, auto kind) {
+    switch (a.tile_parts) {
+      case 1: return launch(d, kind, std::integral_constant<int, 1>{});
+      case 2: return launch(d, kind, std::integral_constant<int, 2>{});
+      case 4: return launch(d, kind, std::integral_constant<int, 4>{});
+      case 8: return launch(d, kind, std::integral_constant<int, 8>{});
+    }
+    return hipErrorInvalidValue;
+  };
   auto of_kind = [&](auto kind) {
     return head_dim == 128 ? of_tiles(std::integral_constant<int, 128>{}, kind) : of_tiles(std::integral_constant<int, 64>{}, kind);
   };
