@@ -20,10 +20,14 @@ namespace rollattn {
 namespace {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef unsigned int uint4_v __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;             // of the merge
 constexpr int kWaves = kThreads / 64;
 constexpr int kRows = kTreeTileRows;      // query rows of a wave
+constexpr float kSumLimit = 16384.f;      // see the softmax
+constexpr float kHalfSumLimit = 65000.f;
+constexpr float kTreeWeightBits = 8.f;    // f16 weights: log2 of a row's largest when its reference moves
 
 __device__ __forceinline__ floatx16 mfma32(bf16x8 x, bf16x8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
 __device__ __forceinline__ floatx16 mfma32(halfx8 x, halfx8 y, floatx16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
@@ -57,25 +61,19 @@ __device__ __forceinline__ unsigned int seen_bits(const uint64_t* words, int n_w
   return x & 0xff;
 }
 
-// Whether any element of a word of a pool is no number (infinite and undefined bf16 values, the undefined code of E4M3).
+// The sign bits of the elements of a word of a pool that are no numbers (infinite and undefined bf16 values, whose exponent is all ones; the
+// undefined code of E4M3): the sum carries into them.
 template <int KV>
-__device__ __forceinline__ bool undefined(uint32_t w) {
-  if constexpr (KV == kKvBf16) return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u;
-  else if constexpr (KV == kKvInt8Head) return false;
-  else return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+__device__ __forceinline__ uint32_t undefined(uint32_t w) {
+  if constexpr (KV == kKvBf16) return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  else if constexpr (KV == kKvInt8Head) return 0;
+  else return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
 }
-
 // The word with zeros in the place of those.
 template <int KV>
 __device__ __forceinline__ uint32_t defined(uint32_t w) {
-  if constexpr (KV == kKvBf16) {
-    if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
-    if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
-    return w;
-  } else {
-    const uint32_t met = (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;   // one in each undefined byte
-    return w & ~(met * 255u);
-  }
+  const uint32_t met = undefined<KV>(w) >> (KV == kKvBf16 ? 15 : 7);
+  return w & ~(met * (KV == kKvBf16 ? 0xffffu : 0xffu));
 }
 
 // The lengths of one trajectory, the same in all lanes.
@@ -99,14 +97,18 @@ struct RowAt {
   }
 };
 
-// A worker's ring: its blocks, the one in work included, so that two waves to a SIMD find their LDS.
+// A worker's ring: its blocks, the one in work included, so that two waves to a SIMD find their LDS.  Addresses are 32-bit offsets in the LDS.
 template <int D, bool FP8, int W>
 struct TreeLds {
-  typedef Geo<D, FP8> G_;
   static constexpr int kSlots = W == 1 ? (FP8 ? 2 : 1) : W == 2 ? (FP8 ? 4 : 2) : 4;
-  __attribute__((aligned(1024))) unsigned char k[kSlots][G_::kTileBytes], v[kSlots][G_::kTileBytes];
-  float scales[FP8 ? kSlots : 1][W][FP8 ? 64 : 4];   // of a block's two pages: K's, V's (the other lanes' are copies), for each wave
+  static constexpr int kTile = Geo<D, FP8>::kTileBytes, kScales = FP8 ? 256 : 0;   // scales of a block's two pages: K's, V's (the other lanes' are copies)
+  static constexpr int kBytes = kSlots * (2 * kTile + W * kScales);
+  static __device__ __forceinline__ unsigned int k(int slot) { return slot * kTile; }
+  static __device__ __forceinline__ unsigned int v(int slot) { return (kSlots + slot) * kTile; }
+  static __device__ __forceinline__ unsigned int scales(int slot, int wave) { return 2 * kSlots * kTile + (slot * W + wave) * kScales; }
 };
+template <class T>
+__device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(unsigned int at) { return (__attribute__((address_space(3))) T*)(uintptr_t)at; }
 
 // One run of n_mine blocks from block blk of row (b, r) on.
 // Loads.  W = 1: the tiles of block i + slots go into the places of block i, K's as soon as the first product has read them and V's behind
@@ -117,10 +119,11 @@ struct TreeLds {
 // with N of these loads sent after the ones that are waited for, no more than N outstanding operations of any kind means that those have
 // landed (others in between only make the wait longer).
 template <int D, int KV, int W, bool STREAM>
-__device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, int blk0, int n_mine, int worker, int wave, TreeLds<D, kv_is_codes(KV), W>& lds) {
+__device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, int blk0, int n_mine, int worker, int wave, unsigned int lds) {
   constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
   constexpr bool INT8 = KV == kKvInt8Head;
   constexpr int kTile = kRows * W, kSlots = TreeLds<D, FP8, W>::kSlots;
+  using L_ = TreeLds<D, FP8, W>;
   constexpr int kKK = D / 16, kDT = D / 32;
   using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
   using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;  // ... and of the second
@@ -139,21 +142,26 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   const bool flip = a.scale_log2 < 0.f;                           // (queries the other way round, so that larger scores are larger exponents)
   const float scale_log2 = __builtin_fabsf(a.scale_log2);
 
-  struct Cursor { int b, r, blk, n, len, tiles; };   // trajectory, row within it, block within the row; blocks in the row, context length, tiles per KV head
+  // trajectory, KV head, tile and block within the row; blocks in the row, context length, tiles per KV head
+  struct Cursor { int b, g, tile, blk, n, len, tiles; };
   auto enter = [&](Cursor& c) {
     const Draft d(a, c.b);
     c.tiles = tree_tiles(a, d.n);
     c.len = c.tiles ? d.len : 0;
     c.n = (c.len + kBlockTokens - 1) / kBlockTokens;
   };
-  Cursor pc{b0, r0, blk0, 0, 0, 0};           // producer: next block to request from HBM
+  Cursor pc{b0, 0, 0, blk0, 0, 0, 0};         // producer: next block to request from HBM
   enter(pc);
+  pc.g = r0 / pc.tiles;
+  pc.tile = r0 - pc.g * pc.tiles;
   Cursor cc = pc;                             // consumer: block being computed
   auto advance = [&](Cursor& c) {             // (whether it is another row now)
     if (++c.blk < c.n) return false;
     c.blk = 0;
-    if (++c.r < hkv * c.tiles) return true;
-    c.r = 0;
+    if (++c.tile < c.tiles) return true;
+    c.tile = 0;
+    if (++c.g < hkv) return true;
+    c.g = 0;
     do {
       ++c.b;
       enter(c);
@@ -168,31 +176,41 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     const int pg = k * 64 + lane;
     return (pg < ((pc.len + kPageSize - 1) >> 4)) ? a.page_table[(size_t)pc.b * a.max_pages + pg] : 0;
   };
-  auto dma16 = [&](const unsigned char* base, unsigned int off, const void* dst) __attribute__((always_inline)) {
-    const unsigned int m0 = __builtin_amdgcn_readfirstlane((unsigned int)(uintptr_t)dst);
+  auto dma16 = [&](const unsigned char* base, unsigned int off, unsigned int dst) __attribute__((always_inline)) {
+    const unsigned int m0 = __builtin_amdgcn_readfirstlane(dst);
     if constexpr (STREAM) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(m0), "v"(off), "s"(base) : "memory");
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(base) : "memory");
   };
-  // this wave's share of a tile of one pool: row row0 + lane / chunks of the block per load; rows at or past L_b read its last one again
-  auto load_tile = [&](const void* pool, int first, auto count_c, auto key_of, unsigned char* dst) __attribute__((always_inline)) {
-    const int c = lane % G_::kChunks, sub = lane / G_::kChunks;
+  // This wave's share of a tile of one pool: row row0 + lane / chunks of the block per load.  What a lane reads of a tile is the same for every
+  // whole block; of a row's ragged last one, rows at or past L_b read its last one again.
+  const bool for_v = kVLoads == 0 && wave % (2 * G_::kLoads) >= G_::kLoads;       // (one pool's tile alone, and that is V's)
+  const int first = G_::kLoads >= W ? wave : wave % G_::kLoads;
+  auto key_of = [&](auto v_c, int row) __attribute__((always_inline)) { return decltype(v_c)::value ? tree_key_v<FP8>(row) : tree_key_k<D, FP8>(row); };
+  auto offset = [&](auto v_c, int i, int lim) __attribute__((always_inline)) {
+    const int row = (first + i * W) * G_::kRowsPerLoad + lane / G_::kChunks;
+    return min(row, lim - 1) % kPageSize * G_::kRowBytes + (((lane % G_::kChunks) ^ key_of(v_c, row)) & (G_::kChunks - 1)) * 16;
+  };
+  unsigned int off_k[kShare], off_v[kShare];
 #pragma unroll
-    for (int i = 0; i < decltype(count_c)::value; ++i) {
-      const int j = first + i * W, row0 = j * G_::kRowsPerLoad, row = row0 + sub;
-      const int page = row0 < kPageSize ? p_page[0] : p_page[1];
-      const unsigned char* tile = (const unsigned char*)pool + (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(page * hkv + p_g) * tile_stride;
-      int slot = row % kPageSize;
-      if (p_lim < kBlockTokens) slot = min(row, p_lim - 1) % kPageSize;      // (the row's last block alone)
-      dma16(tile, slot * G_::kRowBytes + ((c ^ key_of(row)) & (G_::kChunks - 1)) * 16, dst + j * 1024);
+  for (int i = 0; i < kShare; ++i) {
+    off_k[i] = offset(std::false_type{}, i, kBlockTokens);
+    off_v[i] = offset(std::true_type{}, i, kBlockTokens);
+  }
+  auto load_tile = [&](auto v_c, int slot) __attribute__((always_inline)) {
+    constexpr bool V = decltype(v_c)::value;
+    size_t at[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) at[i] = (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(p_page[i] * hkv + p_g) * tile_stride;
+#pragma unroll
+    for (int i = 0; i < kShare; ++i) {
+      const int j = first + i * W;
+      const unsigned char* tile = (const unsigned char*)(V ? a.v_pages : a.k_pages) + (j * G_::kRowsPerLoad < kPageSize ? at[0] : at[1]);
+      const unsigned int off = p_lim == kBlockTokens ? (V ? off_v[i] : off_k[i]) : offset(v_c, i, p_lim);
+      dma16(tile, off, lds + (V ? L_::v(slot) : L_::k(slot)) + j * 1024);
     }
   };
-  constexpr std::integral_constant<int, kShare> share_c{};
-  auto load_k = [&](int slot, int first) __attribute__((always_inline)) {
-    load_tile(a.k_pages, first, share_c, [](int row) { return tree_key_k<D, FP8>(row); }, lds.k[slot]);
-  };
-  auto load_v = [&](int slot, int first) __attribute__((always_inline)) {
-    load_tile(a.v_pages, first, share_c, [](int row) { return tree_key_v<FP8>(row); }, lds.v[slot]);
-  };
+  auto load_k = [&](int slot) __attribute__((always_inline)) { load_tile(std::false_type{}, slot); };
+  auto load_v = [&](int slot) __attribute__((always_inline)) { load_tile(std::true_type{}, slot); };
   // what block pc of the run needs
   auto look_up = [&]() __attribute__((always_inline)) {
     const int k = pc.blk >> 5;
@@ -201,7 +219,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       pid_next = load_window(k + 1);
       pwin = k;
     }
-    p_g = pc.r / pc.tiles;
+    p_g = pc.g;
     p_lim = min(pc.len - pc.blk * kBlockTokens, kBlockTokens);
     p_page[0] = __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1));
     p_page[1] = p_lim > kPageSize ? __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1) + 1) : p_page[0];
@@ -210,7 +228,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     if constexpr (FP8) {
       const int page = lane & 1 ? p_page[1] : p_page[0];
       const float* from = (lane & 2 ? a.v_scale : a.k_scale) + (HEAD ? (size_t)page * hkv + p_g : (size_t)page);
-      const unsigned int m0 = __builtin_amdgcn_readfirstlane((unsigned int)(uintptr_t)lds.scales[slot][wave]);
+      const unsigned int m0 = __builtin_amdgcn_readfirstlane(lds + L_::scales(slot, wave));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(from) : "memory");
     }
   };
@@ -223,22 +241,22 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   auto all_read = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
   auto issue_k = [&](int slot) __attribute__((always_inline)) {      // W = 1: K and scales, then V
     look_up();
-    load_k(slot, 0);
+    load_k(slot);
     load_scales(slot);
   };
   auto issue_v = [&](int slot) __attribute__((always_inline)) {
-    load_v(slot, 0);
+    load_v(slot);
     step();
   };
   auto issue = [&](int slot) __attribute__((always_inline)) {
     look_up();
     if constexpr (kVLoads > 0) {
-      load_k(slot, wave);
-      load_v(slot, wave);
-    } else if (wave % (2 * G_::kLoads) < G_::kLoads) {
-      load_k(slot, wave % G_::kLoads);
+      load_k(slot);
+      load_v(slot);
+    } else if (for_v) {
+      load_v(slot);
     } else {
-      load_v(slot, wave % G_::kLoads);
+      load_k(slot);
     }
     load_scales(slot);
     step();
@@ -256,15 +274,16 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   kx8 qop[kKK];              // Q^T as the B operand: lane (row n32, half h2), 8 dims per step
   float q_unit = 0.f;        // int8: what a unit of this lane's row is worth
   floatx16 acc[kDT];        // O^T: lane (row n32, half h2) holds dims dt*32 + (i/4)*8 + h2*4 + i%4
-  float m_run = 0.f, l_run = 0.f;   // running max (log2 units) of this lane's rows, its share of the running sums
+  float m_ref = 0.f, l_run = 0.f;   // reference of this lane's row (log2 units), zero as long as it has seen nothing; its share of the running sum
+  float sum_limit = -1.f;           // a lane's exponentials of a block may add up to this much; below zero: no reference yet
   int seg_first_blk = 0;     // block of the row at which the current segment started
   bool first_segment = true, dirty = false;   // dirty: values of the segment that are no numbers have been left out of its sums
   int rows_here = 0, prefix = 0, n_b = 0, q_off = 0, j0 = 0, g = 0;   // of the consumer's row
 
   auto begin_segment = [&]() __attribute__((always_inline)) {
     const Draft d(a, cc.b);
-    g = cc.r / cc.tiles;
-    j0 = (cc.r - g * cc.tiles) * kTile + wave * kRows;
+    g = cc.g;
+    j0 = cc.tile * kTile + wave * kRows;
     n_b = d.n;
     q_off = d.off;
     prefix = d.len - d.n;
@@ -303,8 +322,8 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
-      m_run = -INFINITY;
-      l_run = 0.f;
+      m_ref = l_run = 0.f;
+      sum_limit = -1.f;
     }
     seg_first_blk = cc.blk;
     dirty = false;
@@ -314,7 +333,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     const size_t slot = (size_t)worker * 2 + (first_segment ? 0 : 1);
     const Draft d(a, cc.b);
     if (rows_here > 0) {
-      const float l_tot = xor32_add(l_run);
+      const float l_tot = xor32_add(l_run), m_run = sum_limit < 0.f ? -INFINITY : m_ref;
       if (whole) {
         // the whole row was ours: normalise and store
         const bool ok = n32 < rows_here;
@@ -392,32 +411,36 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
     const int t = (n32 & 16) + tau(n32 & 15);
-    const unsigned char* rowp = lds.k[slot] + t * G_::kRowBytes;
+    const unsigned int rowp = lds + L_::k(slot) + t * G_::kRowBytes;
     const int key = tree_key_k<D, FP8>(t);
+    // (all operands on their way before the first product: the products hang together and would each wait for a trip to the LDS)
     if constexpr (FP8) {
+      uint4_v raw[kKK / 2];
+#pragma unroll
+      for (int p = 0; p < kKK / 2; ++p) raw[p] = *lds_at<const uint4_v>(rowp + ((p * 2 + h2) ^ key) * 16);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int p = 0; p < kKK / 2; ++p) {
-        const uint4 raw = *(const uint4*)(rowp + ((p * 2 + h2) ^ key) * 16);
-        const auto lo = widen_k8<KV>(raw.x, raw.y), hi = widen_k8<KV>(raw.z, raw.w);
-s = mfma32(lo, qop[2 * p], s);
-s = mfma32(hi, qop[2 * p + 1], s);
+        s = mfma32(widen_k8<KV>(raw[p][0], raw[p][1]), qop[2 * p], s);
+        s = mfma32(widen_k8<KV>(raw[p][2], raw[p][3]), qop[2 * p + 1], s);
       }
     } else {
+      kx8 kop[kKK];
 #pragma unroll
-      for (int kk = 0; kk < kKK; ++kk) {
-        const kx8 kop = *(const kx8*)(rowp + (((kk * 2 + h2) ^ key) & (G_::kChunks - 1)) * 16);
-s = mfma32(kop, qop[kk], s);
-      }
+      for (int kk = 0; kk < kKK; ++kk) kop[kk] = *lds_at<const kx8>(rowp + (((kk * 2 + h2) ^ key) & (G_::kChunks - 1)) * 16);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kk = 0; kk < kKK; ++kk) s = mfma32(kop[kk], qop[kk], s);
     }
   };
   // This lane then holds, for its rows, the scores of tokens tok0 + (i/8)*16 + h2*8 + i%8: eight of each page.
   opx8 pop[2];
   unsigned int seen = 0;                             // bit i: of this lane's score i (set in the blocks behind the prefix alone)
-  auto softmax = [&](bool edge, const float4& scales) __attribute__((always_inline)) {
+  auto softmax = [&](bool edge, const floatx4& scales) __attribute__((always_inline)) {
     const int tok0 = cc.blk * kBlockTokens;
     float kscale[2] = {1.f, 1.f}, vscale[2] = {1.f, 1.f}, lvs[2] = {0.f, 0.f}, ivs[2] = {1.f, 1.f};
     if constexpr (FP8) {
-      kscale[0] = scales.x; kscale[1] = scales.y; vscale[0] = scales.z; vscale[1] = scales.w;
+      kscale[0] = scales[0]; kscale[1] = scales[1]; vscale[0] = scales[2]; vscale[1] = scales[3];
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
         if constexpr (HEAD) {
@@ -442,110 +465,120 @@ s = mfma32(kop, qop[kk], s);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = seen >> i & 1 ? s[i] : -INFINITY;
       }
-      float mx[2];
+      // The reference of a row only moves when it has to: exponentials are taken against it as it stands, and may exceed one.  Only when
+      // a lane's add up to more than kSumLimit (f16 weights: a page's to kHalfSumLimit, so that none is too large for f16), or while a row has no
+      // reference, are the maxima found, the references moved there and the block's exponentials taken again.
+      float psum[2], p[16];
+      auto exponentials = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int pg = 0; pg < 2; ++pg) {
-        const int o = pg * 8;
-        float x = fmaxf(fmaxf(s[o], s[o + 1]), s[o + 2]);
-        x = fmaxf(fmaxf(x, s[o + 3]), s[o + 4]);
-        x = fmaxf(fmaxf(x, s[o + 5]), s[o + 6]);
-        mx[pg] = fmaxf(x, s[o + 7]);
-        mx[pg] = HEAD ? __builtin_fmaf(mx[pg], sc[pg], lvs[pg]) : mx[pg] * sc[pg];
-      }
-      float top = xor32_max(fmaxf(mx[0], mx[1]));
-      if constexpr (HEAD) {
-        // (of a score past 2^25 the difference may come out larger, more than f16 holds)
-        const float below = top - kWeightBits;
-        top = top - below > kMostBits ? top : below;
-      }
-      const float m_new = fmaxf(m_run, top);
-      const float base = m_new == -INFINITY ? 0.f : m_new;   // (a row that has seen nothing yet)
-      const float alpha = __builtin_amdgcn_exp2f(m_run - base);
-      float psum[2] = {0.f, 0.f};
+        for (int i = 0; i < 16; ++i) {
+          const int pg = i >> 3;
+          float x;
+          if constexpr (HEAD) x = __builtin_fmaf(s[i], sc[pg], lvs[pg]) - m_ref;
+          else x = __builtin_fmaf(s[i], sc[pg], -m_ref);
+          p[i] = __builtin_amdgcn_exp2f(x);
+          psum[pg] = (i & 7) == 0 ? p[i] : psum[pg] + p[i];
+        }
+      };
+      exponentials();
+      // (an undefined sum takes the slow way, too; HEAD: it need not, the row is undefined with either)
+      if (__builtin_amdgcn_ballot_w64(!((HEAD ? fmaxf(psum[0], psum[1]) : psum[0] + psum[1]) <= sum_limit))) {
+        float mx[2];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int pg = i >> 3;
-        float x;
-        if constexpr (HEAD) x = __builtin_fmaf(s[i], sc[pg], lvs[pg]) - base;
-        else x = __builtin_fmaf(s[i], sc[pg], -base);
-        const float p = __builtin_amdgcn_exp2f(x);
-        psum[pg] += p;
-        pop[pg][i & 7] = (op)(FP8 && !HEAD ? p * vscale[pg] : p);
-      }
-      l_run = l_run * alpha + (HEAD ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1]);
-      if (__builtin_amdgcn_ballot_w64(m_new > m_run)) {
+        for (int pg = 0; pg < 2; ++pg) {
+          const int o = pg * 8;
+          float x = fmaxf(fmaxf(s[o], s[o + 1]), s[o + 2]);
+          x = fmaxf(fmaxf(x, s[o + 3]), s[o + 4]);
+          x = fmaxf(fmaxf(x, s[o + 5]), s[o + 6]);
+          mx[pg] = fmaxf(x, s[o + 7]);
+          mx[pg] = HEAD ? __builtin_fmaf(mx[pg], sc[pg], lvs[pg]) : mx[pg] * sc[pg];
+        }
+        float top = xor32_max(fmaxf(mx[0], mx[1]));            // the same in both lanes of a row
+        if constexpr (HEAD) {
+          // (of a score past 2^25 the difference may come out larger, more than f16 holds; exponents are differences of numbers that were
+          // rounded like this one, so none is larger)
+          const float below = top - kTreeWeightBits;
+          top = top - below > kMostBits ? top : below;
+        }
+        const float m_old = sum_limit < 0.f ? -INFINITY : m_ref, m_new = fmaxf(m_old, top);
+        const float m_safe = m_new == -INFINITY ? 0.f : m_new;   // (a row that has seen nothing yet)
+        const float alpha = __builtin_amdgcn_exp2f(m_old - m_safe);
+        l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+        m_ref = m_safe;
+        if (m_new != -INFINITY) sum_limit = HEAD ? kHalfSumLimit : kSumLimit;
+        exponentials();
       }
-      m_run = m_new;
-    }
-  };
-  // ---- O^T += V^T P^T : A = V^T tile (32 dims x 16 tokens) read transposed from LDS
-  auto v_operand = [&](int slot, int ks, int dt) __attribute__((always_inline)) -> opx8 {
-    if constexpr (FP8) {
-      typedef __attribute__((address_space(3))) intx2 lds_i2;
-      const int t = ks * 16 + h2 * 8 + ((lane & 15) >> 1);
-      const int col = ((dt * 2 + ((lane >> 4) & 1)) ^ tree_key_v<true>(t)) & (G_::kChunks - 1);
-      const intx2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2*)(lds.v[slot] + t * G_::kRowBytes + col * 16 + (lane & 1) * 8));
-      return widen_v8<KV>((uint32_t)raw[0], (uint32_t)raw[1]);
-    } else {
-      typedef __attribute__((address_space(3))) shortx4 lds_s4;
-      bf16x8 v;
+      l_run += HEAD ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1];
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const int j = lane & 15, t = ks * 16 + h2 * 8 + hf * 4 + (j >> 2);
-        const int col = ((dt * 4 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1)) ^ tree_key_v<false>(t)) & (G_::kChunks - 1);
-        const shortx4 raw = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(lds.v[slot] + t * G_::kRowBytes + col * 16 + (j & 1) * 8));
-        const bf16x4 h4 = __builtin_bit_cast(bf16x4, raw);
-        v[hf * 4 + 0] = h4[0]; v[hf * 4 + 1] = h4[1]; v[hf * 4 + 2] = h4[2]; v[hf * 4 + 3] = h4[3];
-      }
-      return v;
+      for (int i = 0; i < 16; ++i) pop[i >> 3][i & 7] = (op)(FP8 && !HEAD ? p[i] * vscale[i >> 3] : p[i]);
     }
   };
-  auto values = [&](int slot) __attribute__((always_inline)) {
+  // ---- O^T += V^T P^T : A = V^T tile (32 dims x 16 tokens) read transposed from LDS, in front of the softmax
+  using raw_v = std::conditional_t<FP8, intx2, bf16x8>;
+  raw_v v_raw[2][kDT];
+  auto read_values = [&](int slot) __attribute__((always_inline)) {
+    const unsigned int v_at = lds + L_::v(slot);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) {
-        const opx8 v = v_operand(slot, ks, dt);
-acc[dt] = mfma32(v, pop[ks], acc[dt]);
+        if constexpr (FP8) {
+          typedef __attribute__((address_space(3))) intx2 lds_i2;
+          const int t = ks * 16 + h2 * 8 + ((lane & 15) >> 1);
+          const int col = ((dt * 2 + ((lane >> 4) & 1)) ^ tree_key_v<true>(t)) & (G_::kChunks - 1);
+          v_raw[ks][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2*)(uintptr_t)(v_at + t * G_::kRowBytes + col * 16 + (lane & 1) * 8));
+        } else {
+          typedef __attribute__((address_space(3))) shortx4 lds_s4;
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const int j = lane & 15, t = ks * 16 + h2 * 8 + hf * 4 + (j >> 2);
+            const int col = ((dt * 4 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1)) ^ tree_key_v<false>(t)) & (G_::kChunks - 1);
+            const shortx4 raw = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)(v_at + t * G_::kRowBytes + col * 16 + (j & 1) * 8));
+            const bf16x4 h4 = __builtin_bit_cast(bf16x4, raw);
+            v_raw[ks][dt][hf * 4 + 0] = h4[0]; v_raw[ks][dt][hf * 4 + 1] = h4[1]; v_raw[ks][dt][hf * 4 + 2] = h4[2]; v_raw[ks][dt][hf * 4 + 3] = h4[3];
+          }
+        }
+      }
+  };
+  auto values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) {
+        if constexpr (FP8) acc[dt] = mfma32(widen_v8<KV>((uint32_t)v_raw[ks][dt][0], (uint32_t)v_raw[ks][dt][1]), pop[ks], acc[dt]);
+        else acc[dt] = mfma32(v_raw[ks][dt], pop[ks], acc[dt]);
       }
   };
   // Whether the values of a block hold any that is no number: then zeros take their places in front of the second product, and those of
   // the segment are added to what is stored of it.
   auto any_undefined = [&](int slot) __attribute__((always_inline)) {
-    bool any = false;
+    uint32_t any = 0;
 #pragma unroll
     for (int j = 0; j < G_::kLoads; ++j) {
-      const uint4 w = *(const uint4*)(lds.v[slot] + j * 1024 + lane * 16);
-      any |= undefined<KV>(w.x) | undefined<KV>(w.y) | undefined<KV>(w.z) | undefined<KV>(w.w);
+      const uint4_v w = *lds_at<const uint4_v>(lds + L_::v(slot) + j * 1024 + lane * 16);
+      any |= undefined<KV>(w[0]) | undefined<KV>(w[1]) | undefined<KV>(w[2]) | undefined<KV>(w[3]);
     }
-    return __builtin_amdgcn_ballot_w64(any) != 0;
+    return __builtin_amdgcn_ballot_w64(any != 0) != 0;
   };
   auto without_undefined = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < G_::kLoads; ++j) {
-      uint4* const at = (uint4*)(lds.v[slot] + j * 1024 + lane * 16);
-      const uint4 w = *at;
-      *at = make_uint4(defined<KV>(w.x), defined<KV>(w.y), defined<KV>(w.z), defined<KV>(w.w));
+      const auto at = lds_at<uint4_v>(lds + L_::v(slot) + j * 1024 + lane * 16);
+      const uint4_v w = *at;
+      *at = uint4_v{defined<KV>(w[0]), defined<KV>(w[1]), defined<KV>(w[2]), defined<KV>(w[3])};
     }
   };
 
-  // the block in `slot`, from its scores on
-  auto consume = [&](int i, int slot, bool edge, const float4& scales) __attribute__((always_inline)) {
-    softmax(edge, scales);
-    if constexpr (!INT8 && W == 1) {
-      if (edge && any_undefined(slot)) {
-        without_undefined(slot);
-        dirty = true;
-      }
-    }
-    values(slot);
-  };
   int slot = 0;
-  auto scales_of = [&](int slot) __attribute__((always_inline)) { return FP8 ? *(const float4*)lds.scales[slot][wave] : make_float4(1.f, 1.f, 1.f, 1.f); };
+  auto scales_of = [&](int slot) __attribute__((always_inline)) { 
+    floatx4 x = {1.f, 1.f, 1.f, 1.f};
+    if constexpr (FP8) x = *lds_at<const floatx4>(lds + L_::scales(slot, wave));
+    return x;
+  };
   if constexpr (W == 1) {
     for (int i = 0; i < min(kSlots, n_mine); ++i) {
       issue_k(i);
@@ -557,7 +590,7 @@ acc[dt] = mfma32(v, pop[ks], acc[dt]);
       const int behind = min(kSlots - 1, n_mine - 1 - i);      // blocks behind this one that are under way
       await(behind, std::integral_constant<int, kVLoads>{});
       scores(slot);
-      const float4 scales = scales_of(slot);
+      const floatx4 scales = scales_of(slot);
       if (more) {
         all_read();
         issue_k(slot);
@@ -565,7 +598,15 @@ acc[dt] = mfma32(v, pop[ks], acc[dt]);
       } else {
         await(behind, std::integral_constant<int, 0>{});
       }
-      consume(i, slot, edge, scales);
+      if constexpr (!INT8) {
+        if (edge && any_undefined(slot)) {
+          without_undefined(slot);
+          dirty = true;
+        }
+      }
+      read_values(slot);
+      softmax(edge, scales);
+      values();
       if (more) {
         all_read();
         issue_v(slot);
@@ -593,7 +634,9 @@ acc[dt] = mfma32(v, pop[ks], acc[dt]);
       }
       if (rows_here > 0) {
         scores(slot);
-        consume(i, slot, edge, scales_of(slot));
+        read_values(slot);
+        softmax(edge, scales_of(slot));
+        values();
       }
       if (cc.blk == cc.n - 1 || i == n_mine - 1) end_segment();
       if (i + 1 < n_mine) advance(cc);
@@ -640,7 +683,8 @@ __device__ __forceinline__ int4 tree_plan_in_wave(const TreeArgs& a, int worker)
 template <int D, int KV, int W>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 2) void tree_mfma_kernel(const TreeArgs a) {
   constexpr int kWorkers = W == 1 ? 4 : 1;       // of a workgroup
-  __shared__ TreeLds<D, kv_is_codes(KV), W> lds[kWorkers];
+  using L_ = TreeLds<D, kv_is_codes(KV), W>;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kWorkers][L_::kBytes];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds);
   const int worker = group * kWorkers + (W == 1 ? wave : 0);
@@ -649,7 +693,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 2) void tree_mfma_kernel(con
   else start = *(const int4*)(a.wstart + 4 * worker);
   const int b = __builtin_amdgcn_readfirstlane(start.x), at = __builtin_amdgcn_readfirstlane(start.y), mine = __builtin_amdgcn_readfirstlane(start.w);
   if (b < 0) return;
-  tree_worker<D, KV, W, false>(a, b, at >> 20, at & 0xFFFFF, mine, worker, W == 1 ? 0 : wave, lds[W == 1 ? wave : 0]);
+  tree_worker<D, KV, W, true>(a, b, at >> 20, at & 0xFFFFF, mine, worker, W == 1 ? 0 : wave, (unsigned int)(uintptr_t)&lds[0][0] + (W == 1 ? wave * L_::kBytes : 0));
 }
 
 __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(const TreeArgs a) {
