@@ -14,6 +14,7 @@
 // slots first and the rest of them to heads, so that a lane keeps its slot over all heads it walks.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "codes_device.h"
 
@@ -91,11 +92,11 @@ struct Turn {
   }
 };
 
-// The norm of a head's row, of which this lane has eight elements x in two runs of four and their weights w: by the root of the mean square,
-// in the order that the interface states (squares and runs in float32, the runs in double, which is exact, so that it does not matter
-// which lane has which).  Every lane of the row takes part.
+// Norms: a head's row, of which this lane has eight elements x in two runs of four, divided by the root of its mean square, in the order that
+// the interface states (squares and runs in float32, the runs in double, which is exact, so that it does not matter which lane has which).
+// Every lane of the row takes part and has the mean.
 template <int D>
-__device__ __forceinline__ void normalise(float (&x)[8], const float (&w)[8], float eps) {
+__device__ __forceinline__ float mean_square(const float (&x)[8]) {
 #pragma clang fp contract(off)
   const float lo = (x[0] * x[0] + x[1] * x[1]) + (x[2] * x[2] + x[3] * x[3]), hi = (x[4] * x[4] + x[5] * x[5]) + (x[6] * x[6] + x[7] * x[7]);
   double sum = (double)lo + (double)hi;
@@ -108,9 +109,28 @@ __device__ __forceinline__ void normalise(float (&x)[8], const float (&w)[8], fl
   add(std::integral_constant<int, 0x4e>{});
   add(std::integral_constant<int, 0x141>{});
   if constexpr (D == 128) add(std::integral_constant<int, 0x140>{});
-  const float r = 1.f / __builtin_sqrtf((float)(sum * (1.0 / D)) + eps);
+  return (float)(sum * (1.0 / D));
+}
+__device__ __forceinline__ float root_inverse(float mean, float eps) { return 1.f / __builtin_sqrtf(mean + eps); }
+__device__ __forceinline__ void scale_by(float (&x)[8], float inverse, const float (&w)[8]) {
+#pragma clang fp contract(off)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (x[i] * r) * w[i];
+  for (int i = 0; i < 8; ++i) x[i] = (x[i] * inverse) * w[i];
+}
+// x of lane `from` of this lane's row
+template <int D, int kFrom>
+__device__ __forceinline__ float from_lane(float x) {
+  if constexpr (D == 128) return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x150 + kFrom, 0xf, 0xf, true));
+  else return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), kFrom << 5 | 0x18));
+}
+
+template <class F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for_impl(f, std::make_integer_sequence<int, N>{});
 }
 
 // The cosines and sines of four pairs from j on; place: the token's place in its context, token: its number among the new ones.
@@ -181,13 +201,13 @@ __device__ __forceinline__ Raw<SRC_BYTES> fetch(const Lane& lane, const void* ro
 }
 
 // A row of the source type, normalised (NORM) and turned where it has to be, at p; STREAM: past the caches' care.
-template <int D, int SRC_BYTES, bool STREAM, bool NORM>
-__device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, const Turn& turn, const Weights<NORM>& weights, void* p, Raw<SRC_BYTES> r) {
+template <int SRC_BYTES, bool STREAM, bool NORM>
+__device__ __forceinline__ void store(const RopeWriteArgs& a, const Lane& lane, const Turn& turn, const Weights<NORM>& weights, float inverse, void* p, Raw<SRC_BYTES> r) {
   if (NORM || lane.turns) {
     float x[8];
     to_float<SRC_BYTES>(r, x);
     if constexpr (NORM) {
-      normalise<D>(x, weights.w, a.eps);
+      scale_by(x, inverse, weights.w);
       if (lane.turns) turn.apply(x, a.interleaved);
     } else {
       turn.apply(x, a.interleaved);
@@ -278,11 +298,29 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
   if (lane.turns) look_up(a, col * 4, place, token, turn);
   for (int h = 0; h < heads; h += kKeep * side) {
     if (h) load(r, h);
+    float inverse = 0.f;
+    if constexpr (NORM) {
+      // of the rows under way each lane works out one's root and quotient, 25 instructions that all lanes of a row would go through alike
+      float mine = 0.f;
 #pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      const int head = h0 + h + i * side + sub;
-      if (head < h1) store<D, SRC_BYTES, STREAM>(a, lane, turn, weights, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
+      for (int i = 0; i < kKeep; ++i) {
+        float x[8];
+        to_float<SRC_BYTES>(r[i], x);
+        const float mean = mean_square<D>(x);
+        mine = col == i ? mean : mine;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // (widened once more below: kept as floats, the rows would take twice the registers)
+#pragma unroll
+      for (int i = 0; i < kKeep; ++i) asm volatile("" : "+v"(r[i].lo), "+v"(r[i].hi));
+      inverse = root_inverse(mine, a.eps);
     }
+    static_for<kKeep>([&](auto i) __attribute__((always_inline)) {
+      const int head = h0 + h + i * side + sub;
+      if constexpr (NORM) __builtin_amdgcn_sched_barrier(0);
+      const float of_row = NORM ? from_lane<D, decltype(i)::value>(inverse) : 0.f;
+      if (head < h1) store<SRC_BYTES, STREAM>(a, lane, turn, weights, of_row, (unsigned char*)a.q_out + ((int64_t)token * a.hq + head) * D * SRC_BYTES, r[i]);
+    });
   }
 }
 
@@ -369,8 +407,14 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
           if (h + i * side < hkv) {
-            if (!NORM || pool == 0) store<D, SRC_BYTES, false>(a, lane, turn, weights, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
-            else store<D, SRC_BYTES, false>(a, lane, turn, Weights<false>{}, tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES, r[i]);
+            unsigned char* const dst = tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES;
+            if (NORM && pool == 0) {
+              float x[8];
+              to_float<SRC_BYTES>(r[i], x);
+              store<SRC_BYTES, false>(a, lane, turn, weights, root_inverse(mean_square<D>(x), a.eps), dst, r[i]);
+            } else {
+              store<SRC_BYTES, false>(a, lane, turn, Weights<false>{}, 0.f, dst, r[i]);
+            }
           }
       }
   } else {
@@ -380,10 +424,14 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
     __shared__ float old_scale[kMost], new_scale[kMost];
     float* const scales = (pool ? a.v_scale : a.k_scale) + page_id * (kHeadScales ? hkv : 1);
     constexpr float kMax = kInt8 ? kInt8Max : kE4m3Max;
-    auto rotated = [&](const Raw<SRC_BYTES>& r, float (&x)[8]) {
+    // inverse: of the row's root mean square, where keys are normalised; found where it is below zero
+    auto rotated = [&](const Raw<SRC_BYTES>& r, float (&x)[8], float& inverse) {
       to_float<2>(r, x);
       if constexpr (NORM) {
-        if (pool == 0) normalise<D>(x, weights.w, a.eps);
+        if (pool == 0) {
+          if (inverse < 0.f) inverse = root_inverse(mean_square<D>(x), a.eps);
+          scale_by(x, inverse, weights.w);
+        }
       }
       if (turns) turn.apply(x, a.interleaved);
     };
@@ -439,9 +487,9 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
       if constexpr (kLanes == 16) t = max(t, __builtin_amdgcn_mov_dpp(t, 0x140, 0xf, 0xf, true));
       return __int_as_float(t);
     };
-    auto emit = [&](int head, const Raw<SRC_BYTES>& r, float scale) {
+    auto emit = [&](int head, const Raw<SRC_BYTES>& r, float scale, float inverse) {
       float x[8];
-      rotated(r, x);
+      rotated(r, x, inverse);
       Quotients<kHeadScales>(scale).divide(x);
       unsigned char* dst = tile + ((size_t)head * kPageSize + s0 + slot) * D;
       *(unsigned int*)(dst + e0) = encode4(x);
@@ -453,12 +501,12 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
         for (int h = head0; h < hkv; h += side) {
           const float before = s0 ? scales[h] : 0.f;
           const Raw<SRC_BYTES> r = fetch_row(h);
-          float x[8];
-          rotated(r, x);
+          float x[8], inverse = -1.f;
+          rotated(r, x, inverse);
           const float now = settled(largest(x), before);
           if (s0 && now > before)
             for (int t = 0; t < s0; ++t) again8(tile + ((size_t)h * kPageSize + t) * D + col * 8, before, now);
-          emit(h, r, now);
+          emit(h, r, now, inverse);
           if (col == 0) scales[h] = now;          // (its lanes read the old one together)
         }
         continue;
@@ -468,6 +516,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
         float before = 0.f;
         if (s0 && (int)threadIdx.x < count) before = scales[r0 + threadIdx.x];
         if (r0 || another) __syncthreads();
+        float inverse[kRound] = {-1.f, -1.f, -1.f, -1.f};
         Raw<SRC_BYTES> keep[kRound] = {};       // (what is not loaded is nothing: else the rows of the round before, all the way)
         if (!idle) {
 #pragma unroll
@@ -477,7 +526,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
           for (int k = 0; k < kRound; ++k)
             if (k * side < count) {
               float x[8];
-              rotated(keep[k], x);
+              rotated(keep[k], x, inverse[k]);
               const float m = largest(x);
               if (col == 0) row_top[k][group] = m;
               __builtin_amdgcn_sched_barrier(0);
@@ -502,7 +551,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
 #pragma unroll
           for (int k = 0; k < kRound; ++k)
             if (head0 + k * side < count) {
-              emit(r0 + head0 + k * side, keep[k], new_scale[head0 + k * side]);
+              emit(r0 + head0 + k * side, keep[k], new_scale[head0 + k * side], inverse[k]);
               __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -514,8 +563,8 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
       float most = 0.f;
       if (!idle)
         for (int h = head0; h < hkv; h += side) {
-          float x[8];
-          rotated(fetch_row(h), x);
+          float x[8], inverse = -1.f;
+          rotated(fetch_row(h), x, inverse);
           most = fmaxf(most, largest(x));
         }
       if (another) __syncthreads();
@@ -532,7 +581,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
       __syncthreads();
       again(0, hkv);
       if (!idle)
-        for (int h = head0; h < hkv; h += side) emit(h, fetch_row(h), new_scale[0]);
+        for (int h = head0; h < hkv; h += side) emit(h, fetch_row(h), new_scale[0], -1.f);
     }
   }
   }
