@@ -1,3 +1,6 @@
+#ifndef VMAXW
+#define VMAXW 8
+#endif
 // Host side of librollattn: argument checks, workspace layout, the host twin of the
 // partition rule, and the launch sequence of each entry point.  Nothing here touches the
 // GPU before every argument check has passed.
@@ -933,7 +936,7 @@ TreeLayout tree_layout(const rollattn_desc& d, int64_t max_q_len) {
     return w;
   }
   const int64_t rows = std::max<int64_t>(1, max_q_len) * (d.num_q_heads / d.num_kv_heads);
-  w.parts = rows <= kTreeTileRows ? 1 : rows <= 2 * kTreeTileRows ? 2 : rows <= 4 * kTreeTileRows ? 4 : 8;
+  w.parts = rows <= kTreeTileRows ? 1 : rows <= 2 * kTreeTileRows ? 2 : rows <= 4 * kTreeTileRows ? 4 : VMAXW;
   w.tiles = (int32_t)std::min<int64_t>((rows + kTreeTileRows * w.parts - 1) / (kTreeTileRows * w.parts), INT32_MAX);
   w.workers = kNumCUs * 8 / w.parts;       // two waves to a SIMD
   const size_t parts = 2 * (size_t)w.workers * w.parts * kTreeTileRows;

@@ -1,3 +1,6 @@
+#ifndef VMT
+#define VMT 2048
+#endif
 // Attention of a tree of drafted tokens (bf16 queries) over bf16 or 8-bit (E4M3, int8) paged KV (gfx950).
 //
 // A row is (trajectory, KV head, tile of 32 W query rows): a query row is a (drafted token, query head of the group) pair,
@@ -25,6 +28,7 @@ typedef unsigned int uint4_v __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;             // of the merge
 constexpr int kWaves = kThreads / 64;
 constexpr int kRows = kTreeTileRows;      // query rows of a wave
+constexpr int kMergeTogether = VMT;
 constexpr float kSumLimit = 16384.f;      // see the softmax
 constexpr float kHalfSumLimit = 65000.f;
 constexpr float kTreeWeightBits = 8.f;    // f16 weights: log2 of a row's largest when its reference moves
@@ -37,7 +41,8 @@ __device__ __forceinline__ floatx16 mfma32(halfx8 x, halfx8 y, floatx16 z) { ret
 __device__ __forceinline__ int tau(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
 // Tiles of 32 W query rows that a draft of n tokens has per KV head (no more than the caller has said that the longest one has).
-__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int n) {
+template <class A>
+__device__ __forceinline__ int tree_tiles(const A& a, int n) {
   const int rows = kRows * a.tile_parts;
   return n > 0 ? min((n * a.group + rows - 1) / rows, a.row_tiles) : 0;
 }
@@ -76,10 +81,20 @@ __device__ __forceinline__ uint32_t defined(uint32_t w) {
   return w & ~(met * (KV == kKvBf16 ? 0xffffu : 0xffu));
 }
 
+// The kernel's arguments, read anew from their segment: what only a row's start and end need is not kept in scalar registers over its blocks
+// (they would spill, into lanes of vector registers that every block then fetches them from).
+typedef const __attribute__((address_space(4))) TreeArgs* tree_args_p;
+__device__ __forceinline__ tree_args_p tree_args() {
+  tree_args_p p = (tree_args_p)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
 // The lengths of one trajectory, the same in all lanes.
 struct Draft {
   int n, len, off;
-  __device__ __forceinline__ Draft(const TreeArgs& a, int b) {
+  template <class A>
+  __device__ __forceinline__ Draft(const A& a, int b) {
     typedef const __attribute__((address_space(4))) int32_t* const_i32_p;
     n = ((const_i32_p)a.q_lens)[b];
     len = ((const_i32_p)a.ctx_lens)[b];
@@ -91,7 +106,8 @@ struct Draft {
 struct RowAt {
   int node;
   size_t out;
-  __device__ __forceinline__ RowAt(const TreeArgs& a, const Draft& d, int g, int j) {
+  template <class A>
+  __device__ __forceinline__ RowAt(const A& a, const Draft& d, int g, int j) {
     node = j / a.group;
     out = (size_t)(d.off + node) * a.hq + (size_t)g * a.group + (j - node * a.group);
   }
@@ -137,16 +153,15 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   const int n32 = lane & 31;   // query row (B column) / K token row (A row) carried by this lane
   const int h2 = lane >> 5;    // half of the contraction this lane feeds
 
-  const int group = a.group, hkv = a.hkv;
-  const size_t tile_stride = (size_t)kPageSize * G_::kRowBytes;   // bytes of one (page, head) tile
-  const bool flip = a.scale_log2 < 0.f;                           // (queries the other way round, so that larger scores are larger exponents)
-  const float scale_log2 = __builtin_fabsf(a.scale_log2);
+  const int hkv = a.hkv;
+  constexpr size_t tile_stride = (size_t)kPageSize * G_::kRowBytes;   // bytes of one (page, head) tile
 
   // trajectory, KV head, tile and block within the row; blocks in the row, context length, tiles per KV head
   struct Cursor { int b, g, tile, blk, n, len, tiles; };
   auto enter = [&](Cursor& c) {
-    const Draft d(a, c.b);
-    c.tiles = tree_tiles(a, d.n);
+    const tree_args_p e = tree_args();
+    const Draft d(*e, c.b);
+    c.tiles = tree_tiles(*e, d.n);
     c.len = c.tiles ? d.len : 0;
     c.n = (c.len + kBlockTokens - 1) / kBlockTokens;
   };
@@ -170,11 +185,14 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   };
 
   // ---- producer: a window of 64 page ids (32 blocks) of the current row, one per lane
-  int pwin = -1, pid_vec = 0, pid_next = 0, issued = 0;
-  int p_page[2] = {0, 0}, p_g = 0, p_lim = 0;         // the block under way: pages, KV head, and tokens of it that are there
+  int pid_vec = 0, pid_next = 0, left = n_mine;
+  bool fresh = true;                          // no window of this row yet
+  int p_page[2] = {0, 0}, p_lim = 0;          // the block under way: its pages, and tokens from its first on
+  size_t p_at[2] = {0, 0};                    // ... and where this wave's loads find them in a pool
   auto load_window = [&](int k) {
+    const tree_args_p e = tree_args();
     const int pg = k * 64 + lane;
-    return (pg < ((pc.len + kPageSize - 1) >> 4)) ? a.page_table[(size_t)pc.b * a.max_pages + pg] : 0;
+    return (pg < ((pc.len + kPageSize - 1) >> 4)) ? e->page_table[(size_t)pc.b * e->max_pages + pg] : 0;
   };
   auto dma16 = [&](const unsigned char* base, unsigned int off, unsigned int dst) __attribute__((always_inline)) {
     const unsigned int m0 = __builtin_amdgcn_readfirstlane(dst);
@@ -196,38 +214,50 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     off_k[i] = offset(std::false_type{}, i, kBlockTokens);
     off_v[i] = offset(std::true_type{}, i, kBlockTokens);
   }
+  const bool upper = first * G_::kRowsPerLoad >= kPageSize;        // (one load of a tile: of its second page)
   auto load_tile = [&](auto v_c, int slot) __attribute__((always_inline)) {
     constexpr bool V = decltype(v_c)::value;
-    size_t at[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) at[i] = (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(p_page[i] * hkv + p_g) * tile_stride;
+    const unsigned int dst = lds + (V ? L_::v(slot) : L_::k(slot)) + first * 1024;
 #pragma unroll
     for (int i = 0; i < kShare; ++i) {
-      const int j = first + i * W;
-      const unsigned char* tile = (const unsigned char*)(V ? a.v_pages : a.k_pages) + (j * G_::kRowsPerLoad < kPageSize ? at[0] : at[1]);
-      const unsigned int off = p_lim == kBlockTokens ? (V ? off_v[i] : off_k[i]) : offset(v_c, i, p_lim);
-      dma16(tile, off, lds + (V ? L_::v(slot) : L_::k(slot)) + j * 1024);
+      const bool second = kShare == 1 ? upper : (first + i * W) * G_::kRowsPerLoad >= kPageSize;
+      const unsigned char* tile = (const unsigned char*)(V ? a.v_pages : a.k_pages) + (kShare == 1 || !second ? p_at[0] : p_at[1]);
+      const unsigned int off = p_lim >= kBlockTokens ? (V ? off_v[i] : off_k[i]) : offset(v_c, i, p_lim);
+      dma16(tile, off, dst + i * W * 1024);
     }
   };
   auto load_k = [&](int slot) __attribute__((always_inline)) { load_tile(std::false_type{}, slot); };
   auto load_v = [&](int slot) __attribute__((always_inline)) { load_tile(std::true_type{}, slot); };
   // what block pc of the run needs
   auto look_up = [&]() __attribute__((always_inline)) {
-    const int k = pc.blk >> 5;
-    if (k != pwin) {
-      pid_vec = (pwin >= 0 && k == pwin + 1) ? pid_next : load_window(k);
+    const int in = pc.blk & 31;
+    if (fresh || in == 0) {
+      const int k = pc.blk >> 5;
+      pid_vec = fresh ? load_window(k) : pid_next;
       pid_next = load_window(k + 1);
-      pwin = k;
+      fresh = false;
     }
-    p_g = pc.g;
-    p_lim = min(pc.len - pc.blk * kBlockTokens, kBlockTokens);
-    p_page[0] = __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1));
-    p_page[1] = p_lim > kPageSize ? __builtin_amdgcn_readlane(pid_vec, ((pc.blk & 31) << 1) + 1) : p_page[0];
+    p_lim = pc.len - pc.blk * kBlockTokens;
+    // (a page that the row's last block does not have: the one in front of it)
+    const int last = p_lim > kPageSize ? 1 : 0;
+    if constexpr (kShare == 1 && !FP8) {
+      p_page[0] = __builtin_amdgcn_readlane(pid_vec, in * 2 + (upper ? last : 0));
+    } else {
+      p_page[0] = __builtin_amdgcn_readlane(pid_vec, in * 2);
+      p_page[1] = __builtin_amdgcn_readlane(pid_vec, in * 2 + last);
+    }
+    auto at = [&](int page) { return (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(page * hkv + pc.g) * tile_stride; };
+    if constexpr (kShare == 1) {
+      p_at[0] = at(FP8 && upper ? p_page[1] : p_page[0]);
+    } else {
+      p_at[0] = at(p_page[0]);
+      p_at[1] = at(p_page[1]);
+    }
   };
   auto load_scales = [&](int slot) __attribute__((always_inline)) {
     if constexpr (FP8) {
       const int page = lane & 1 ? p_page[1] : p_page[0];
-      const float* from = (lane & 2 ? a.v_scale : a.k_scale) + (HEAD ? (size_t)page * hkv + p_g : (size_t)page);
+      const float* from = (lane & 2 ? a.v_scale : a.k_scale) + (HEAD ? (size_t)page * hkv + pc.g : (size_t)page);
       const unsigned int m0 = __builtin_amdgcn_readfirstlane(lds + L_::scales(slot, wave));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(from) : "memory");
     }
@@ -235,7 +265,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   // step to the next block of the run (never past its end: the rows after the last block need not exist); a new row starts with a
   // fresh page-id window
   auto step = [&]() __attribute__((always_inline)) {
-    if (++issued < n_mine && advance(pc)) pwin = -1;
+    if (--left > 0 && advance(pc)) fresh = true;
   };
   // (what the loads overwrite has been read)
   auto all_read = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
@@ -261,37 +291,35 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     load_scales(slot);
     step();
   };
-  // until all but this wave's loads of `blocks` blocks, and kMore others, have landed
-  auto await = [&](int blocks, auto more_c) __attribute__((always_inline)) {
+  // until all but this wave's loads of kBlocks blocks, and kMore others, have landed; near the run's end, where fewer blocks follow, of none
+  auto await = [&](bool follow, auto blocks_c, auto more_c) __attribute__((always_inline)) {
     constexpr int kMore = decltype(more_c)::value, kBlock = kVLoads + kKLoads;
-    if (kSlots > 3 && blocks == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 3 ? 3 * kBlock + kMore : 0) : "memory");
-    else if (kSlots > 2 && blocks == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 2 ? 2 * kBlock + kMore : 0) : "memory");
-    else if (kSlots > 1 && blocks == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSlots > 1 ? kBlock + kMore : 0) : "memory");
+    if (follow) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(blocks_c)::value * kBlock + kMore) : "memory");
     else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMore) : "memory");
   };
 
   // ---- consumer state
   kx8 qop[kKK];              // Q^T as the B operand: lane (row n32, half h2), 8 dims per step
-  float q_unit = 0.f;        // int8: what a unit of this lane's row is worth
+  float q_unit = 0.f;        // what a unit of this lane's row is worth, softmax scale included
   floatx16 acc[kDT];        // O^T: lane (row n32, half h2) holds dims dt*32 + (i/4)*8 + h2*4 + i%4
   float m_ref = 0.f, l_run = 0.f;   // reference of this lane's row (log2 units), zero as long as it has seen nothing; its share of the running sum
   float sum_limit = -1.f;           // a lane's exponentials of a block may add up to this much; below zero: no reference yet
   int seg_first_blk = 0;     // block of the row at which the current segment started
   bool first_segment = true, dirty = false;   // dirty: values of the segment that are no numbers have been left out of its sums
-  int rows_here = 0, prefix = 0, n_b = 0, q_off = 0, j0 = 0, g = 0;   // of the consumer's row
+  int rows_here = 0, edge_blk = 0;            // of the consumer's row: query rows of this wave, first block with tokens behind the prefix
 
   auto begin_segment = [&]() __attribute__((always_inline)) {
-    const Draft d(a, cc.b);
-    g = cc.g;
-    j0 = cc.tile * kTile + wave * kRows;
-    n_b = d.n;
-    q_off = d.off;
-    prefix = d.len - d.n;
-    rows_here = min(kRows, d.n * group - j0);        // (none: a wave past the last row helps with the loads)
+    const tree_args_p e = tree_args();
+    const Draft d(*e, cc.b);
+    const int j0 = cc.tile * kTile + wave * kRows;
+    rows_here = min(kRows, d.n * e->group - j0);     // (none: a wave past the last row helps with the loads)
+    edge_blk = (d.len - d.n) / kBlockTokens;
+    const bool flip = e->scale_log2 < 0.f;           // (queries the other way round, so that larger scores are larger exponents)
+    const float scale_log2 = __builtin_fabsf(e->scale_log2);
     {
       // (rows past the last read it again; what becomes of them is not stored)
-      const RowAt at(a, d, g, max(0, min(j0 + n32, d.n * group - 1)));
-      const __bf16* qrow = (const __bf16*)a.q + at.out * D;
+      const RowAt at(*e, d, cc.g, max(0, min(j0 + n32, d.n * e->group - 1)));
+      const __bf16* qrow = (const __bf16*)e->q + at.out * D;
 #pragma unroll
       for (int kk = 0; kk < kKK; ++kk) {
         // FP8: 16-byte K chunks hold 16 dims; step 2p+e uses bytes e*8.. of chunk p*2+h2
@@ -331,16 +359,18 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   auto end_segment = [&]() __attribute__((always_inline)) {
     const bool whole = seg_first_blk == 0 && cc.blk == cc.n - 1;
     const size_t slot = (size_t)worker * 2 + (first_segment ? 0 : 1);
-    const Draft d(a, cc.b);
+    const tree_args_p e = tree_args();
+    const Draft d(*e, cc.b);
+    const int g = cc.g, j0 = cc.tile * kTile + wave * kRows, prefix = d.len - d.n;
     if (rows_here > 0) {
       const float l_tot = xor32_add(l_run), m_run = sum_limit < 0.f ? -INFINITY : m_ref;
       if (whole) {
         // the whole row was ours: normalise and store
         const bool ok = n32 < rows_here;
-        const RowAt at(a, d, g, max(0, min(j0 + n32, d.n * group - 1)));
+        const RowAt at(*e, d, g, max(0, min(j0 + n32, d.n * e->group - 1)));
         const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot;   // (nothing seen: a row of zeros)
-        if (a.lse && ok && h2 == 0) a.lse[at.out] = m_run + __builtin_amdgcn_logf(l_tot);
-        __bf16* dst = (__bf16*)a.out + at.out * D + h2 * 4;
+        if (e->lse && ok && h2 == 0) e->lse[at.out] = m_run + __builtin_amdgcn_logf(l_tot);
+        __bf16* dst = (__bf16*)e->out + at.out * D + h2 * 4;
         if (ok) {
 #pragma unroll
           for (int dt = 0; dt < kDT; ++dt)
@@ -352,47 +382,47 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
               *(bf16x4*)(dst + dt * 32 + i4 * 8) = pk;
             }
         }
-      } else {
-        float* dst = a.partial_o + (slot * W + wave) * (kRows * D) + lane * 4;
+      } else if (n32 < rows_here) {
+        float* dst = e->partial_o + (slot * W + wave) * (kRows * D) + lane * 4;
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
           for (int i4 = 0; i4 < 4; ++i4)
             *(floatx4*)(dst + (dt * 4 + i4) * 256) = floatx4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
-        if (h2 == 0) *(floatx2*)(a.partial_ml + ((slot * W + wave) * kRows + n32) * 2) = floatx2{m_run, l_tot};
+        if (h2 == 0) *(floatx2*)(e->partial_ml + ((slot * W + wave) * kRows + n32) * 2) = floatx2{m_run, l_tot};
       }
     }
     if (!INT8 && dirty) {
       // rare, and one token after the other: each lane adds to the values that it has just stored
       if (n32 < rows_here) {
-        const RowAt at(a, d, g, j0 + n32);
-        const uint64_t* const words = a.mask + (size_t)(d.off + at.node) * a.mask_words;
+        const RowAt at(*e, d, g, j0 + n32);
+        const uint64_t* const words = e->mask + (size_t)(d.off + at.node) * e->mask_words;
         for (int t = max(prefix, seg_first_blk * kBlockTokens); t < min(d.len, (cc.blk + 1) * kBlockTokens); ++t) {
           const int rel = t - prefix;
-          if (rel >= 64 * a.mask_words || !(words[rel >> 6] >> (rel & 63) & 1)) continue;
-          const size_t row = ((size_t)a.page_table[(size_t)cc.b * a.max_pages + t / kPageSize] * hkv + g) * kPageSize + t % kPageSize;
+          if (rel >= 64 * e->mask_words || !(words[rel >> 6] >> (rel & 63) & 1)) continue;
+          const size_t row = ((size_t)e->page_table[(size_t)cc.b * e->max_pages + t / kPageSize] * hkv + g) * kPageSize + t % kPageSize;
           for (int dim = h2 * 4; dim < D; dim += 8) {
             float x[4];
             if constexpr (FP8) {
-              const uint32_t w = *(const uint32_t*)((const unsigned char*)a.v_pages + row * D + dim);
+              const uint32_t w = *(const uint32_t*)((const unsigned char*)e->v_pages + row * D + dim);
               if (!undefined<KV>(w)) continue;
 #pragma unroll
               for (int e = 0; e < 4; ++e) x[e] = (w >> (8 * e) & 0x7f) == 0x7f ? NAN : 0.f;
             } else {
-              const uint2 w = *(const uint2*)((const __bf16*)a.v_pages + row * D + dim);
+              const uint2 w = *(const uint2*)((const __bf16*)e->v_pages + row * D + dim);
               if (!undefined<KV>(w.x) && !undefined<KV>(w.y)) continue;
               const uint32_t bits[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
 #pragma unroll
               for (int e = 0; e < 4; ++e) x[e] = (bits[e] & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits[e]) : 0.f;
             }
             if (whole) {
-              bf16x4* const o = (bf16x4*)((__bf16*)a.out + at.out * D + dim);
+              bf16x4* const o = (bf16x4*)((__bf16*)e->out + at.out * D + dim);
               bf16x4 y = *o;
 #pragma unroll
               for (int e = 0; e < 4; ++e) y[e] = (__bf16)((float)y[e] + x[e]);
               *o = y;
             } else {
-              floatx4* const o = (floatx4*)(a.partial_o + (slot * W + wave) * (kRows * D) + (dim / 8 * 64 + lane) * 4);
+              floatx4* const o = (floatx4*)(e->partial_o + (slot * W + wave) * (kRows * D) + (dim / 8 * 64 + lane) * 4);
               floatx4 y = *o;
 #pragma unroll
               for (int e = 0; e < 4; ++e) y[e] += x[e];
@@ -437,7 +467,6 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   opx8 pop[2];
   unsigned int seen = 0;                             // bit i: of this lane's score i (set in the blocks behind the prefix alone)
   auto softmax = [&](bool edge, const floatx4& scales) __attribute__((always_inline)) {
-    const int tok0 = cc.blk * kBlockTokens;
     float kscale[2] = {1.f, 1.f}, vscale[2] = {1.f, 1.f}, lvs[2] = {0.f, 0.f}, ivs[2] = {1.f, 1.f};
     if constexpr (FP8) {
       kscale[0] = scales[0]; kscale[1] = scales[1]; vscale[0] = scales[2]; vscale[1] = scales[3];
@@ -452,16 +481,18 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     {
       float sc[2];
 #pragma unroll
-      for (int pg = 0; pg < 2; ++pg) sc[pg] = (INT8 ? q_unit : scale_log2) * (FP8 ? kscale[pg] : 1.f);
+      for (int pg = 0; pg < 2; ++pg) sc[pg] = q_unit * (FP8 ? kscale[pg] : 1.f);
       if (edge) {
         // (faint queries over faint keys: a unit that has gone to zero would make a masked token's exponent undefined)
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) sc[pg] = fmaxf(sc[pg], 0x1p-126f);
-        const int j = max(0, min(j0 + n32, n_b * group - 1));
-        const uint64_t* words = a.mask + (size_t)(q_off + j / group) * a.mask_words;
+        const tree_args_p e = tree_args();
+        const Draft d(*e, cc.b);
+        const int j = max(0, min(cc.tile * kTile + wave * kRows + n32, d.n * e->group - 1)), n_words = e->mask_words;
+        const uint64_t* words = e->mask + (size_t)(d.off + j / e->group) * n_words;
         seen = 0;
 #pragma unroll
-        for (int pg = 0; pg < 2; ++pg) seen |= seen_bits(words, a.mask_words, tok0 + pg * kPageSize + h2 * 8 - prefix, n_b, 0xffu) << (8 * pg);
+        for (int pg = 0; pg < 2; ++pg) seen |= seen_bits(words, n_words, cc.blk * kBlockTokens + pg * kPageSize + h2 * 8 - (d.len - d.n), d.n, 0xffu) << (8 * pg);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = seen >> i & 1 ? s[i] : -INFINITY;
       }
@@ -469,18 +500,21 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       // a lane's add up to more than kSumLimit (f16 weights: a page's to kHalfSumLimit, so that none is too large for f16), or while a row has no
       // reference, are the maxima found, the references moved there and the block's exponentials taken again.
       float psum[2], p[16];
-      auto exponentials = [&]() __attribute__((always_inline)) {
+      auto exponentials = [&](auto first_c) __attribute__((always_inline)) {
+        float ad[2];
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) ad[pg] = lvs[pg] - m_ref;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int pg = i >> 3;
           float x;
-          if constexpr (HEAD) x = __builtin_fmaf(s[i], sc[pg], lvs[pg]) - m_ref;
-          else x = __builtin_fmaf(s[i], sc[pg], -m_ref);
+          if constexpr (HEAD && !decltype(first_c)::value) x = __builtin_fmaf(s[i], sc[pg], lvs[pg]) - m_ref;
+          else x = __builtin_fmaf(s[i], sc[pg], ad[pg]);
           p[i] = __builtin_amdgcn_exp2f(x);
           psum[pg] = (i & 7) == 0 ? p[i] : psum[pg] + p[i];
         }
       };
-      exponentials();
+      exponentials(std::true_type{});
       // (an undefined sum takes the slow way, too; HEAD: it need not, the row is undefined with either)
       if (__builtin_amdgcn_ballot_w64(!((HEAD ? fmaxf(psum[0], psum[1]) : psum[0] + psum[1]) <= sum_limit))) {
         float mx[2];
@@ -510,7 +544,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
           for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
         m_ref = m_safe;
         if (m_new != -INFINITY) sum_limit = HEAD ? kHalfSumLimit : kSumLimit;
-        exponentials();
+        exponentials(std::false_type{});
       }
       l_run += HEAD ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1];
 #pragma unroll
@@ -579,24 +613,31 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
     if constexpr (FP8) x = *lds_at<const floatx4>(lds + L_::scales(slot, wave));
     return x;
   };
-  if constexpr (W == 1) {
-    for (int i = 0; i < min(kSlots, n_mine); ++i) {
+  for (int i = 0; i < min(W == 1 ? kSlots : kSlots - 1, n_mine); ++i) {
+    if constexpr (W == 1) {
       issue_k(i);
       issue_v(i);
+    } else {
+      issue(i);
     }
-    for (int i = 0; i < n_mine; ++i) {
-      if (i == 0 || cc.blk == 0) begin_segment();
-      const bool edge = (cc.blk + 1) * kBlockTokens > prefix, more = i + kSlots < n_mine;
-      const int behind = min(kSlots - 1, n_mine - 1 - i);      // blocks behind this one that are under way
-      await(behind, std::integral_constant<int, kVLoads>{});
+  }
+  constexpr std::integral_constant<int, kSlots - (W == 1 ? 1 : 2)> ahead_c{};   // blocks behind the one in work that are under way
+  constexpr std::integral_constant<int, 0> c0{};
+  bool begins = true;
+  for (int i = n_mine; i > 0; --i) {                 // (blocks that are left)
+    if (begins) begin_segment();
+    const bool edge = cc.blk >= edge_blk;
+    if constexpr (W == 1) {
+      const bool more = i > kSlots, follow = i >= kSlots;
+      await(follow, ahead_c, std::integral_constant<int, kVLoads>{});
       scores(slot);
       const floatx4 scales = scales_of(slot);
       if (more) {
         all_read();
         issue_k(slot);
-        await(behind, std::integral_constant<int, kKLoads>{});
+        await(true, ahead_c, std::integral_constant<int, kKLoads>{});
       } else {
-        await(behind, std::integral_constant<int, 0>{});
+        await(follow, ahead_c, c0);
       }
       if constexpr (!INT8) {
         if (edge && any_undefined(slot)) {
@@ -611,20 +652,12 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
         all_read();
         issue_v(slot);
       }
-      if (cc.blk == cc.n - 1 || i == n_mine - 1) end_segment();
-      if (i + 1 < n_mine) advance(cc);
-      slot = slot + 1 == kSlots ? 0 : slot + 1;
-    }
-  } else {
-    for (int i = 0; i < min(kSlots - 1, n_mine); ++i) issue(i);
-    for (int i = 0; i < n_mine; ++i) {
-      if (i == 0 || cc.blk == 0) begin_segment();
-      const bool edge = (cc.blk + 1) * kBlockTokens > prefix;
-      await(min(kSlots - 2, n_mine - 1 - i), std::integral_constant<int, 0>{});
+    } else {
+      await(i >= kSlots - 1, ahead_c, c0);
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (i + kSlots - 1 < n_mine) issue(slot == 0 ? kSlots - 1 : slot - 1);
+      if (left > 0) issue(slot == 0 ? kSlots - 1 : slot - 1);
       if constexpr (!INT8) {
-        // (the ones that are told apart: every wave looks at all of the tile, and none reads it until all have put zeros into it)
+        // (every wave looks at all of the tile, and none reads it for the product until all have put zeros into it)
         if (edge && any_undefined(slot)) {
           asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
           without_undefined(slot);
@@ -638,10 +671,11 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
         softmax(edge, scales_of(slot));
         values();
       }
-      if (cc.blk == cc.n - 1 || i == n_mine - 1) end_segment();
-      if (i + 1 < n_mine) advance(cc);
-      slot = slot + 1 == kSlots ? 0 : slot + 1;
     }
+    begins = cc.blk + 1 == cc.n;
+    if (begins || i == 1) end_segment();
+    if (i > 1) advance(cc);
+    slot = slot + 1 == kSlots ? 0 : slot + 1;
   }
 }
 
@@ -742,12 +776,17 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(const TreeArgs 
 }
 
 // Merge of the partials that runs left of rows they did not cover alone, as in combine.hip: one wave per (row, 32 query rows, 32 dims),
-// lanes as in the accumulators, four pieces under way at a time.  A piece of which a query row saw nothing has weight zero.
-template <int D>
+// lanes as in the accumulators, four pieces under way at a time; where those waves are few, a workgroup of four, which share the pieces and
+// fold their sums in order.  A piece of which a query row saw nothing has weight zero.
+// Bound by the latency of the partials' loads.
+template <int D, bool TOGETHER>
 __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) {
   constexpr int kDT = D / 32;
+  __shared__ __attribute__((aligned(16))) float sum_s[TOGETHER ? kWaves : 1][TOGETHER ? 4 : 1][TOGETHER ? 64 : 1][4];
+  __shared__ float ml_s[TOGETHER ? kWaves : 1][TOGETHER ? 64 : 1][2];
   const int lane = lane_id(), n32 = lane & 31, h2 = lane >> 5, parts = a.tile_parts;
-  const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + (threadIdx.x >> 6)));
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int unit = TOGETHER ? (int)blockIdx.x : (int)blockIdx.x * kWaves + wave;
   const int dt = unit % kDT, part0 = unit / kDT, most = a.row_tiles * parts;   // (of the longest draft: 32 query rows each)
   const int row = part0 / most, p = part0 - row * most, tile = p / parts, c = p - tile * parts, b = row / a.hkv, g = row - b * a.hkv;
   if (b >= a.batch) return;
@@ -760,27 +799,18 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) 
   const int wf = (int)(r0 / per), wl = (int)((r0 + n - 1) / per), pieces = wl - wf + 1;
   if (pieces == 1) return;                                  // one worker had the whole row
   const int first_slot = ((long)wf * per < r0) ? 1 : 0;
-  const bool ok = j0 + n32 < d.n * a.group;
+  const bool ok = j0 + n32 < d.n * a.group;                 // (there are no partials of the others)
   floatx4 o[4];
 #pragma unroll
   for (int i4 = 0; i4 < 4; ++i4) o[i4] = floatx4{0.f, 0.f, 0.f, 0.f};
   float ref = -INFINITY, l = 0.f;
-  constexpr int kN = 4;
-  for (int s0 = 0; s0 < pieces; s0 += kN) {
-    floatx2 x[kN];
-    floatx4 y[kN][4];
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int s = min(s0 + i, pieces - 1);
-      const size_t part = ((size_t)(wf + s) * 2 + (s == 0 ? first_slot : 0)) * parts + c;
-      x[i] = *(const floatx2*)(a.partial_ml + (part * kRows + n32) * 2);
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = *(const floatx4*)(a.partial_o + part * (kRows * D) + ((dt * 4 + i4) * 64 + lane) * 4);
-    }
+  // folds (maximum, sum, values) of kN things into the sums; those past the last have weight zero (zero times an infinity would not be zero)
+  auto fold = [&](auto n_c, int there, floatx2* x, floatx4 (*y)[4]) __attribute__((always_inline)) {
+    constexpr int kN = decltype(n_c)::value;
     float top = ref;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      if (s0 + i >= pieces) {                               // (zero times an infinity would not be zero)
+      if (i >= there) {
         x[i] = floatx2{-INFINITY, 0.f};
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -800,6 +830,39 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) 
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) o[i4] += f * y[i][i4];
     }
+  };
+  constexpr int kN = 4;
+  const int step = TOGETHER ? kWaves : 1, from = TOGETHER ? wave : 0;
+  if (ok)
+    for (int s0 = from; s0 < pieces; s0 += kN * step) {
+      floatx2 x[kN];
+      floatx4 y[kN][4];
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const int s = min(s0 + i * step, pieces - 1);
+        const size_t part = ((size_t)(wf + s) * 2 + (s == 0 ? first_slot : 0)) * parts + c;
+        x[i] = *(const floatx2*)(a.partial_ml + (part * kRows + n32) * 2);
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = *(const floatx4*)(a.partial_o + part * (kRows * D) + ((dt * 4 + i4) * 64 + lane) * 4);
+      }
+      fold(std::integral_constant<int, kN>{}, (pieces - s0 + step - 1) / step, x, y);
+    }
+  if constexpr (TOGETHER) {
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) *(floatx4*)sum_s[wave][i4][lane] = o[i4];
+    ml_s[wave][lane][0] = ref;
+    ml_s[wave][lane][1] = l;
+    __syncthreads();
+    if (wave != 0 || !ok) return;
+    floatx2 x[kWaves - 1];
+    floatx4 y[kWaves - 1][4];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+      x[w - 1] = floatx2{ml_s[w][lane][0], ml_s[w][lane][1]};
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) y[w - 1][i4] = *(const floatx4*)sum_s[w][i4][lane];
+    }
+    fold(std::integral_constant<int, kWaves - 1>{}, kWaves - 1, x, y);
   }
   if (!ok) return;
   const RowAt at(a, d, g, j0 + n32);
@@ -824,13 +887,15 @@ hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, hipStrea
     if (e != hipSuccess) return e;
   }
   const int64_t units = (int64_t)a.batch * a.hkv * a.row_tiles * a.tile_parts * (head_dim / 32);
-  const dim3 merge_grid((unsigned)((units + kWaves - 1) / kWaves));
+  const bool together = units <= kMergeTogether;
+  const dim3 merge_grid((unsigned)(together ? units : (units + kWaves - 1) / kWaves));
   auto launch = [&](auto d, auto kind, auto w) {
     constexpr int W = decltype(w)::value;
     hipLaunchKernelGGL((tree_mfma_kernel<decltype(d)::value, decltype(kind)::value, W>), dim3(a.workers / (W == 1 ? 4 : 1)), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((tree_merge_kernel<decltype(d)::value>), merge_grid, dim3(kThreads), 0, s, a);
+    if (together) hipLaunchKernelGGL((tree_merge_kernel<decltype(d)::value, true>), merge_grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((tree_merge_kernel<decltype(d)::value, false>), merge_grid, dim3(kThreads), 0, s, a);
     return hipGetLastError();
   };
   auto of_tiles = [&](auto d, auto kind) {
