@@ -1,6 +1,3 @@
-#ifndef VMAXW
-#define VMAXW 8
-#endif
 // Host side of librollattn: argument checks, workspace layout, the host twin of the
 // partition rule, and the launch sequence of each entry point.  Nothing here touches the
 // GPU before every argument check has passed.
@@ -925,7 +922,7 @@ int attn_tree_mask(const int32_t* parents, const int32_t* q_lens, const int32_t*
 namespace {
 // Workspace of attn_tree: the plan and the partials of rows that were cut.
 struct TreeLayout {
-  int32_t parts, tiles, workers;
+  int32_t parts, tiles, along, workers;
   size_t header, prefix, wstart, partial_ml, partial_o, total;
 };
 TreeLayout tree_layout(const rollattn_desc& d, int64_t max_q_len) {
@@ -936,9 +933,17 @@ TreeLayout tree_layout(const rollattn_desc& d, int64_t max_q_len) {
     return w;
   }
   const int64_t rows = std::max<int64_t>(1, max_q_len) * (d.num_q_heads / d.num_kv_heads);
-  w.parts = rows <= kTreeTileRows ? 1 : rows <= 2 * kTreeTileRows ? 2 : rows <= 4 * kTreeTileRows ? 4 : VMAXW;
+  w.parts = rows <= kTreeTileRows ? 1 : rows <= 2 * kTreeTileRows ? 2 : rows <= 4 * kTreeTileRows ? 4 : 8;
   w.tiles = (int32_t)std::min<int64_t>((rows + kTreeTileRows * w.parts - 1) / (kTreeTileRows * w.parts), INT32_MAX);
-  w.workers = kNumCUs * 8 / w.parts;       // two waves to a SIMD
+  w.along = w.parts == 1 ? 4 : w.parts == 2 && !has_codes(d) ? 2 : 1;
+  if (w.parts <= 2 && d.max_pages_per_seq <= kTreeWholePages) {
+    w.tiles = w.parts;
+    w.parts = 1;
+    w.along = 4;
+    w.total = off;
+    return w;
+  }
+  w.workers = kNumCUs * 8 / (w.parts * w.along);       // two waves to a SIMD
   const size_t parts = 2 * (size_t)w.workers * w.parts * kTreeTileRows;
   w.header = 0;
   w.prefix = off;      off += align256(sizeof(int32_t) * ((size_t)d.batch + 1));
@@ -980,7 +985,7 @@ int attn_tree(const rollattn_desc* desc, const void* q, const int32_t* q_lens, c
   }
   TreeArgs a{};
   char* base = (char*)workspace;
-  a.tile_parts = w.parts; a.row_tiles = w.tiles; a.workers = w.workers;
+  a.tile_parts = w.parts; a.row_tiles = w.tiles; a.along = w.along; a.workers = w.workers;
   a.header = (int32_t*)(base + w.header); a.prefix = (int32_t*)(base + w.prefix); a.wstart = (int32_t*)(base + w.wstart);
   a.partial_ml = (float*)(base + w.partial_ml); a.partial_o = (float*)(base + w.partial_o);
   a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.page_table = page_table; a.ctx_lens = ctx_lens;

@@ -24,6 +24,7 @@ constexpr int kDirectPagesFew = 64;     // the latter where their rows are resid
 constexpr int kDirectRowsFew = 512;     // ... two to a CU
 constexpr int kAppendTileRows = 256;    // query rows (token, head-in-group pairs) per append workgroup
 constexpr int kTreeTileRows = 32;       // drafts: query rows of a wave
+constexpr int kTreeWholePages = 64;     // drafts: tables of up to so many pages are not cut over workgroups
 constexpr int kXcds = 8;                // accelerator dies, each with its own L2; workgroups are dealt to them round-robin
 constexpr int kAppendBlockTokens = 64;  // KV tokens staged per step of the append kernel
 constexpr int kTileRecWords = 8;       // append: int32 per tile record (32 bytes: one scalar load)
@@ -224,8 +225,9 @@ struct TreeArgs {
   const float* v_scale;
   int32_t batch, hq, hkv, group, max_pages, mask_words, total_q;
   float scale_log2;
-  // bf16 queries: waves of 32 query rows in a tile (1, 2, 4 or 8), tiles per KV head that the longest draft has, workers, and the plan
-  int32_t tile_parts, row_tiles, workers;
+  // bf16 queries: waves of 32 query rows in a tile (1, 2, 4 or 8), tiles per KV head that the longest draft has, waves of a worker that share a
+  // row's blocks, workers (none: a workgroup to every row), and the plan
+  int32_t tile_parts, row_tiles, along, workers;
   int32_t *header, *prefix, *wstart;
   float *partial_ml, *partial_o;   // float[2 workers][tile_parts][32][2] (max in log2 units, sum) and [..][D / 8][64][4], as the accumulators lie
 };

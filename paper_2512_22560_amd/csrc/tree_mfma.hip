@@ -1,12 +1,10 @@
-#ifndef VMT
-#define VMT 2048
-#endif
 // Attention of a tree of drafted tokens (bf16 queries) over bf16 or 8-bit (E4M3, int8) paged KV (gfx950).
 //
-// A row is (trajectory, KV head, tile of 32 W query rows): a query row is a (drafted token, query head of the group) pair,
-// token-major, so the heads that share the KV head and the tokens of a draft that fit one tile read K and V once.  As in decode, rows
-// are cut into 32-token blocks, laid end to end, and every worker has one equal run of that sequence; a worker is W waves of 32 query rows
-// each.  It streams its run from memory straight into a ring of LDS tiles, and each of its waves consumes a block with
+// A query row is a (drafted token, query head of the group) pair, token-major, so the heads that share the KV head and the tokens of a draft that
+// fit one tile read K and V once; a wave has 32 of them.  A row is (trajectory, KV head, tile of query rows): of 32, or 64, as teams of four waves
+// that share its 32-token blocks take them, else of as many as the 2, 4 or 8 waves of a workgroup have that go through its blocks together.  As in
+// decode, the steps of all rows (of as many blocks as a worker does at a time) are laid end to end, and every worker, a workgroup, has one equal run
+// of that sequence; short tables' rows are not cut.  A worker streams its run from memory straight into LDS, and each wave consumes a block with
 //   S^T = K Q^T          (tokens x query rows, v_mfma_f32_32x32x16, K rows as A)
 //   O^T += V^T P^T       (dims x query rows, V read back transposed with ds_read_b64_tr_*)
 // A run that covers a whole row writes the row's output itself; one that starts or ends inside a row leaves an un-normalised partial
@@ -28,7 +26,9 @@ typedef unsigned int uint4_v __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;             // of the merge
 constexpr int kWaves = kThreads / 64;
 constexpr int kRows = kTreeTileRows;      // query rows of a wave
-constexpr int kMergeTogether = VMT;
+// Up to so many merged tiles of 32 query rows and 32 dims, a workgroup of four waves shares a tile's pieces: 57.1 -> 49.4 us for 3 drafts behind
+// 2k .. 32k, whose rows are of hundreds of pieces.  Above, a wave has a tile for itself (64 drafts behind 1k .. 8k, 4096 tiles: 140.2, shared 144.8).
+constexpr int kMergeTogether = 2048;
 constexpr float kSumLimit = 16384.f;      // see the softmax
 constexpr float kHalfSumLimit = 65000.f;
 constexpr float kTreeWeightBits = 8.f;    // f16 weights: log2 of a row's largest when its reference moves
@@ -113,32 +113,87 @@ struct RowAt {
   }
 };
 
-// A worker's ring: its blocks, the one in work included, so that two waves to a SIMD find their LDS.  Addresses are 32-bit offsets in the LDS.
+// A ring of blocks in LDS: a wave's own (W = 1), or that of W waves together.  Addresses are 32-bit offsets in the LDS.
 template <int D, bool FP8, int W>
 struct TreeLds {
   static constexpr int kSlots = W == 1 ? (FP8 ? 2 : 1) : W == 2 ? (FP8 ? 4 : 2) : 4;
   static constexpr int kTile = Geo<D, FP8>::kTileBytes, kScales = FP8 ? 256 : 0;   // scales of a block's two pages: K's, V's (the other lanes' are copies)
-  static constexpr int kBytes = kSlots * (2 * kTile + W * kScales);
+  static constexpr int kRing = kSlots * (2 * kTile + W * kScales);
   static __device__ __forceinline__ unsigned int k(int slot) { return slot * kTile; }
   static __device__ __forceinline__ unsigned int v(int slot) { return (kSlots + slot) * kTile; }
   static __device__ __forceinline__ unsigned int scales(int slot, int wave) { return 2 * kSlots * kTile + (slot * W + wave) * kScales; }
 };
+// The rings of a team of four waves, one each or one for two; and in their places, when a segment is done, what each wave's blocks came to: four
+// values of a lane, as the accumulators lie, and (maximum, sum) of a query row.
+template <int D, bool FP8>
+struct TeamLds {
+  static constexpr int kPart = kRows * D * 4, kEach = kPart + kRows * 8;
+  static constexpr int kOne = TreeLds<D, FP8, 1>::kRing, kTwo = TreeLds<D, FP8, 2>::kRing;
+  static constexpr int kMost = kEach > kOne ? kEach : kOne, kRoom = (2 * kMost > kTwo ? 2 * kMost : kTwo) + 2047 & ~2047;   // of two waves
+  static constexpr int kBytes = 2 * kRoom;
+  static __device__ __forceinline__ unsigned int of_wave(int wave) { return wave * (kRoom / 2); }
+  static __device__ __forceinline__ unsigned int part(int dt, int i4, int lane) { return ((dt * 4 + i4) * 64 + lane) * 16; }
+  static __device__ __forceinline__ unsigned int ml(int row) { return kPart + row * 8; }
+};
 template <class T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(unsigned int at) { return (__attribute__((address_space(3))) T*)(uintptr_t)at; }
 
-// One run of n_mine blocks from block blk of row (b, r) on.
+// Values of a segment's blocks that are no numbers, which its sums leave out, to the row of `node`, where that sees them: add(dim, four of them).
+// Rare, and one token after the other.
+template <int D, int KV, class F>
+__device__ __forceinline__ void add_undefined(const Draft& d, int b, int g, int node, int blk0, int n, int stride, int h2, F&& add) {
+  const tree_args_p e = tree_args();
+  const uint64_t* const words = e->mask + (size_t)(d.off + node) * e->mask_words;
+  const int prefix = d.len - d.n;
+  for (int blk = blk0; n > 0; --n, blk += stride)
+    for (int t = max(prefix, blk * kBlockTokens); t < min(d.len, (blk + 1) * kBlockTokens); ++t) {
+      const int rel = t - prefix;
+      if (rel >= 64 * e->mask_words || !(words[rel >> 6] >> (rel & 63) & 1)) continue;
+      const size_t row = ((size_t)e->page_table[(size_t)b * e->max_pages + t / kPageSize] * e->hkv + g) * kPageSize + t % kPageSize;
+      for (int dim = h2 * 4; dim < D; dim += 8) {
+        floatx4 x;
+        if constexpr (kv_is_codes(KV)) {
+          const uint32_t w = *(const uint32_t*)((const unsigned char*)e->v_pages + row * D + dim);
+          if (!undefined<KV>(w)) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = (w >> (8 * i) & 0x7f) == 0x7f ? NAN : 0.f;
+        } else {
+          const uint2 w = *(const uint2*)((const __bf16*)e->v_pages + row * D + dim);
+          if (!undefined<KV>(w.x) && !undefined<KV>(w.y)) continue;
+          const uint32_t bits[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = (bits[i] & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits[i]) : 0.f;
+        }
+        add(dim, x);
+      }
+    }
+}
+
+// What a wave's blocks of a row come to: O^T (lane (row n32, half h2) holds dims dt*32 + (i/4)*8 + h2*4 + i%4), the row's maximum (or a reference
+// near it, log2 units) and sum; undefined: values that are no numbers have been left out.
+template <int D>
+struct TreeSums {
+  floatx16 acc[D / 32];
+  float ref, sum;
+  bool undefined;
+};
+
+// n_mine blocks blk0, blk0 + stride, .. of KV head g of trajectory b, for the query rows j0 .. j0 + rows_here - 1 of its draft (none: a wave past
+// the last row helps with the loads).
 // Loads.  W = 1: the tiles of block i + slots go into the places of block i, K's as soon as the first product has read them and V's behind
 // the second; no barriers.  Else each wave loads its share of a block, waits for its own loads and meets the others at one barrier per block:
-// behind it the block is there, and the place of the block before is free for the one that is slots - 1 ahead.
+// behind it the block is there, and the place of the block before is free for the one that is slots - 1 ahead.  rounds: barriers, as many for
+// all waves of the workgroup (n_mine or more).
 // HBM -> LDS without a register stop: lane l's 16 bytes land at M0 + 16 l, so a row's chunks are swizzled by the address a lane
 // reads from.  The compiler does not see these loads as loads; they are awaited by count: vector-memory counts go down in order, so
 // with N of these loads sent after the ones that are waited for, no more than N outstanding operations of any kind means that those have
 // landed (others in between only make the wait longer).
-template <int D, int KV, int W, bool STREAM>
-__device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, int blk0, int n_mine, int worker, int wave, unsigned int lds) {
+template <int D, int KV, int W>
+__device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const Draft& d, int b, int g, int j0, int rows_here, int blk0, int n_mine,
+                                                      int stride, int rounds, int wave, unsigned int lds) {
   constexpr bool FP8 = kv_is_codes(KV), HEAD = kv_has_head_scales(KV);   // FP8: 8-bit codes of either kind
   constexpr bool INT8 = KV == kKvInt8Head;
-  constexpr int kTile = kRows * W, kSlots = TreeLds<D, FP8, W>::kSlots;
+  constexpr int kSlots = TreeLds<D, FP8, W>::kSlots;
   using L_ = TreeLds<D, FP8, W>;
   constexpr int kKK = D / 16, kDT = D / 32;
   using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
@@ -156,48 +211,18 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   const int hkv = a.hkv;
   constexpr size_t tile_stride = (size_t)kPageSize * G_::kRowBytes;   // bytes of one (page, head) tile
 
-  // trajectory, KV head, tile and block within the row; blocks in the row, context length, tiles per KV head
-  struct Cursor { int b, g, tile, blk, n, len, tiles; };
-  auto enter = [&](Cursor& c) {
-    const tree_args_p e = tree_args();
-    const Draft d(*e, c.b);
-    c.tiles = tree_tiles(*e, d.n);
-    c.len = c.tiles ? d.len : 0;
-    c.n = (c.len + kBlockTokens - 1) / kBlockTokens;
-  };
-  Cursor pc{b0, 0, 0, blk0, 0, 0, 0};         // producer: next block to request from HBM
-  enter(pc);
-  pc.g = r0 / pc.tiles;
-  pc.tile = r0 - pc.g * pc.tiles;
-  Cursor cc = pc;                             // consumer: block being computed
-  auto advance = [&](Cursor& c) {             // (whether it is another row now)
-    if (++c.blk < c.n) return false;
-    c.blk = 0;
-    if (++c.tile < c.tiles) return true;
-    c.tile = 0;
-    if (++c.g < hkv) return true;
-    c.g = 0;
-    do {
-      ++c.b;
-      enter(c);
-    } while (c.len == 0);
-    return true;
-  };
-
-  // ---- producer: a window of 64 page ids (32 blocks) of the current row, one per lane
-  int pid_vec = 0, pid_next = 0, left = n_mine;
-  bool fresh = true;                          // no window of this row yet
+  // ---- producer: a window of 64 page ids (32 of this wave's blocks), one per lane
+  int pid_vec = 0, pid_next = 0, sent = 0;    // blocks that have been sent for
   int p_page[2] = {0, 0}, p_lim = 0;          // the block under way: its pages, and tokens from its first on
   size_t p_at[2] = {0, 0};                    // ... and where this wave's loads find them in a pool
   auto load_window = [&](int k) {
     const tree_args_p e = tree_args();
-    const int pg = k * 64 + lane;
-    return (pg < ((pc.len + kPageSize - 1) >> 4)) ? e->page_table[(size_t)pc.b * e->max_pages + pg] : 0;
+    const int pg = (blk0 + (k * 32 + (lane >> 1)) * stride) * 2 + (lane & 1);
+    return (pg < ((d.len + kPageSize - 1) >> 4)) ? e->page_table[(size_t)b * e->max_pages + pg] : 0;
   };
   auto dma16 = [&](const unsigned char* base, unsigned int off, unsigned int dst) __attribute__((always_inline)) {
     const unsigned int m0 = __builtin_amdgcn_readfirstlane(dst);
-    if constexpr (STREAM) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(m0), "v"(off), "s"(base) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(m0), "v"(off), "s"(base) : "memory");
   };
   // This wave's share of a tile of one pool: row row0 + lane / chunks of the block per load.  What a lane reads of a tile is the same for every
   // whole block; of a row's ragged last one, rows at or past L_b read its last one again.
@@ -228,16 +253,15 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   };
   auto load_k = [&](int slot) __attribute__((always_inline)) { load_tile(std::false_type{}, slot); };
   auto load_v = [&](int slot) __attribute__((always_inline)) { load_tile(std::true_type{}, slot); };
-  // what block pc of the run needs
+  // what the next block needs
   auto look_up = [&]() __attribute__((always_inline)) {
-    const int in = pc.blk & 31;
-    if (fresh || in == 0) {
-      const int k = pc.blk >> 5;
-      pid_vec = fresh ? load_window(k) : pid_next;
+    const int in = sent & 31;
+    if (in == 0) {
+      const int k = sent >> 5;
+      pid_vec = k == 0 ? load_window(0) : pid_next;
       pid_next = load_window(k + 1);
-      fresh = false;
     }
-    p_lim = pc.len - pc.blk * kBlockTokens;
+    p_lim = d.len - (blk0 + sent * stride) * kBlockTokens;
     // (a page that the row's last block does not have: the one in front of it)
     const int last = p_lim > kPageSize ? 1 : 0;
     if constexpr (kShare == 1 && !FP8) {
@@ -246,7 +270,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       p_page[0] = __builtin_amdgcn_readlane(pid_vec, in * 2);
       p_page[1] = __builtin_amdgcn_readlane(pid_vec, in * 2 + last);
     }
-    auto at = [&](int page) { return (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(page * hkv + pc.g) * tile_stride; };
+    auto at = [&](int page) { return (size_t)(unsigned int)__builtin_amdgcn_readfirstlane(page * hkv + g) * tile_stride; };
     if constexpr (kShare == 1) {
       p_at[0] = at(FP8 && upper ? p_page[1] : p_page[0]);
     } else {
@@ -257,15 +281,10 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   auto load_scales = [&](int slot) __attribute__((always_inline)) {
     if constexpr (FP8) {
       const int page = lane & 1 ? p_page[1] : p_page[0];
-      const float* from = (lane & 2 ? a.v_scale : a.k_scale) + (HEAD ? (size_t)page * hkv + pc.g : (size_t)page);
+      const float* from = (lane & 2 ? a.v_scale : a.k_scale) + (HEAD ? (size_t)page * hkv + g : (size_t)page);
       const unsigned int m0 = __builtin_amdgcn_readfirstlane(lds + L_::scales(slot, wave));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(from) : "memory");
     }
-  };
-  // step to the next block of the run (never past its end: the rows after the last block need not exist); a new row starts with a
-  // fresh page-id window
-  auto step = [&]() __attribute__((always_inline)) {
-    if (--left > 0 && advance(pc)) fresh = true;
   };
   // (what the loads overwrite has been read)
   auto all_read = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
@@ -276,7 +295,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   };
   auto issue_v = [&](int slot) __attribute__((always_inline)) {
     load_v(slot);
-    step();
+    ++sent;
   };
   auto issue = [&](int slot) __attribute__((always_inline)) {
     look_up();
@@ -289,7 +308,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       load_k(slot);
     }
     load_scales(slot);
-    step();
+    ++sent;
   };
   // until all but this wave's loads of kBlocks blocks, and kMore others, have landed; near the run's end, where fewer blocks follow, of none
   auto await = [&](bool follow, auto blocks_c, auto more_c) __attribute__((always_inline)) {
@@ -299,174 +318,83 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
   };
 
   // ---- consumer state
-  kx8 qop[kKK];              // Q^T as the B operand: lane (row n32, half h2), 8 dims per step
-  float q_unit = 0.f;        // what a unit of this lane's row is worth, softmax scale included
-  floatx16 acc[kDT];        // O^T: lane (row n32, half h2) holds dims dt*32 + (i/4)*8 + h2*4 + i%4
+  TreeSums<D> own;
+  floatx16 (&acc)[kDT] = own.acc;
+  own.undefined = false;
   float m_ref = 0.f, l_run = 0.f;   // reference of this lane's row (log2 units), zero as long as it has seen nothing; its share of the running sum
   float sum_limit = -1.f;           // a lane's exponentials of a block may add up to this much; below zero: no reference yet
-  int seg_first_blk = 0;     // block of the row at which the current segment started
-  bool first_segment = true, dirty = false;   // dirty: values of the segment that are no numbers have been left out of its sums
-  int rows_here = 0, edge_blk = 0;            // of the consumer's row: query rows of this wave, first block with tokens behind the prefix
+  const int edge_blk = (d.len - d.n) / kBlockTokens;       // first block with tokens behind the prefix
 
-  auto begin_segment = [&]() __attribute__((always_inline)) {
+  kx8 qop[kKK];              // Q^T as the B operand: lane (row n32, half h2), 8 dims per step
+  float q_unit;              // what a unit of this lane's row is worth, softmax scale included
+  auto load_queries = [&]() __attribute__((always_inline)) {
     const tree_args_p e = tree_args();
-    const Draft d(*e, cc.b);
-    const int j0 = cc.tile * kTile + wave * kRows;
-    rows_here = min(kRows, d.n * e->group - j0);     // (none: a wave past the last row helps with the loads)
-    edge_blk = (d.len - d.n) / kBlockTokens;
     const bool flip = e->scale_log2 < 0.f;           // (queries the other way round, so that larger scores are larger exponents)
     const float scale_log2 = __builtin_fabsf(e->scale_log2);
-    {
-      // (rows past the last read it again; what becomes of them is not stored)
-      const RowAt at(*e, d, cc.g, max(0, min(j0 + n32, d.n * e->group - 1)));
-      const __bf16* qrow = (const __bf16*)e->q + at.out * D;
+    // (rows past the last read it again; what becomes of them is not stored)
+    const RowAt at(*e, d, g, max(0, min(j0 + n32, d.n * e->group - 1)));
+    const __bf16* qrow = (const __bf16*)e->q + at.out * D;
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) {
+      // FP8: 16-byte K chunks hold 16 dims; step 2p+e uses bytes e*8.. of chunk p*2+h2
+      uint4 v = *(const uint4*)(qrow + (FP8 ? ((kk >> 1) * 2 + h2) * 16 + (kk & 1) * 8 : kk * 16 + h2 * 8));
+      const uint32_t sign = flip ? 0x80008000u : 0u;
+      v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign;
+      qop[kk] = __builtin_bit_cast(kx8, v);     // (int8: as it came, until all of the row is there)
+    }
+    q_unit = scale_log2;
+    if constexpr (INT8) {
+      float top = 0.f;
 #pragma unroll
       for (int kk = 0; kk < kKK; ++kk) {
-        // FP8: 16-byte K chunks hold 16 dims; step 2p+e uses bytes e*8.. of chunk p*2+h2
-        uint4 v = *(const uint4*)(qrow + (FP8 ? ((kk >> 1) * 2 + h2) * 16 + (kk & 1) * 8 : kk * 16 + h2 * 8));
-        const uint32_t sign = flip ? 0x80008000u : 0u;
-        v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign;
-        qop[kk] = __builtin_bit_cast(kx8, v);     // (int8: as it came, until all of the row is there)
+        const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, __builtin_fabsf((float)v[e]));
       }
-      q_unit = scale_log2;
-      if constexpr (INT8) {
-        float top = 0.f;
+      const int up = kQueryBits - __builtin_amdgcn_frexp_expf(xor32_max(top));
 #pragma unroll
-        for (int kk = 0; kk < kKK; ++kk) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
+      for (int kk = 0; kk < kKK; ++kk) {
+        const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, __builtin_fabsf((float)v[e]));
-        }
-        const int up = kQueryBits - __builtin_amdgcn_frexp_expf(xor32_max(top));
-#pragma unroll
-        for (int kk = 0; kk < kKK; ++kk) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, qop[kk]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) qop[kk][e] = (_Float16)__builtin_amdgcn_ldexpf((float)v[e], up);
-        }
-        q_unit = __builtin_amdgcn_ldexpf(scale_log2, -up);
+        for (int e = 0; e < 8; ++e) qop[kk][e] = (_Float16)__builtin_amdgcn_ldexpf((float)v[e], up);
       }
-#pragma unroll
-      for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
-      m_ref = l_run = 0.f;
-      sum_limit = -1.f;
+      q_unit = __builtin_amdgcn_ldexpf(scale_log2, -up);
     }
-    seg_first_blk = cc.blk;
-    dirty = false;
-  };
-  auto end_segment = [&]() __attribute__((always_inline)) {
-    const bool whole = seg_first_blk == 0 && cc.blk == cc.n - 1;
-    const size_t slot = (size_t)worker * 2 + (first_segment ? 0 : 1);
-    const tree_args_p e = tree_args();
-    const Draft d(*e, cc.b);
-    const int g = cc.g, j0 = cc.tile * kTile + wave * kRows, prefix = d.len - d.n;
-    if (rows_here > 0) {
-      const float l_tot = xor32_add(l_run), m_run = sum_limit < 0.f ? -INFINITY : m_ref;
-      if (whole) {
-        // the whole row was ours: normalise and store
-        const bool ok = n32 < rows_here;
-        const RowAt at(*e, d, g, max(0, min(j0 + n32, d.n * e->group - 1)));
-        const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot;   // (nothing seen: a row of zeros)
-        if (e->lse && ok && h2 == 0) e->lse[at.out] = m_run + __builtin_amdgcn_logf(l_tot);
-        __bf16* dst = (__bf16*)e->out + at.out * D + h2 * 4;
-        if (ok) {
 #pragma unroll
-          for (int dt = 0; dt < kDT; ++dt)
+    for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-              bf16x4 pk;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) pk[e] = (__bf16)(acc[dt][i4 * 4 + e] * inv);
-              *(bf16x4*)(dst + dt * 32 + i4 * 8) = pk;
-            }
-        }
-      } else if (n32 < rows_here) {
-        float* dst = e->partial_o + (slot * W + wave) * (kRows * D) + lane * 4;
-#pragma unroll
-        for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4)
-            *(floatx4*)(dst + (dt * 4 + i4) * 256) = floatx4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
-        if (h2 == 0) *(floatx2*)(e->partial_ml + ((slot * W + wave) * kRows + n32) * 2) = floatx2{m_run, l_tot};
-      }
-    }
-    if (!INT8 && dirty) {
-      // rare, and one token after the other: each lane adds to the values that it has just stored
-      if (n32 < rows_here) {
-        const RowAt at(*e, d, g, j0 + n32);
-        const uint64_t* const words = e->mask + (size_t)(d.off + at.node) * e->mask_words;
-        for (int t = max(prefix, seg_first_blk * kBlockTokens); t < min(d.len, (cc.blk + 1) * kBlockTokens); ++t) {
-          const int rel = t - prefix;
-          if (rel >= 64 * e->mask_words || !(words[rel >> 6] >> (rel & 63) & 1)) continue;
-          const size_t row = ((size_t)e->page_table[(size_t)cc.b * e->max_pages + t / kPageSize] * hkv + g) * kPageSize + t % kPageSize;
-          for (int dim = h2 * 4; dim < D; dim += 8) {
-            float x[4];
-            if constexpr (FP8) {
-              const uint32_t w = *(const uint32_t*)((const unsigned char*)e->v_pages + row * D + dim);
-              if (!undefined<KV>(w)) continue;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = (w >> (8 * e) & 0x7f) == 0x7f ? NAN : 0.f;
-            } else {
-              const uint2 w = *(const uint2*)((const __bf16*)e->v_pages + row * D + dim);
-              if (!undefined<KV>(w.x) && !undefined<KV>(w.y)) continue;
-              const uint32_t bits[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = (bits[e] & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits[e]) : 0.f;
-            }
-            if (whole) {
-              bf16x4* const o = (bf16x4*)((__bf16*)e->out + at.out * D + dim);
-              bf16x4 y = *o;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) y[e] = (__bf16)((float)y[e] + x[e]);
-              *o = y;
-            } else {
-              floatx4* const o = (floatx4*)(e->partial_o + (slot * W + wave) * (kRows * D) + (dim / 8 * 64 + lane) * 4);
-              floatx4 y = *o;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) y[e] += x[e];
-              *o = y;
-            }
-          }
-        }
-      }
-    }
-    first_segment = false;
+      for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
   };
 
   floatx16 s;
-  // ---- S^T = K Q^T
-  auto scores = [&](int slot) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+  // ---- S^T = K Q^T.  All operands are on their way before the first product: the products hang together and would each wait for a trip to
+  // the LDS.
+  constexpr int kKeyReads = FP8 ? kKK / 2 : kKK;
+  uint4_v k_raw[kKeyReads];
+  auto read_keys = [&](int slot) __attribute__((always_inline)) {
     const int t = (n32 & 16) + tau(n32 & 15);
     const unsigned int rowp = lds + L_::k(slot) + t * G_::kRowBytes;
     const int key = tree_key_k<D, FP8>(t);
-    // (all operands on their way before the first product: the products hang together and would each wait for a trip to the LDS)
-    if constexpr (FP8) {
-      uint4_v raw[kKK / 2];
 #pragma unroll
-      for (int p = 0; p < kKK / 2; ++p) raw[p] = *lds_at<const uint4_v>(rowp + ((p * 2 + h2) ^ key) * 16);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < kKeyReads; ++i) k_raw[i] = *lds_at<const uint4_v>(rowp + (((i * 2 + h2) ^ key) & (G_::kChunks - 1)) * 16);
+  };
+  auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int p = 0; p < kKK / 2; ++p) {
-        s = mfma32(widen_k8<KV>(raw[p][0], raw[p][1]), qop[2 * p], s);
-        s = mfma32(widen_k8<KV>(raw[p][2], raw[p][3]), qop[2 * p + 1], s);
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kKeyReads; ++i) {
+      if constexpr (FP8) {
+        s = mfma32(widen_k8<KV>(k_raw[i][0], k_raw[i][1]), qop[2 * i], s);
+        s = mfma32(widen_k8<KV>(k_raw[i][2], k_raw[i][3]), qop[2 * i + 1], s);
+      } else {
+        s = mfma32(__builtin_bit_cast(kx8, k_raw[i]), qop[i], s);
       }
-    } else {
-      kx8 kop[kKK];
-#pragma unroll
-      for (int kk = 0; kk < kKK; ++kk) kop[kk] = *lds_at<const kx8>(rowp + (((kk * 2 + h2) ^ key) & (G_::kChunks - 1)) * 16);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int kk = 0; kk < kKK; ++kk) s = mfma32(kop[kk], qop[kk], s);
     }
   };
   // This lane then holds, for its rows, the scores of tokens tok0 + (i/8)*16 + h2*8 + i%8: eight of each page.
   opx8 pop[2];
   unsigned int seen = 0;                             // bit i: of this lane's score i (set in the blocks behind the prefix alone)
-  auto softmax = [&](bool edge, const floatx4& scales) __attribute__((always_inline)) {
+  auto softmax = [&](int blk, bool edge, const floatx4& scales) __attribute__((always_inline)) {
     float kscale[2] = {1.f, 1.f}, vscale[2] = {1.f, 1.f}, lvs[2] = {0.f, 0.f}, ivs[2] = {1.f, 1.f};
     if constexpr (FP8) {
       kscale[0] = scales[0]; kscale[1] = scales[1]; vscale[0] = scales[2]; vscale[1] = scales[3];
@@ -487,19 +415,19 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) sc[pg] = fmaxf(sc[pg], 0x1p-126f);
         const tree_args_p e = tree_args();
-        const Draft d(*e, cc.b);
-        const int j = max(0, min(cc.tile * kTile + wave * kRows + n32, d.n * e->group - 1)), n_words = e->mask_words;
+        const int j = max(0, min(j0 + n32, d.n * e->group - 1)), n_words = e->mask_words;
         const uint64_t* words = e->mask + (size_t)(d.off + j / e->group) * n_words;
         seen = 0;
 #pragma unroll
-        for (int pg = 0; pg < 2; ++pg) seen |= seen_bits(words, n_words, cc.blk * kBlockTokens + pg * kPageSize + h2 * 8 - (d.len - d.n), d.n, 0xffu) << (8 * pg);
+        for (int pg = 0; pg < 2; ++pg) seen |= seen_bits(words, n_words, blk * kBlockTokens + pg * kPageSize + h2 * 8 - (d.len - d.n), d.n, 0xffu) << (8 * pg);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = seen >> i & 1 ? s[i] : -INFINITY;
       }
       // The reference of a row only moves when it has to: exponentials are taken against it as it stands, and may exceed one.  Only when
       // a lane's add up to more than kSumLimit (f16 weights: a page's to kHalfSumLimit, so that none is too large for f16), or while a row has no
-      // reference, are the maxima found, the references moved there and the block's exponentials taken again.
+      // reference, is its maximum found, the reference moved there and the row's exponentials of the block taken again.
       float psum[2], p[16];
+      bool moves = false;                                    // this lane's row does (the others' stay, whatever their neighbours are)
       auto exponentials = [&](auto first_c) __attribute__((always_inline)) {
         float ad[2];
 #pragma unroll
@@ -510,13 +438,16 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
           float x;
           if constexpr (HEAD && !decltype(first_c)::value) x = __builtin_fmaf(s[i], sc[pg], lvs[pg]) - m_ref;
           else x = __builtin_fmaf(s[i], sc[pg], ad[pg]);
-          p[i] = __builtin_amdgcn_exp2f(x);
+          const float y = __builtin_amdgcn_exp2f(x);
+          p[i] = decltype(first_c)::value || moves ? y : p[i];
           psum[pg] = (i & 7) == 0 ? p[i] : psum[pg] + p[i];
         }
       };
       exponentials(std::true_type{});
       // (an undefined sum takes the slow way, too; HEAD: it need not, the row is undefined with either)
-      if (__builtin_amdgcn_ballot_w64(!((HEAD ? fmaxf(psum[0], psum[1]) : psum[0] + psum[1]) <= sum_limit))) {
+      const uint64_t past = __builtin_amdgcn_ballot_w64(!((HEAD ? fmaxf(psum[0], psum[1]) : psum[0] + psum[1]) <= sum_limit));
+      if (past) {
+        moves = ((uint32_t)past | (uint32_t)(past >> 32)) >> n32 & 1;
         float mx[2];
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
@@ -534,7 +465,7 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
           const float below = top - kTreeWeightBits;
           top = top - below > kMostBits ? top : below;
         }
-        const float m_old = sum_limit < 0.f ? -INFINITY : m_ref, m_new = fmaxf(m_old, top);
+        const float m_old = sum_limit < 0.f ? -INFINITY : m_ref, m_new = moves ? fmaxf(m_old, top) : m_old;
         const float m_safe = m_new == -INFINITY ? 0.f : m_new;   // (a row that has seen nothing yet)
         const float alpha = __builtin_amdgcn_exp2f(m_old - m_safe);
         l_run *= alpha;
@@ -587,28 +518,35 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
         else acc[dt] = mfma32(v_raw[ks][dt], pop[ks], acc[dt]);
       }
   };
-  // Whether the values of a block hold any that is no number: then zeros take their places in front of the second product, and those of
-  // the segment are added to what is stored of it.
-  auto any_undefined = [&](int slot) __attribute__((always_inline)) {
-    uint32_t any = 0;
+  // Where the values hold any that is no number, zeros take their places, and those of the segment are added to what is stored of it.
+  auto without_undefined = [&]() __attribute__((always_inline)) {
+    if constexpr (!INT8) {
+      constexpr int kWords = FP8 ? 2 : 4;
+      typedef unsigned int words_v __attribute__((ext_vector_type(kWords)));
+      uint32_t any = 0;
 #pragma unroll
-    for (int j = 0; j < G_::kLoads; ++j) {
-      const uint4_v w = *lds_at<const uint4_v>(lds + L_::v(slot) + j * 1024 + lane * 16);
-      any |= undefined<KV>(w[0]) | undefined<KV>(w[1]) | undefined<KV>(w[2]) | undefined<KV>(w[3]);
-    }
-    return __builtin_amdgcn_ballot_w64(any != 0) != 0;
-  };
-  auto without_undefined = [&](int slot) __attribute__((always_inline)) {
+      for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-    for (int j = 0; j < G_::kLoads; ++j) {
-      const auto at = lds_at<uint4_v>(lds + L_::v(slot) + j * 1024 + lane * 16);
-      const uint4_v w = *at;
-      *at = uint4_v{defined<KV>(w[0]), defined<KV>(w[1]), defined<KV>(w[2]), defined<KV>(w[3])};
+        for (int dt = 0; dt < kDT; ++dt) {
+          const words_v w = __builtin_bit_cast(words_v, v_raw[ks][dt]);
+#pragma unroll
+          for (int i = 0; i < kWords; ++i) any |= undefined<KV>(w[i]);
+        }
+      if (__builtin_amdgcn_ballot_w64(any != 0)) {
+        own.undefined = true;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int dt = 0; dt < kDT; ++dt) {
+            words_v w = __builtin_bit_cast(words_v, v_raw[ks][dt]);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = defined<KV>(w[i]);
+            v_raw[ks][dt] = __builtin_bit_cast(raw_v, w);
+          }
+      }
     }
   };
-
-  int slot = 0;
-  auto scales_of = [&](int slot) __attribute__((always_inline)) { 
+  auto scales_of = [&](int slot) __attribute__((always_inline)) {
     floatx4 x = {1.f, 1.f, 1.f, 1.f};
     if constexpr (FP8) x = *lds_at<const floatx4>(lds + L_::scales(slot, wave));
     return x;
@@ -621,16 +559,18 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       issue(i);
     }
   }
+  load_queries();
   constexpr std::integral_constant<int, kSlots - (W == 1 ? 1 : 2)> ahead_c{};   // blocks behind the one in work that are under way
   constexpr std::integral_constant<int, 0> c0{};
-  bool begins = true;
-  for (int i = n_mine; i > 0; --i) {                 // (blocks that are left)
-    if (begins) begin_segment();
-    const bool edge = cc.blk >= edge_blk;
+  int slot = 0, blk = blk0;
+  for (int i = n_mine, rest = W == 1 ? n_mine : rounds; rest > 0; --i, --rest, blk += stride) {               // (blocks that are left)
+    const bool edge = blk >= edge_blk;
     if constexpr (W == 1) {
       const bool more = i > kSlots, follow = i >= kSlots;
       await(follow, ahead_c, std::integral_constant<int, kVLoads>{});
-      scores(slot);
+      read_keys(slot);
+      __builtin_amdgcn_sched_barrier(0);
+      scores();
       const floatx4 scales = scales_of(slot);
       if (more) {
         all_read();
@@ -639,51 +579,40 @@ __device__ __forceinline__ void tree_worker(const TreeArgs& a, int b0, int r0, i
       } else {
         await(follow, ahead_c, c0);
       }
-      if constexpr (!INT8) {
-        if (edge && any_undefined(slot)) {
-          without_undefined(slot);
-          dirty = true;
-        }
-      }
       read_values(slot);
-      softmax(edge, scales);
+      softmax(blk, edge, scales);
+      if (edge) without_undefined();
       values();
       if (more) {
         all_read();
         issue_v(slot);
       }
     } else {
-      await(i >= kSlots - 1, ahead_c, c0);
+      if (i > 0) await(i >= kSlots - 1, ahead_c, c0);
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (left > 0) issue(slot == 0 ? kSlots - 1 : slot - 1);
-      if constexpr (!INT8) {
-        // (every wave looks at all of the tile, and none reads it for the product until all have put zeros into it)
-        if (edge && any_undefined(slot)) {
-          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          without_undefined(slot);
-          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          dirty = true;
-        }
-      }
-      if (rows_here > 0) {
-        scores(slot);
+      if (sent < n_mine) issue(slot == 0 ? kSlots - 1 : slot - 1);
+      if (rows_here > 0 && i > 0) {
+        read_keys(slot);
+        __builtin_amdgcn_sched_barrier(0);
+        scores();
         read_values(slot);
-        softmax(edge, scales_of(slot));
+        softmax(blk, edge, scales_of(slot));
+        if (edge) without_undefined();
         values();
       }
     }
-    begins = cc.blk + 1 == cc.n;
-    if (begins || i == 1) end_segment();
-    if (i > 1) advance(cc);
     slot = slot + 1 == kSlots ? 0 : slot + 1;
   }
+  own.ref = sum_limit < 0.f ? -INFINITY : m_ref;
+  own.sum = xor32_add(l_run);
+  return own;
 }
 
-// The partition: as plan_decode's, with hkv * tiles rows of a trajectory, of its own number of tiles.  Blocks of b before all heads:
-// prefix[b], in units of its KV heads.
-__device__ __forceinline__ int tree_blocks(const TreeArgs& a, int b, int& per_row) {
-  const int tiles = tree_tiles(a, a.q_lens[b]);
-  per_row = tiles ? (a.ctx_lens[b] + kBlockTokens - 1) / kBlockTokens : 0;
+// The partition: as plan_decode's, with hkv * tiles rows of a trajectory, of its own number of tiles, and in steps: what a worker's waves do at a
+// time, a block for every run of its waves along the row.  Steps of b before all heads: prefix[b], in units of its KV heads.
+__device__ __forceinline__ int tree_steps(const TreeArgs& a, int b, int& per_row) {
+  const int n = a.q_lens[b], tiles = tree_tiles(a, n), along = a.along;
+  per_row = tiles ? ((a.ctx_lens[b] + kBlockTokens - 1) / kBlockTokens + along - 1) / along : 0;
   return tiles * per_row;
 }
 
@@ -692,7 +621,7 @@ __device__ __forceinline__ int tree_blocks(const TreeArgs& a, int b, int& per_ro
 __device__ __forceinline__ int4 tree_plan_in_wave(const TreeArgs& a, int worker) {
   const int lane = lane_id(), hkv = a.hkv;
   int per_row = 0, count = 0;
-  if (lane < a.batch) count = tree_blocks(a, lane, per_row);
+  if (lane < a.batch) count = tree_steps(a, lane, per_row);
   const int upto = wave_inclusive_scan(count), first = upto - count;
   const int blocks = __builtin_amdgcn_readlane(upto, 63);
   const int total = blocks * hkv;
@@ -713,23 +642,6 @@ __device__ __forceinline__ int4 tree_plan_in_wave(const TreeArgs& a, int worker)
   return make_int4(b, ((rem / n) << 20) | (rem % n), 0, min(per, total - (int)x));
 }
 
-// Workgroups go to the XCDs in turn; workers that follow each other, whose rows may read the same K and V, have one XCD's cache in common.
-template <int D, int KV, int W>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, 2) void tree_mfma_kernel(const TreeArgs a) {
-  constexpr int kWorkers = W == 1 ? 4 : 1;       // of a workgroup
-  using L_ = TreeLds<D, kv_is_codes(KV), W>;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[kWorkers][L_::kBytes];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds);
-  const int worker = group * kWorkers + (W == 1 ? wave : 0);
-  int4 start;
-  if (a.batch <= kWavePlanBatch) start = tree_plan_in_wave(a, worker);
-  else start = *(const int4*)(a.wstart + 4 * worker);
-  const int b = __builtin_amdgcn_readfirstlane(start.x), at = __builtin_amdgcn_readfirstlane(start.y), mine = __builtin_amdgcn_readfirstlane(start.w);
-  if (b < 0) return;
-  tree_worker<D, KV, W, true>(a, b, at >> 20, at & 0xFFFFF, mine, worker, W == 1 ? 0 : wave, (unsigned int)(uintptr_t)&lds[0][0] + (W == 1 ? wave * L_::kBytes : 0));
-}
-
 __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(const TreeArgs a) {
   __shared__ int4 wave_tot[kPlanThreads / 256];
   __shared__ int prefix_s[kLdsPrefix + 1];
@@ -739,7 +651,7 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(const TreeArgs 
   for (int b0 = 0; b0 < batch; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int per_row, all;
-    const int count = b < batch ? tree_blocks(a, b, per_row) : 0;
+    const int count = b < batch ? tree_steps(a, b, per_row) : 0;
     const int first = running + block_exclusive_scan(count, wave_tot, &all);
     if (b < batch) {
       a.prefix[b] = first;
@@ -767,12 +679,223 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(const TreeArgs 
         if ((long)hkv * pf[mid] <= x) lo = mid; else hi = mid;
       }
       int n;
-      tree_blocks(a, lo, n);
+      tree_steps(a, lo, n);
       const int rem = (int)(x - (long)hkv * pf[lo]);
       st = make_int4(lo, ((rem / n) << 20) | (rem % n), 0, (int)min((long)per, (long)total - x));
     }
     *(int4*)(a.wstart + 4 * w) = st;
   }
+}
+
+// Folds (maximum, sum, values) of kN parts, of which `there` are there, into those of the sums.  Those past the last have weight zero (zero times
+// an infinity would not be zero).
+template <int kN>
+__device__ __forceinline__ void fold_parts(float& ref, float& l, floatx4 (&o)[4], int there, floatx2 (&x)[kN], floatx4 (&y)[kN][4]) {
+  float top = ref;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    if (i >= there) {
+      x[i] = floatx2{-INFINITY, 0.f};
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    top = fmaxf(top, x[i][0]);
+  }
+  const float base = top == -INFINITY ? 0.f : top;
+  const float keep = __builtin_amdgcn_exp2f(ref - base);
+  ref = top;
+  l *= keep;
+#pragma unroll
+  for (int i4 = 0; i4 < 4; ++i4) o[i4] *= keep;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    const float f = __builtin_amdgcn_exp2f(x[i][0] - base);
+    l += f * x[i][1];
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) o[i4] += f * y[i][i4];
+  }
+}
+
+// 32 dims of query row j of a draft, as a lane holds them of its sums.
+__device__ __forceinline__ void store_folded(const TreeArgs& a, const Draft& d, int g, int j, int D, int dt, int h2, float ref, float l, const floatx4 (&o)[4]) {
+  const RowAt at(a, d, g, j);
+  if (a.lse && dt == 0 && h2 == 0) a.lse[at.out] = ref + __builtin_amdgcn_logf(l);
+  const float inv = l > 0.f ? 1.f / l : l;
+  __bf16* dst = (__bf16*)a.out + at.out * D + dt * 32 + h2 * 4;
+#pragma unroll
+  for (int i4 = 0; i4 < 4; ++i4) {
+    bf16x4 pk;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) pk[e] = (__bf16)(o[i4][e] * inv);
+    *(bf16x4*)(dst + i4 * 8) = pk;
+  }
+}
+
+// A worker's run: a segment of a row after the other, until its steps are done.  seg(d, b, g, tile, step of the row, steps, is this all of the
+// row, where its partial goes if not)
+template <class F>
+__device__ __forceinline__ void tree_run(const TreeArgs& a, int worker, F&& seg) {
+  int4 start;
+  if (a.batch <= kWavePlanBatch) start = tree_plan_in_wave(a, worker);
+  else start = *(const int4*)(a.wstart + 4 * worker);
+  int b = __builtin_amdgcn_readfirstlane(start.x), left = __builtin_amdgcn_readfirstlane(start.w);
+  if (b < 0) return;
+  const int at = __builtin_amdgcn_readfirstlane(start.y);
+  int first = at & 0xFFFFF, r = at >> 20;
+  for (int slot = 0;; slot = 1) {
+    const tree_args_p e = tree_args();
+    const Draft d(*e, b);
+    const int tiles = tree_tiles(*e, d.n), along = e->along;
+    const int steps = tiles ? ((d.len + kBlockTokens - 1) / kBlockTokens + along - 1) / along : 0;
+    if (steps > 0) {
+      const int g = r / tiles, now = min(left, steps - first);
+      seg(d, b, g, r - g * tiles, first, now, now == steps, (size_t)worker * 2 + slot);
+      left -= now;
+      if (left <= 0) return;
+      __syncthreads();                                     // (the ring is free)
+      first = 0;
+      if (++r < tiles * e->hkv) continue;
+    }
+    r = 0;
+    ++b;
+  }
+}
+
+// Workgroups go to the XCDs in turn; workers that follow each other, whose rows may read the same K and V, have one XCD's cache in common.
+__device__ __forceinline__ int xcd_order() { return (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds); }
+
+// Small drafts.  A workgroup is a team: of four waves that have every fourth block of a segment each, without a barrier among them (up to 32 query
+// rows per KV head), or of two pairs of waves that have every second (PAIRS: up to 64, over bf16 pools).  What they come to is joined in LDS when
+// the segment ends, 32 dims to a wave, so that a cut costs one partial of a row and not four.  Measured against a worker for every wave, or for every
+// two, with its own equal run (us):
+//   64 drafts of 1 .. 8 behind 4000 tokens (32/8/128, bf16) 188 -> 163 (6.5 TB/s), 8 of them 35 -> 29, 3 of 5 .. 16 behind 2k .. 32k (pairs) 50 -> 47,
+//   64 of 6 .. 16 behind 512 .. 8k (pairs) 140 -> 140; int8 pools in pairs lose: 160 of 2 .. 4 behind 1k .. 16k (64/4/128) 240 -> 248.
+// Waves that read the blocks of a pair twice, through the caches, in place of a ring for two: 140 -> 182 (64 of 6 .. 16).
+// WHOLE: a workgroup has a row of 32 query rows to itself, without plan and merge, for tables of up to kTreeWholePages pages: 1 draft of 1 .. 8
+// behind 500 / 1000 / 2000 tokens 12.9 -> 9.6 / 15.5 -> 14.0 / 15.6 -> 23, 64 of them 29.7 -> 23.8 / 48.7 -> 42.9 / 86.7 -> 80.8.
+template <int D, int KV, bool WHOLE, bool PAIRS>
+__global__ __launch_bounds__(256, 2) void tree_team_kernel(const TreeArgs a) {
+  constexpr int kDT = D / 32;
+  using L_ = TeamLds<D, kv_is_codes(KV)>;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[L_::kBytes];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned int base = (unsigned int)(uintptr_t)&lds[0];
+  auto seg = [&](const Draft& d, int b, int g, int tile, int step0, int steps, bool whole, size_t slot) __attribute__((always_inline)) {
+    const int lane = lane_id(), n32 = lane & 31, h2 = lane >> 5;
+    constexpr int along = PAIRS ? 2 : 4;
+    const int half = PAIRS ? wave & 1 : 0, t = PAIRS ? wave >> 1 : wave;
+    const int blocks = min(steps * along, (d.len + kBlockTokens - 1) / kBlockTokens - step0 * along), n_mine = (blocks - t + along - 1) / along;
+    const int j0 = (tile + half) * kRows, rows_here = min(kRows, d.n * a.group - j0), blk0 = step0 * along + t;
+    auto leave = [&](const TreeSums<D>& own) __attribute__((always_inline)) {
+      const unsigned int mine = base + L_::of_wave(wave);
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4)
+          *lds_at<floatx4>(mine + L_::part(dt, i4, lane)) = floatx4{own.acc[dt][i4 * 4], own.acc[dt][i4 * 4 + 1], own.acc[dt][i4 * 4 + 2], own.acc[dt][i4 * 4 + 3]};
+      if (h2 == 0) *lds_at<floatx2>(mine + L_::ml(n32)) = floatx2{own.ref, own.sum};
+      if (own.undefined && n32 < rows_here)
+        add_undefined<D, KV>(d, b, g, (j0 + n32) / a.group, blk0, n_mine, along, h2,
+                             [&](int dim, floatx4 x) { *lds_at<floatx4>(mine + L_::part(dim / 32, dim / 8 % 4, lane)) += x; });
+    };
+    if constexpr (PAIRS) {
+      const TreeSums<D> own = tree_blocks_of<D, KV, 2>(a, d, b, g, j0, rows_here, blk0, n_mine, along, steps, half, base + L_::of_wave(wave & 2));
+      __syncthreads();                                      // (the partner has read the last block)
+      leave(own);
+    } else {
+      if (n_mine > 0) leave(tree_blocks_of<D, KV, 1>(a, d, b, g, j0, rows_here, blk0, n_mine, along, 0, 0, base + L_::of_wave(wave)));
+    }
+    __syncthreads();
+    const int there = min(along, blocks);
+    for (int dt = t; dt < kDT; dt += along) {
+      if (n32 >= rows_here) break;
+      floatx2 x[along];
+      floatx4 o[4], y[along][4];
+#pragma unroll
+      for (int i = 0; i < along; ++i) {
+        const int from = min(i, there - 1);
+        const unsigned int at = base + L_::of_wave(PAIRS ? from * 2 + half : from);
+        x[i] = *lds_at<const floatx2>(at + L_::ml(n32));
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = *lds_at<const floatx4>(at + L_::part(dt, i4, lane));
+      }
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) o[i4] = floatx4{0.f, 0.f, 0.f, 0.f};
+      float ref = -INFINITY, l = 0.f;
+      fold_parts(ref, l, o, there, x, y);
+      if (WHOLE || whole) {
+        store_folded(a, d, g, j0 + n32, D, dt, h2, ref, l, o);
+      } else {
+        const size_t part = slot * a.tile_parts + half;
+        float* const dst = a.partial_o + part * (kRows * D) + (dt * 256 + lane) * 4;
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) *(floatx4*)(dst + i4 * 256) = o[i4];
+        if (dt == 0 && h2 == 0) *(floatx2*)(a.partial_ml + (part * kRows + n32) * 2) = floatx2{ref, l};
+      }
+    }
+  };
+  if constexpr (WHOLE) {
+    const int row = xcd_order(), tile = row % a.row_tiles, g = row / a.row_tiles % a.hkv, b = row / a.row_tiles / a.hkv;
+    if (b >= a.batch) return;
+    const Draft d(a, b);
+    if (tile >= tree_tiles(a, d.n) || d.len <= 0) return;
+    seg(d, b, g, tile, 0, (d.len + 4 * kBlockTokens - 1) / (4 * kBlockTokens), true, 0);
+  } else {
+    tree_run(a, xcd_order(), seg);
+  }
+}
+
+// Larger drafts: a worker is a workgroup of W waves that share a ring, 32 query rows each.
+template <int D, int KV, int W>
+__global__ __launch_bounds__(64 * W, 2) void tree_wide_kernel(const TreeArgs a) {
+  constexpr int kDT = D / 32;
+  using L_ = TreeLds<D, kv_is_codes(KV), W>;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[L_::kRing];
+  const int lane = lane_id(), n32 = lane & 31, h2 = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  tree_run(a, xcd_order(), [&](const Draft& d, int b, int g, int tile, int blk0, int n, bool whole, size_t slot) __attribute__((always_inline)) {
+    const int j0 = (tile * W + wave) * kRows, rows_here = min(kRows, d.n * a.group - j0);
+    const TreeSums<D> own = tree_blocks_of<D, KV, W>(a, d, b, g, j0, rows_here, blk0, n, 1, n, wave, (unsigned int)(uintptr_t)&lds[0]);
+    if (n32 >= rows_here) return;
+    const tree_args_p e = tree_args();
+    const RowAt at(*e, d, g, j0 + n32);
+    const size_t part = slot * W + wave;
+    if (whole) {
+      // (nothing seen: a row of zeros)
+      const float inv = own.sum > 0.f ? 1.f / own.sum : own.sum;
+      if (e->lse && h2 == 0) e->lse[at.out] = own.ref + __builtin_amdgcn_logf(own.sum);
+      __bf16* dst = (__bf16*)e->out + at.out * D + h2 * 4;
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          bf16x4 pk;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pk[i] = (__bf16)(own.acc[dt][i4 * 4 + i] * inv);
+          *(bf16x4*)(dst + dt * 32 + i4 * 8) = pk;
+        }
+    } else {
+      float* dst = e->partial_o + part * (kRows * D) + lane * 4;
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4)
+          *(floatx4*)(dst + (dt * 4 + i4) * 256) = floatx4{own.acc[dt][i4 * 4], own.acc[dt][i4 * 4 + 1], own.acc[dt][i4 * 4 + 2], own.acc[dt][i4 * 4 + 3]};
+      if (h2 == 0) *(floatx2*)(e->partial_ml + (part * kRows + n32) * 2) = floatx2{own.ref, own.sum};
+    }
+    if (own.undefined)                                       // to the values that this lane has just stored
+      add_undefined<D, KV>(d, b, g, at.node, blk0, n, 1, h2, [&](int dim, floatx4 x) {
+        if (whole) {
+          bf16x4* const o = (bf16x4*)((__bf16*)e->out + at.out * D + dim);
+          bf16x4 y = *o;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = (__bf16)((float)y[i] + x[i]);
+          *o = y;
+        } else {
+          *(floatx4*)(e->partial_o + part * (kRows * D) + (dim / 8 * 64 + lane) * 4) += x;
+        }
+      });
+  });
 }
 
 // Merge of the partials that runs left of rows they did not cover alone, as in combine.hip: one wave per (row, 32 query rows, 32 dims),
@@ -804,33 +927,6 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) 
 #pragma unroll
   for (int i4 = 0; i4 < 4; ++i4) o[i4] = floatx4{0.f, 0.f, 0.f, 0.f};
   float ref = -INFINITY, l = 0.f;
-  // folds (maximum, sum, values) of kN things into the sums; those past the last have weight zero (zero times an infinity would not be zero)
-  auto fold = [&](auto n_c, int there, floatx2* x, floatx4 (*y)[4]) __attribute__((always_inline)) {
-    constexpr int kN = decltype(n_c)::value;
-    float top = ref;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      if (i >= there) {
-        x[i] = floatx2{-INFINITY, 0.f};
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = floatx4{0.f, 0.f, 0.f, 0.f};
-      }
-      top = fmaxf(top, x[i][0]);
-    }
-    const float base = top == -INFINITY ? 0.f : top;
-    const float keep = __builtin_amdgcn_exp2f(ref - base);
-    ref = top;
-    l *= keep;
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) o[i4] *= keep;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float f = __builtin_amdgcn_exp2f(x[i][0] - base);
-      l += f * x[i][1];
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) o[i4] += f * y[i][i4];
-    }
-  };
   constexpr int kN = 4;
   const int step = TOGETHER ? kWaves : 1, from = TOGETHER ? wave : 0;
   if (ok)
@@ -845,7 +941,7 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) 
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) y[i][i4] = *(const floatx4*)(a.partial_o + part * (kRows * D) + ((dt * 4 + i4) * 64 + lane) * 4);
       }
-      fold(std::integral_constant<int, kN>{}, (pieces - s0 + step - 1) / step, x, y);
+      fold_parts(ref, l, o, (pieces - s0 + step - 1) / step, x, y);
     }
   if constexpr (TOGETHER) {
 #pragma unroll
@@ -862,25 +958,36 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(const TreeArgs a) 
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) y[w - 1][i4] = *(const floatx4*)sum_s[w][i4][lane];
     }
-    fold(std::integral_constant<int, kWaves - 1>{}, kWaves - 1, x, y);
+    fold_parts(ref, l, o, kWaves - 1, x, y);
   }
-  if (!ok) return;
-  const RowAt at(a, d, g, j0 + n32);
-  if (a.lse && dt == 0 && h2 == 0) a.lse[at.out] = ref + __builtin_amdgcn_logf(l);
-  const float inv = l > 0.f ? 1.f / l : l;
-  __bf16* dst = (__bf16*)a.out + at.out * D + dt * 32 + h2 * 4;
-#pragma unroll
-  for (int i4 = 0; i4 < 4; ++i4) {
-    bf16x4 pk;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) pk[e] = (__bf16)(o[i4][e] * inv);
-    *(bf16x4*)(dst + i4 * 8) = pk;
+  if (ok) store_folded(a, d, g, j0 + n32, D, dt, h2, ref, l, o);
+}
+
+template <class F>
+hipError_t by_kind(KvKind kv, F&& f) {
+  switch (kv) {
+    case kKvBf16: return f(std::integral_constant<int, kKvBf16>{});
+    case kKvFp8: return f(std::integral_constant<int, kKvFp8>{});
+    case kKvFp8Head: return f(std::integral_constant<int, kKvFp8Head>{});
+    case kKvInt8Head: return f(std::integral_constant<int, kKvInt8Head>{});
   }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, hipStream_t s) {
+  if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
+  if (a.workers == 0) {
+    const int64_t rows = (int64_t)a.batch * a.hkv * a.row_tiles;
+    const dim3 grid((unsigned)((rows + kXcds - 1) / kXcds * kXcds));
+    return by_kind(kv, [&](auto kind) {
+      constexpr int KV = decltype(kind)::value;
+      if (head_dim == 128) hipLaunchKernelGGL((tree_team_kernel<128, KV, true, false>), grid, dim3(kThreads), 0, s, a);
+      else hipLaunchKernelGGL((tree_team_kernel<64, KV, true, false>), grid, dim3(kThreads), 0, s, a);
+      return hipGetLastError();
+    });
+  }
   if (a.batch > kWavePlanBatch) {
     hipLaunchKernelGGL(tree_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
@@ -888,36 +995,27 @@ hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, hipStrea
   }
   const int64_t units = (int64_t)a.batch * a.hkv * a.row_tiles * a.tile_parts * (head_dim / 32);
   const bool together = units <= kMergeTogether;
-  const dim3 merge_grid((unsigned)(together ? units : (units + kWaves - 1) / kWaves));
-  auto launch = [&](auto d, auto kind, auto w) {
-    constexpr int W = decltype(w)::value;
-    hipLaunchKernelGGL((tree_mfma_kernel<decltype(d)::value, decltype(kind)::value, W>), dim3(a.workers / (W == 1 ? 4 : 1)), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
+  const dim3 grid((unsigned)a.workers), merge_grid((unsigned)(together ? units : (units + kWaves - 1) / kWaves));
+  auto launch_two = [&](auto d, auto kind) {
+    constexpr int D = decltype(d)::value, KV = decltype(kind)::value;
+    if constexpr (kv_is_codes(KV)) hipLaunchKernelGGL((tree_wide_kernel<D, KV, 2>), grid, dim3(128), 0, s, a);
+    else hipLaunchKernelGGL((tree_team_kernel<D, KV, false, true>), grid, dim3(kThreads), 0, s, a);
+  };
+  auto launch = [&](auto d, auto kind) {
+    constexpr int D = decltype(d)::value, KV = decltype(kind)::value;
+    if (a.tile_parts == 1) hipLaunchKernelGGL((tree_team_kernel<D, KV, false, false>), grid, dim3(kThreads), 0, s, a);
+    else if (a.tile_parts == 2) launch_two(d, kind);
+    else if (a.tile_parts == 4) hipLaunchKernelGGL((tree_wide_kernel<D, KV, 4>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((tree_wide_kernel<D, KV, 8>), grid, dim3(512), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (together) hipLaunchKernelGGL((tree_merge_kernel<decltype(d)::value, true>), merge_grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((tree_merge_kernel<decltype(d)::value, false>), merge_grid, dim3(kThreads), 0, s, a);
+    if (together) hipLaunchKernelGGL((tree_merge_kernel<D, true>), merge_grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((tree_merge_kernel<D, false>), merge_grid, dim3(kThreads), 0, s, a);
     return hipGetLastError();
   };
-  auto of_tiles = [&](auto d, auto kind) {
-    switch (a.tile_parts) {
-      case 1: return launch(d, kind, std::integral_constant<int, 1>{});
-      case 2: return launch(d, kind, std::integral_constant<int, 2>{});
-      case 4: return launch(d, kind, std::integral_constant<int, 4>{});
-      case 8: return launch(d, kind, std::integral_constant<int, 8>{});
-    }
-    return hipErrorInvalidValue;
-  };
-  auto of_kind = [&](auto kind) {
-    return head_dim == 128 ? of_tiles(std::integral_constant<int, 128>{}, kind) : of_tiles(std::integral_constant<int, 64>{}, kind);
-  };
-  if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
-  switch (kv) {
-    case kKvBf16: return of_kind(std::integral_constant<int, kKvBf16>{});
-    case kKvFp8: return of_kind(std::integral_constant<int, kKvFp8>{});
-    case kKvFp8Head: return of_kind(std::integral_constant<int, kKvFp8Head>{});
-    case kKvInt8Head: return of_kind(std::integral_constant<int, kKvInt8Head>{});
-  }
-  return hipErrorInvalidValue;
+  return by_kind(kv, [&](auto kind) {
+    return head_dim == 128 ? launch(std::integral_constant<int, 128>{}, kind) : launch(std::integral_constant<int, 64>{}, kind);
+  });
 }
 
 }  // namespace rollattn
