@@ -259,6 +259,8 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
     if (in == 0) {
       const int k = sent >> 5;
       pid_vec = k == 0 ? load_window(0) : pid_next;
+      // (here the compiler waits for it; left to the uses below it would wait in front of every block, and for all loads under way)
+      asm volatile("" : "+v"(pid_vec));
       pid_next = load_window(k + 1);
     }
     p_lim = d.len - (blk0 + sent * stride) * kBlockTokens;
