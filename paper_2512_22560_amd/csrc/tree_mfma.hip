@@ -222,7 +222,11 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
   };
   auto dma16 = [&](const unsigned char* base, unsigned int off, unsigned int dst) __attribute__((always_inline)) {
     const unsigned int m0 = __builtin_amdgcn_readfirstlane(dst);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(m0), "v"(off), "s"(base) : "memory");
+// (streamed: read once.  The tiles of larger drafts follow each other through the same blocks, and find some in the caches: 24 drafts of 24 .. 72
+    // behind 1k .. 8k (64/4/128) 167 -> 161 us over bf16, 343 -> 321 over int8 pools; of one tile, 9 .. 16, 77 -> 78 and 123 -> 124.  Hint taken from
+    // the smaller ones, 64 of 6 .. 16 behind 512 .. 8k (32/8/128): 140 -> 156.)
+    if constexpr (W < 8) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(m0), "v"(off), "s"(base) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(base) : "memory");
   };
   // This wave's share of a tile of one pool: row row0 + lane / chunks of the block per load.  What a lane reads of a tile is the same for every
   // whole block; of a row's ragged last one, rows at or past L_b read its last one again.
