@@ -981,7 +981,7 @@ int attn_tree(const rollattn_desc* desc, const void* q, const int32_t* q_lens, c
   if (desc->q_dtype != ROLLATTN_F32) {
     // a worker's start packs the row into 11 bits and the block into 20; blocks are counted in 32 bits, as are the merge's waves
     const int64_t rows = (int64_t)desc->num_kv_heads * w.tiles, blocks = (int64_t)desc->max_pages_per_seq / 2 + 1;
-    if (rows > 2047 || blocks > (1 << 20) || desc->batch * rows * blocks > INT32_MAX || desc->batch * rows * 8 > INT32_MAX) return ROLLATTN_ESHAPE;
+    if (rows > 2047 || blocks > (1 << 20) || desc->batch * rows * blocks > INT32_MAX || desc->batch * rows * 32 > INT32_MAX) return ROLLATTN_ESHAPE;
   }
   TreeArgs a{};
   char* base = (char*)workspace;

@@ -68,17 +68,19 @@ __device__ __forceinline__ unsigned int seen_bits(const uint64_t* words, int n_w
 
 // The sign bits of the elements of a word of a pool that are no numbers (infinite and undefined bf16 values, whose exponent is all ones; the
 // undefined code of E4M3): the sum carries into them.
+constexpr int kHalves = -1;               // (codes that have become f16)
 template <int KV>
 __device__ __forceinline__ uint32_t undefined(uint32_t w) {
-  if constexpr (KV == kKvBf16) return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  if constexpr (KV == kHalves) return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+  else if constexpr (KV == kKvBf16) return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
   else if constexpr (KV == kKvInt8Head) return 0;
   else return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
 }
 // The word with zeros in the place of those.
 template <int KV>
 __device__ __forceinline__ uint32_t defined(uint32_t w) {
-  const uint32_t met = undefined<KV>(w) >> (KV == kKvBf16 ? 15 : 7);
-  return w & ~(met * (KV == kKvBf16 ? 0xffffu : 0xffu));
+  const uint32_t met = undefined<KV>(w) >> (KV == kKvBf16 || KV == kHalves ? 15 : 7);
+  return w & ~(met * (KV == kKvBf16 || KV == kHalves ? 0xffffu : 0xffu));
 }
 
 // The kernel's arguments, read anew from their segment: what only a row's start and end need is not kept in scalar registers over its blocks
@@ -118,7 +120,14 @@ template <int D, bool FP8, int W>
 struct TreeLds {
   static constexpr int kSlots = W == 1 ? (FP8 ? 2 : 1) : W == 2 ? (FP8 ? 4 : 2) : 4;
   static constexpr int kTile = Geo<D, FP8>::kTileBytes, kScales = FP8 ? 256 : 0;   // scales of a block's two pages: K's, V's (the other lanes' are copies)
-  static constexpr int kRing = kSlots * (2 * kTile + W * kScales);
+  // Codes that eight waves share are widened once, into one of two tiles of 16-bit operands, and not by each wave for itself: 64 drafts of 24 .. 72
+  // behind 1k .. 8k (64/4/128) 740 -> 559 us over int8 and 637 -> 542 over E4M3 pools, of 9 .. 16 261 -> 190 and 227 -> 186.  Four waves gain
+  // nothing (of 5 .. 8, 121 -> 120 and 102 -> 118), nor do heads of 64, whose rows need more LDS reads to a product (of 40 .. 64 with 8/2/64
+  // over E4M3 87 -> 103).
+  static constexpr bool kWidens = FP8 && W == 8 && D == 128;
+  static constexpr int kWide = kWidens ? Geo<D, false>::kTileBytes : 0, kCodes = kSlots * (2 * kTile + W * kScales), kRing = kCodes + 4 * kWide;
+  static __device__ __forceinline__ unsigned int wide_k(int at) { return kCodes + at * kWide; }
+  static __device__ __forceinline__ unsigned int wide_v(int at) { return kCodes + (2 + at) * kWide; }
   static __device__ __forceinline__ unsigned int k(int slot) { return slot * kTile; }
   static __device__ __forceinline__ unsigned int v(int slot) { return (kSlots + slot) * kTile; }
   static __device__ __forceinline__ unsigned int scales(int slot, int wave) { return 2 * kSlots * kTile + (slot * W + wave) * kScales; }
@@ -183,7 +192,8 @@ struct TreeSums {
 // Loads.  W = 1: the tiles of block i + slots go into the places of block i, K's as soon as the first product has read them and V's behind
 // the second; no barriers.  Else each wave loads its share of a block, waits for its own loads and meets the others at one barrier per block:
 // behind it the block is there, and the place of the block before is free for the one that is slots - 1 ahead.  rounds: barriers, as many for
-// all waves of the workgroup (n_mine or more).
+// all waves of the workgroup (n_mine or more).  Where codes are widened once for all, the next block is there, too, and becomes operands, each
+// wave its share, in the tile that the block before has left.
 // HBM -> LDS without a register stop: lane l's 16 bytes land at M0 + 16 l, so a row's chunks are swizzled by the address a lane
 // reads from.  The compiler does not see these loads as loads; they are awaited by count: vector-memory counts go down in order, so
 // with N of these loads sent after the ones that are waited for, no more than N outstanding operations of any kind means that those have
@@ -200,6 +210,8 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
   using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;  // ... and of the second
   using op = std::conditional_t<HEAD, _Float16, __bf16>;
   using G_ = Geo<D, FP8>;
+  constexpr bool kWidens = L_::kWidens, RAW8 = FP8 && !kWidens;   // RAW8: operands are codes in LDS
+  using O_ = Geo<D, RAW8>;
   // this wave's loads of a block: of each pool's tile its share, or where there are more waves than a tile has loads, of one pool's tile one
   // (where there are more than both have, some twice: the same bytes to the same place); its copy of the scales
   constexpr int kShare = G_::kLoads >= W ? G_::kLoads / W : 1;
@@ -342,8 +354,8 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
     const __bf16* qrow = (const __bf16*)e->q + at.out * D;
 #pragma unroll
     for (int kk = 0; kk < kKK; ++kk) {
-      // FP8: 16-byte K chunks hold 16 dims; step 2p+e uses bytes e*8.. of chunk p*2+h2
-      uint4 v = *(const uint4*)(qrow + (FP8 ? ((kk >> 1) * 2 + h2) * 16 + (kk & 1) * 8 : kk * 16 + h2 * 8));
+      // RAW8: 16-byte K chunks hold 16 dims; step 2p+e uses bytes e*8.. of chunk p*2+h2
+      uint4 v = *(const uint4*)(qrow + (RAW8 ? ((kk >> 1) * 2 + h2) * 16 + (kk & 1) * 8 : kk * 16 + h2 * 8));
       const uint32_t sign = flip ? 0x80008000u : 0u;
       v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign;
       qop[kk] = __builtin_bit_cast(kx8, v);     // (int8: as it came, until all of the row is there)
@@ -375,21 +387,21 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
   floatx16 s;
   // ---- S^T = K Q^T.  All operands are on their way before the first product: the products hang together and would each wait for a trip to
   // the LDS.
-  constexpr int kKeyReads = FP8 ? kKK / 2 : kKK;
+  constexpr int kKeyReads = RAW8 ? kKK / 2 : kKK;
   uint4_v k_raw[kKeyReads];
   auto read_keys = [&](int slot) __attribute__((always_inline)) {
     const int t = (n32 & 16) + tau(n32 & 15);
-    const unsigned int rowp = lds + L_::k(slot) + t * G_::kRowBytes;
-    const int key = tree_key_k<D, FP8>(t);
+    const unsigned int rowp = lds + (kWidens ? L_::wide_k(slot & 1) : L_::k(slot)) + t * O_::kRowBytes;
+    const int key = tree_key_k<D, RAW8>(t);
 #pragma unroll
-    for (int i = 0; i < kKeyReads; ++i) k_raw[i] = *lds_at<const uint4_v>(rowp + (((i * 2 + h2) ^ key) & (G_::kChunks - 1)) * 16);
+    for (int i = 0; i < kKeyReads; ++i) k_raw[i] = *lds_at<const uint4_v>(rowp + (((i * 2 + h2) ^ key) & (O_::kChunks - 1)) * 16);
   };
   auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int i = 0; i < kKeyReads; ++i) {
-      if constexpr (FP8) {
+      if constexpr (RAW8) {
         s = mfma32(widen_k8<KV>(k_raw[i][0], k_raw[i][1]), qop[2 * i], s);
         s = mfma32(widen_k8<KV>(k_raw[i][2], k_raw[i][3]), qop[2 * i + 1], s);
       } else {
@@ -489,26 +501,26 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
     }
   };
   // ---- O^T += V^T P^T : A = V^T tile (32 dims x 16 tokens) read transposed from LDS, in front of the softmax
-  using raw_v = std::conditional_t<FP8, intx2, bf16x8>;
+  using raw_v = std::conditional_t<RAW8, intx2, bf16x8>;
   raw_v v_raw[2][kDT];
   auto read_values = [&](int slot) __attribute__((always_inline)) {
-    const unsigned int v_at = lds + L_::v(slot);
+    const unsigned int v_at = lds + (kWidens ? L_::wide_v(slot & 1) : L_::v(slot));
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) {
-        if constexpr (FP8) {
+        if constexpr (RAW8) {
           typedef __attribute__((address_space(3))) intx2 lds_i2;
           const int t = ks * 16 + h2 * 8 + ((lane & 15) >> 1);
-          const int col = ((dt * 2 + ((lane >> 4) & 1)) ^ tree_key_v<true>(t)) & (G_::kChunks - 1);
-          v_raw[ks][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2*)(uintptr_t)(v_at + t * G_::kRowBytes + col * 16 + (lane & 1) * 8));
+          const int col = ((dt * 2 + ((lane >> 4) & 1)) ^ tree_key_v<true>(t)) & (O_::kChunks - 1);
+          v_raw[ks][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2*)(uintptr_t)(v_at + t * O_::kRowBytes + col * 16 + (lane & 1) * 8));
         } else {
           typedef __attribute__((address_space(3))) shortx4 lds_s4;
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
             const int j = lane & 15, t = ks * 16 + h2 * 8 + hf * 4 + (j >> 2);
-            const int col = ((dt * 4 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1)) ^ tree_key_v<false>(t)) & (G_::kChunks - 1);
-            const shortx4 raw = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)(v_at + t * G_::kRowBytes + col * 16 + (j & 1) * 8));
+            const int col = ((dt * 4 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1)) ^ tree_key_v<false>(t)) & (O_::kChunks - 1);
+            const shortx4 raw = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)(v_at + t * O_::kRowBytes + col * 16 + (j & 1) * 8));
             const bf16x4 h4 = __builtin_bit_cast(bf16x4, raw);
             v_raw[ks][dt][hf * 4 + 0] = h4[0]; v_raw[ks][dt][hf * 4 + 1] = h4[1]; v_raw[ks][dt][hf * 4 + 2] = h4[2]; v_raw[ks][dt][hf * 4 + 3] = h4[3];
           }
@@ -520,14 +532,14 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int dt = 0; dt < kDT; ++dt) {
-        if constexpr (FP8) acc[dt] = mfma32(widen_v8<KV>((uint32_t)v_raw[ks][dt][0], (uint32_t)v_raw[ks][dt][1]), pop[ks], acc[dt]);
-        else acc[dt] = mfma32(v_raw[ks][dt], pop[ks], acc[dt]);
+        if constexpr (RAW8) acc[dt] = mfma32(widen_v8<KV>((uint32_t)v_raw[ks][dt][0], (uint32_t)v_raw[ks][dt][1]), pop[ks], acc[dt]);
+        else acc[dt] = mfma32(__builtin_bit_cast(opx8, v_raw[ks][dt]), pop[ks], acc[dt]);
       }
   };
   // Where the values hold any that is no number, zeros take their places, and those of the segment are added to what is stored of it.
   auto without_undefined = [&]() __attribute__((always_inline)) {
     if constexpr (!INT8) {
-      constexpr int kWords = FP8 ? 2 : 4;
+      constexpr int kWords = RAW8 ? 2 : 4, kAs = RAW8 ? KV : HEAD ? kHalves : kKvBf16;
       typedef unsigned int words_v __attribute__((ext_vector_type(kWords)));
       uint32_t any = 0;
 #pragma unroll
@@ -536,7 +548,7 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
         for (int dt = 0; dt < kDT; ++dt) {
           const words_v w = __builtin_bit_cast(words_v, v_raw[ks][dt]);
 #pragma unroll
-          for (int i = 0; i < kWords; ++i) any |= undefined<KV>(w[i]);
+          for (int i = 0; i < kWords; ++i) any |= undefined<kAs>(w[i]);
         }
       if (__builtin_amdgcn_ballot_w64(any != 0)) {
         own.undefined = true;
@@ -546,9 +558,45 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
           for (int dt = 0; dt < kDT; ++dt) {
             words_v w = __builtin_bit_cast(words_v, v_raw[ks][dt]);
 #pragma unroll
-            for (int i = 0; i < kWords; ++i) w[i] = defined<KV>(w[i]);
+            for (int i = 0; i < kWords; ++i) w[i] = defined<kAs>(w[i]);
             v_raw[ks][dt] = __builtin_bit_cast(raw_v, w);
           }
+      }
+    }
+  };
+  // ---- codes of 16 dims of a row to operands: each wave its share of a block
+  constexpr int kPieces = kWidens ? 2 * kBlockTokens * (D / 16) : 0, kEach = kWidens ? (kPieces + 64 * W - 1) / (64 * W) : 0;
+  uint4_v codes[kWidens ? kEach : 1];
+  auto piece = [&](int n, int& row, int& c) __attribute__((always_inline)) {       // (whether there is one, and it is of V)
+    const int at = n * 64 * W + wave * 64 + lane;
+    row = at / (D / 16) % kBlockTokens;
+    c = at % (D / 16);
+    return at < kPieces / 2 ? 0 : at < kPieces ? 1 : 2;
+  };
+  auto read_codes = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+      int row, c;
+      const int which = piece(n, row, c);
+      const int key = which == 1 ? tree_key_v<true>(row) : tree_key_k<D, true>(row);
+      if (which < 2) codes[n] = *lds_at<const uint4_v>(lds + (which == 1 ? L_::v(slot) : L_::k(slot)) + row * G_::kRowBytes + ((c ^ key) & (G_::kChunks - 1)) * 16);
+    }
+  };
+  auto write_wide = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+      int row, c;
+      const int which = piece(n, row, c);
+      if (which == 0) {
+        const unsigned int at = lds + L_::wide_k(slot & 1) + row * O_::kRowBytes;
+        const int key = tree_key_k<D, false>(row);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) *lds_at<uint4_v>(at + (((c * 2 + e) ^ key) & (O_::kChunks - 1)) * 16) = __builtin_bit_cast(uint4_v, widen_k8<KV>(codes[n][2 * e], codes[n][2 * e + 1]));
+      } else if (which == 1) {
+        const unsigned int at = lds + L_::wide_v(slot & 1) + row * O_::kRowBytes;
+        const int key = tree_key_v<false>(row);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) *lds_at<uint4_v>(at + (((c * 2 + e) ^ key) & (O_::kChunks - 1)) * 16) = __builtin_bit_cast(uint4_v, widen_v8<KV>(codes[n][2 * e], codes[n][2 * e + 1]));
       }
     }
   };
@@ -569,6 +617,12 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
   constexpr std::integral_constant<int, kSlots - (W == 1 ? 1 : 2)> ahead_c{};   // blocks behind the one in work that are under way
   constexpr std::integral_constant<int, 0> c0{};
   int slot = 0, blk = blk0;
+  if constexpr (kWidens) {
+    await(n_mine >= kSlots - 1, std::integral_constant<int, kSlots - 2>{}, c0);
+    asm volatile("s_barrier" ::: "memory");
+    read_codes(0);
+    write_wide(0);
+  }
   for (int i = n_mine, rest = W == 1 ? n_mine : rounds; rest > 0; --i, --rest, blk += stride) {               // (blocks that are left)
     const bool edge = blk >= edge_blk;
     if constexpr (W == 1) {
@@ -594,9 +648,16 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
         issue_v(slot);
       }
     } else {
-      if (i > 0) await(i >= kSlots - 1, ahead_c, c0);
+      if (i > 0) await(i >= kSlots - 1, std::integral_constant<int, kSlots - 2 - (kWidens ? 1 : 0)>{}, c0);
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (sent < n_mine) issue(slot == 0 ? kSlots - 1 : slot - 1);
+      const int next = slot + 1 == kSlots ? 0 : slot + 1;
+      if constexpr (kWidens) {
+        if (i > 1) {
+          read_codes(next);
+          write_wide(next);
+        }
+      }
       if (rows_here > 0 && i > 0) {
         read_keys(slot);
         __builtin_amdgcn_sched_barrier(0);
