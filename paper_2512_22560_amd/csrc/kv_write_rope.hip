@@ -306,13 +306,14 @@ __device__ __forceinline__ void turn_queries(const RopeWriteArgs& a, unsigned in
       // of the rows under way each lane works out one's root and quotient, 25 instructions that all lanes of a row would go through alike
       float mine = 0.f;
 #pragma unroll
-      for (int i = 0; i < kKeep; ++i) {
-        float x[8];
-        to_float<SRC_BYTES>(r[i], x);
-        const float mean = mean_square<D>(x);
-        mine = col == i ? mean : mine;
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int i = 0; i < kKeep; ++i)
+        if (h + i * side < heads) {                 // (a wave of few tokens has one row a lane, and waits for no others' sums)
+          float x[8];
+          to_float<SRC_BYTES>(r[i], x);
+          const float mean = mean_square<D>(x);
+          mine = col == i ? mean : mine;
+          __builtin_amdgcn_sched_barrier(0);
+        }
       // (widened once more below: kept as floats, the rows would take twice the registers)
 #pragma unroll
       for (int i = 0; i < kKeep; ++i) asm volatile("" : "+v"(r[i].lo), "+v"(r[i].hi));
@@ -407,18 +408,28 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
           if (h - head0 + i * side < hkv) r[i] = fetch_row(min(h + i * side, hkv - 1));
+        auto to = [&](int i) { return tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES; };
+        if (NORM && pool == 0) {
+          // (roots as for queries)
+          float mine = 0.f;
 #pragma unroll
-        for (int i = 0; i < kKeep; ++i)
-          if (h + i * side < hkv) {
-            unsigned char* const dst = tile + ((size_t)(h + i * side) * kPageSize + s0 + slot) * D * SRC_BYTES;
-            if (NORM && pool == 0) {
+          for (int i = 0; i < kKeep; ++i)
+            if (h - head0 + i * side < hkv) {
               float x[8];
               to_float<SRC_BYTES>(r[i], x);
-              store<SRC_BYTES, false>(a, lane, turn, weights, root_inverse(mean_square<D>(x), a.eps), dst, r[i]);
-            } else {
-              store<SRC_BYTES, false>(a, lane, turn, Weights<false>{}, 0.f, dst, r[i]);
+              const float mean = mean_square<D>(x);
+              mine = col == i ? mean : mine;
             }
-          }
+          const float inverse = root_inverse(mine, a.eps);
+          static_for<kKeep>([&](auto i) __attribute__((always_inline)) {
+            const float of_row = from_lane<D, decltype(i)::value>(inverse);
+            if (h + i * side < hkv) store<SRC_BYTES, false>(a, lane, turn, weights, of_row, to(i), r[i]);
+          });
+        } else {
+#pragma unroll
+          for (int i = 0; i < kKeep; ++i)
+            if (h + i * side < hkv) store<SRC_BYTES, false>(a, lane, turn, Weights<false>{}, 0.f, to(i), r[i]);
+        }
       }
   } else {
     static_assert(SRC_BYTES == 2, "codes are made of bf16 rows");
