@@ -530,21 +530,34 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
         float before = 0.f;
         if (s0 && (int)threadIdx.x < count) before = scales[r0 + threadIdx.x];
         if (r0 || another) __syncthreads();
-        float inverse[kRound] = {-1.f, -1.f, -1.f, -1.f};
+        float inverse = -1.f;                   // (norms: of row `col` of this lane's rows)
         Raw<SRC_BYTES> keep[kRound] = {};       // (what is not loaded is nothing: else the rows of the round before, all the way)
         if (!idle) {
 #pragma unroll
           for (int k = 0; k < kRound; ++k)
             if (k * side < count) keep[k] = fetch_row(r0 + min(head0 + k * side, count - 1));
+          if (NORM && pool == 0) {
+            // (roots as for queries)
+            float mine = 0.f;
 #pragma unroll
-          for (int k = 0; k < kRound; ++k)
+            for (int k = 0; k < kRound; ++k)
+              if (k * side < count) {
+                float x[8];
+                to_float<2>(keep[k], x);
+                const float mean = mean_square<D>(x);
+                mine = col == k ? mean : mine;
+              }
+            inverse = root_inverse(mine, a.eps);
+          }
+          static_for<kRound>([&](auto k) __attribute__((always_inline)) {
             if (k * side < count) {
-              float x[8];
-              rotated(keep[k], x, inverse[k]);
+              float x[8], of_row = NORM ? from_lane<D, decltype(k)::value>(inverse) : 0.f;
+              rotated(keep[k], x, of_row);
               const float m = largest(x);
               if (col == 0) row_top[k][group] = m;
               __builtin_amdgcn_sched_barrier(0);
             }
+          });
         }
         __syncthreads();
         if ((int)threadIdx.x < count) {
@@ -562,12 +575,12 @@ __global__ __launch_bounds__(kThreads) void kv_write_rope_kernel(const RopeWrite
           // (turned once more: kept as floats over the barriers, rows would take twice the registers)
 #pragma unroll
           for (int k = 0; k < kRound; ++k) asm volatile("" : "+v"(keep[k].lo), "+v"(keep[k].hi));
-#pragma unroll
-          for (int k = 0; k < kRound; ++k)
+          static_for<kRound>([&](auto k) __attribute__((always_inline)) {
             if (head0 + k * side < count) {
-              emit(r0 + head0 + k * side, keep[k], new_scale[head0 + k * side], inverse[k]);
+              emit(r0 + head0 + k * side, keep[k], new_scale[head0 + k * side], NORM ? from_lane<D, decltype(k)::value>(inverse) : 0.f);
               __builtin_amdgcn_sched_barrier(0);
             }
+          });
         }
       }
     } else {
