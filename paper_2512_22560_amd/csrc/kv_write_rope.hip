@@ -97,7 +97,7 @@ struct Turn {
 // Every lane of the row takes part and has the mean.
 // Norms leave the write bound by what it was bound by: 256 trajectories of 3 .. 17 tokens (64/4/128, E4M3, 79 MB) 19.8 us, 64 chunks of 64 .. 1024
 // (32/8/128, int8, 507 MB) 104 to 107, 4.8 TB/s; with every lane of a row at its root and quotient, and keys normalised anew in the second pass,
-// 21.3 and 112.
+// 21.3 and 112.  5 drafts of 5 .. 24 (32/8/128, bf16) 5.7, of which the host's part is 5.
 template <int D>
 __device__ __forceinline__ float mean_square(const float (&x)[8]) {
 #pragma clang fp contract(off)
