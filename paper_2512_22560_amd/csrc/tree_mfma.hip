@@ -148,16 +148,17 @@ template <class T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(unsigned int at) { return (__attribute__((address_space(3))) T*)(uintptr_t)at; }
 
 // Values of a segment's blocks that are no numbers, which its sums leave out, to the row of `node`, where that sees them: add(dim, four of them).
-// Rare, and one token after the other.
+// They were left out of every block that ends behind the prefix, so of the last cached tokens, too, which all rows see.  Rare, and one token
+// after the other.
 template <int D, int KV, class F>
 __device__ __forceinline__ void add_undefined(const Draft& d, int b, int g, int node, int blk0, int n, int stride, int h2, F&& add) {
   const tree_args_p e = tree_args();
   const uint64_t* const words = e->mask + (size_t)(d.off + node) * e->mask_words;
   const int prefix = d.len - d.n;
   for (int blk = blk0; n > 0; --n, blk += stride)
-    for (int t = max(prefix, blk * kBlockTokens); t < min(d.len, (blk + 1) * kBlockTokens); ++t) {
+    for (int t = max(prefix / kBlockTokens, blk) * kBlockTokens; t < min(d.len, (blk + 1) * kBlockTokens); ++t) {
       const int rel = t - prefix;
-      if (rel >= 64 * e->mask_words || !(words[rel >> 6] >> (rel & 63) & 1)) continue;
+      if (rel >= 0 && (rel >= 64 * e->mask_words || !(words[rel >> 6] >> (rel & 63) & 1))) continue;
       const size_t row = ((size_t)e->page_table[(size_t)b * e->max_pages + t / kPageSize] * e->hkv + g) * kPageSize + t % kPageSize;
       for (int dim = h2 * 4; dim < D; dim += 8) {
         floatx4 x;
