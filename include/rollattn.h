@@ -318,6 +318,7 @@ int attn_tree_mask(const int32_t *parents, const int32_t *q_lens, const int32_t 
 int attn_tree(const rollattn_desc *desc, const void *q, const int32_t *q_lens, const int32_t *q_offsets, int32_t total_q, int32_t max_q_len,
               const uint64_t *tree_mask, int32_t mask_words, const void *k_pages, const void *v_pages, const int32_t *page_table,
               const int32_t *ctx_lens, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+/* Never less for more: not in total_q, max_q_len, batch or max_pages_per_seq.  A workspace made for the largest step serves the smaller ones. */
 size_t rollattn_tree_workspace_bytes(const rollattn_desc *desc, int32_t total_q, int32_t max_q_len);
 
 /* The accepted rows of drafts: accepted [total_q] int32 (device), packed like the drafts' rows, holds in its first m_b =

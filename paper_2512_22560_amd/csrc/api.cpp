@@ -920,7 +920,9 @@ int attn_tree_mask(const int32_t* parents, const int32_t* q_lens, const int32_t*
 }
 
 namespace {
-// Workspace of attn_tree: the plan and the partials of rows that were cut.
+// Workspace of attn_tree: the plan and the partials of rows that were cut.  Its size grows with the step or stays, so that one buffer serves
+// an engine's largest step and all smaller ones: there is room for as many starts as any split of the waves has workers, and the tiles of
+// partials, 2 parts to a worker, are 4096 / along, of an `along` that shrinks as drafts grow.
 struct TreeLayout {
   int32_t parts, tiles, along, workers;
   size_t header, prefix, wstart, partial_ml, partial_o, total;
@@ -943,11 +945,12 @@ TreeLayout tree_layout(const rollattn_desc& d, int64_t max_q_len) {
     w.total = off;
     return w;
   }
-  w.workers = kNumCUs * 8 / (w.parts * w.along);       // two waves to a SIMD
+  constexpr int kWaves = kNumCUs * 8, kMostWorkers = kWaves / 2;       // two waves to a SIMD; a worker has two at least
+  w.workers = kWaves / (w.parts * w.along);
   const size_t parts = 2 * (size_t)w.workers * w.parts * kTreeTileRows;
   w.header = 0;
   w.prefix = off;      off += align256(sizeof(int32_t) * ((size_t)d.batch + 1));
-  w.wstart = off;      off += align256(sizeof(int32_t) * 4 * (size_t)w.workers);
+  w.wstart = off;      off += align256(sizeof(int32_t) * 4 * (size_t)kMostWorkers);
   w.partial_ml = off;  off += align256(sizeof(float) * 2 * parts);
   w.partial_o = off;   off += align256(sizeof(float) * d.head_dim * parts);
   w.total = off;
