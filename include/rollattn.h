@@ -329,8 +329,8 @@ size_t rollattn_tree_workspace_bytes(const rollattn_desc *desc, int32_t total_q,
  * scale' = max(scale, need), and every row of the page that is alive then, those in front of the draft included, becomes
  * enc(code * scale of its page / scale'), which leaves codes alone where neither page nor scale is another.  Every product and quotient
  * is one float32 operation: the result is defined bit for bit.  What is behind the accepted rows means nothing afterwards; pages in which
- * no row moves are left as they are.  A page written here must belong to exactly one trajectory of the batch.  max_q_len >= max n_b only
- * shapes the launch: one that understates costs speed, not correctness.  total_q == 0 succeeds without a launch.  No workspace. */
+ * no row moves are left as they are.  A page written here must belong to exactly one trajectory of the batch.  max_q_len is there as in
+ * the other calls of the step and must not be negative; nothing else depends on it.  total_q == 0 succeeds without a launch.  No workspace. */
 int kv_accept(const rollattn_desc *desc, const int32_t *accepted, const int32_t *accept_lens, const int32_t *q_lens, const int32_t *q_offsets,
               int32_t total_q, int32_t max_q_len, void *k_pages, void *v_pages, const int32_t *page_table, const int32_t *ctx_lens, float *k_scale,
               float *v_scale, void *hip_stream);

@@ -473,7 +473,8 @@ def attn_tree(q, q_lens, q_offsets, tree_mask, k_pages, v_pages, page_table, ctx
 def kv_accept(accepted, accept_lens, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, *, max_q_len, k_scale=None, v_scale=None, stream=None) -> None:
     """Moves the K and V rows of the accepted nodes of every draft together, in place: node accepted[q_offsets[b] + i], i below
     accept_lens[b], goes to place i of the draft.  accepted [total_q] int32 ascends within a trajectory.  ctx_lens includes the
-    drafts; afterwards a trajectory has ctx_lens - q_lens + accept_lens tokens.  8-bit pools get their scales updated in place."""
+    drafts; afterwards a trajectory has ctx_lens - q_lens + accept_lens tokens.  8-bit pools get their scales updated in place.
+    max_q_len is there as in the other calls of a step; nothing depends on it."""
     rc = (_host or _load_host()).kv_accept(accepted, accept_lens, q_lens, q_offsets, k_pages, v_pages, page_table, ctx_lens, max_q_len, k_scale, v_scale, _stream_of(accepted, stream))
     if rc:
         raise RollattnError(rc, "kv_accept")

@@ -1023,7 +1023,7 @@ int kv_accept(const rollattn_desc* desc, const int32_t* accepted, const int32_t*
   a.accepted = accepted; a.accept_lens = accept_lens; a.q_lens = q_lens; a.q_offsets = q_offsets; a.page_table = page_table; a.ctx_lens = ctx_lens;
   a.k_pages = k_pages; a.v_pages = v_pages; a.k_scale = k_scale; a.v_scale = v_scale;
   a.batch = desc->batch; a.hkv = desc->num_kv_heads; a.max_pages = desc->max_pages_per_seq;
-  const hipError_t e = launch_kv_accept(a, max_q_len, desc->head_dim, desc->head_dim * dtype_bytes(desc->kv_dtype), codes ? (int)kv_kind(*desc) : -1, (hipStream_t)hip_stream);
+  const hipError_t e = launch_kv_accept(a, desc->head_dim, desc->head_dim * dtype_bytes(desc->kv_dtype), codes ? (int)kv_kind(*desc) : -1, (hipStream_t)hip_stream);
   return e == hipSuccess ? ROLLATTN_OK : fail_hip(e);
 }
 

@@ -244,7 +244,7 @@ hipError_t launch_tree_mask(const TreeMaskArgs& a, int32_t max_q_len, hipStream_
   return hipGetLastError();
 }
 
-hipError_t launch_kv_accept(const AcceptArgs& a, int32_t, int head_dim, int row_bytes, int pool, hipStream_t s) {
+hipError_t launch_kv_accept(const AcceptArgs& a, int head_dim, int row_bytes, int pool, hipStream_t s) {
   const dim3 grid(a.batch, 2);
   auto go = [&](auto bytes, auto kind) {
     hipLaunchKernelGGL((kv_accept_kernel<decltype(bytes)::value, decltype(kind)::value>), grid, dim3(kThreads), 0, s, a);

@@ -280,7 +280,7 @@ hipError_t launch_tree_mfma(const TreeArgs& a, int head_dim, KvKind kv, hipStrea
 hipError_t launch_tree_f32(const TreeArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_tree_mask(const TreeMaskArgs& a, int32_t max_q_len, hipStream_t s);
 // row_bytes: of a token and KV head in the pools; pool as in launch_kv_write_rope
-hipError_t launch_kv_accept(const AcceptArgs& a, int32_t max_q_len, int head_dim, int row_bytes, int pool, hipStream_t s);
+hipError_t launch_kv_accept(const AcceptArgs& a, int head_dim, int row_bytes, int pool, hipStream_t s);
 hipError_t launch_kv_write_norm_rope(const RopeWriteArgs& a, int32_t max_q_len, int head_dim, int src_bytes, int pool, hipStream_t s);   // (with norms)
 hipError_t launch_merge_states(const void* o1, const float* d1, const void* o2, const float* d2, void* out, float* d_out,
                                long rows, int head_dim, bool f32, hipStream_t s);
