@@ -327,7 +327,7 @@ size_t rollattn_tree_workspace_bytes(const rollattn_desc *desc, int32_t total_q,
  * Pools of the source type: rows move bit for bit.  8-bit pools (k_scale, v_scale read and written as in kv_write): per page (and KV head
  * for the _HEAD types) that rows go to, need = the largest |code * scale| of the rows that come from other pages / 448 (INT8: 127),
  * scale' = max(scale, need), and every row of the page that is alive then, those in front of the draft included, becomes
- * enc(code * scale of its page / scale'), which leaves codes alone where neither page nor scale is another.  Every product and quotient
+ * enc(code * scale of its page / scale'), or keeps its codes where the scale of its page is scale' already.  Every product and quotient
  * is one float32 operation: the result is defined bit for bit.  What is behind the accepted rows means nothing afterwards; pages in which
  * no row moves are left as they are.  A page written here must belong to exactly one trajectory of the batch.  max_q_len is there as in
  * the other calls of the step and must not be negative; nothing else depends on it.  total_q == 0 succeeds without a launch.  No workspace. */

@@ -14,7 +14,8 @@ A draft is n_b nodes behind the L_b - n_b cached tokens of trajectory b; L_b cou
   accept      rows accepted[0] < accepted[1] < .. of a draft move to its places 0, 1, ..  8-bit pools, per page that a row moves into
               (and KV head where scales are per head): need = largest |code * scale of its page| among the rows that come from other
               pages / 448 or / 127; now = max(scale, need); the page's rows up to the last accepted one: enc(code * scale of its page /
-              now), each product and quotient one float32 operation
+              now), each product and quotient one float32 operation, or the codes as they are where the scale of their page is now
+              already (products with a subnormal scale would not come back as they went)
 The published method of scoring drafts as a tree and the root-mean-square norm; the paper this library serves prints nothing to check
 against.
 """
@@ -118,11 +119,11 @@ def accept(accepted, accept_lens, q_lens, ctx_lens, page_table, k_pages, v_pages
                     at = (lambda p: (p, h)) if per_head else (lambda p: p)
                     x = [(dec(c[h]) * scale[at(p)]).astype(np.float32) for (_, p, _), c in zip(came, src)]
                     amax = max([np.float32(np.max(np.abs(y))) for y, (_, p, _) in zip(x, came) if p != page], default=np.float32(0))
-                    old = scale[at(page)]
+                    old, froms = scale[at(page)], {p: scale[at(p)] for _, p, _ in came}
                     now = max(old, np.float32(amax / qmax))
                     if now > old:
                         pool[page, h, :s0] = enc(((dec(pool[page, h, :s0]) * old).astype(np.float32) / now).astype(np.float32))
-                    for (d, _, _), y in zip(came, x):
-                        pool[page, h, d] = enc((y / now).astype(np.float32))
+                    for (d, p, _), c, y in zip(came, src, x):
+                        pool[page, h, d] = c[h] if froms[p] == now else enc((y / now).astype(np.float32))
                     scale[at(page)] = now
     return pools[0], pools[1], scales[0], scales[1]
