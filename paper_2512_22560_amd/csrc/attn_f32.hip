@@ -152,7 +152,7 @@ __device__ void attend_f32(const float* const* qrows, int n_heads, const float* 
     const int h = e / D, d = e % D;
     float mmax = ml_part[0][h][0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) mmax = fmaxf(mmax, ml_part[w][h][0]);   // finite: some wave has the first token
+    for (int w = 1; w < kWaves; ++w) mmax = fmaxf(mmax, ml_part[w][h][0]);   // (All: finite, some wave has the first token)
     const float base = !kAll && mmax == -INFINITY ? 0.f : mmax;
     float o = 0.f, ls = 0.f;
 #pragma unroll

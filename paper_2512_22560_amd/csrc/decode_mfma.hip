@@ -34,6 +34,48 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
+constexpr float kWeightBits = 14.f;   // f16 weights: log2 of the largest
+
+template <int D, bool FP8>
+struct DecodeGeo : Geo<D, FP8> {
+  static constexpr int kStages = FP8 ? 4 : 2;              // blocks in flight per wave
+  static constexpr int kDT = D / 16;                       // 16-wide output tiles along D
+  static constexpr int kKK = D / 32;                       // 32-deep steps of the QK product
+};
+
+// Swizzle keys: which 16-byte column a logical chunk of token row t lands in.  K rows are
+// read 16 rows at a time (rows {0-3, 8-11, 16-19, 24-27} + 4*tile), V rows 4 or 8 at a time.
+__device__ __forceinline__ int key_k(int t) { return (t & 3) | (((t >> 3) & 3) << 2); }
+__device__ __forceinline__ int key_v16(int t) { return ((t & 3) << 1) | (((t >> 3) & 1) << 3); }
+__device__ __forceinline__ int key_v8(int t) { return t & 7; }
+
+__device__ __forceinline__ float xor16_max(float x) {
+  uintx2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float xor16_add(float x) {
+  uintx2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ floatx4 mfma(bf16x8 x, bf16x8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
+__device__ __forceinline__ floatx4 mfma(halfx8 x, halfx8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, z, 0, 0, 0); }
+
+struct Cursor {
+  int b, r, blk;   // trajectory, row within it, block within the row
+  int n, len;      // blocks in the row, context length of the trajectory
+};
+
+// 16 bytes of a K or V row.  Where every byte of a run is read once per call, by one wave (see all_read_again), it is read
+// with the streaming hint.  Over FP8 pools that keeps page scales, 32 pages' to a cache line, from being displaced (384
+// contexts: 4.73 -> 4.54 GB read); over bf16 pools as many bytes come faster.  Worth 8 to 11 % of a launch: 64 contexts of
+// 512 .. 8k (32/8/128, bf16) 154.0 -> 138.1 us with the merge, 256 long-tailed ones (64/8/128) 1440 -> 1323 us, 384 over
+// FP8 pools (64/4/128) 798 -> 713 us (6.3 TB/s, what a streaming read reaches).
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16(const unsigned char* p) {
+  typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
+  const uintx4 x = STREAM ? __builtin_nontemporal_load((const uintx4*)p) : *(const uintx4*)p;
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
 
 // One run of blocks.  WHOLE: it is one row from its first block to its last; FOLD: whose other part, in attn_decode_shared, is there
 // and folded in.  PART: it lies in one row and its result stays in LDS, un-normalised, [heads][D] in the wave's tiles and (max, sum) of
@@ -46,7 +88,7 @@ __device__ __forceinline__ void decode_worker(const DecodeArgs& a, const int4 st
   constexpr bool INT8 = KV == kKvInt8Head;
   using kx8 = std::conditional_t<INT8, halfx8, bf16x8>;   // operands of the first product
   using opx8 = std::conditional_t<HEAD, halfx8, bf16x8>;  // ... and of the second
-  using G_ = Geo<D, FP8>;
+  using G_ = DecodeGeo<D, FP8>;
   int tid = lane_id();
   asm volatile("" : "+v"(tid));   // (what is worked out from it stays in this instance: shared by both in front of the branch, it would not fit the registers)
   const int lane = tid & 63;

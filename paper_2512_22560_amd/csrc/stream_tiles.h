@@ -1,5 +1,4 @@
-// What the kernels that stream K and V rows through wave-private LDS tiles share: the tiles' layout, codes to operands, small steps
-// across lanes.
+// What the kernels that stream K and V rows through tiles in LDS share: a tile's layout, codes to operands, small steps across lanes.
 #pragma once
 
 #include <type_traits>
@@ -22,8 +21,7 @@ typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 
-constexpr float kWeightBits = 14.f;   // f16 weights: log2 of the largest,
-constexpr float kMostBits = 15.f;     // ... and the most that rounding may make of it
+constexpr float kMostBits = 15.f;     // f16 weights: log2 of the most that rounding may make of the largest
 constexpr int kQueryBits = 15;        // f16 queries: the largest is below two to this
 
 template <int D, bool FP8>
@@ -33,29 +31,12 @@ struct Geo {
   static constexpr int kRowsPerLoad = 64 / kChunks;        // token rows one wave-wide load covers
   static constexpr int kLoads = kBlockTokens / kRowsPerLoad;  // loads per block, per pool
   static constexpr int kTileBytes = kBlockTokens * kRowBytes; // LDS bytes per block, per pool
-  static constexpr int kStages = FP8 ? 4 : 2;              // blocks in flight per wave
-  static constexpr int kDT = D / 16;                       // 16-wide output tiles along D
-  static constexpr int kKK = D / 32;                       // 32-deep steps of the QK product
   static_assert(kRowsPerLoad <= 16 && 16 % kRowsPerLoad == 0, "a load must stay inside one page");
 };
 
-// Swizzle keys: which 16-byte column a logical chunk of token row t lands in.  K rows are
-// read 16 rows at a time (rows {0-3, 8-11, 16-19, 24-27} + 4*tile), V rows 4 or 8 at a time.
-__device__ __forceinline__ int key_k(int t) { return (t & 3) | (((t >> 3) & 3) << 2); }
-__device__ __forceinline__ int key_v16(int t) { return ((t & 3) << 1) | (((t >> 3) & 1) << 3); }
-__device__ __forceinline__ int key_v8(int t) { return t & 7; }
-
-__device__ __forceinline__ float xor16_max(float x) {
-  uintx2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
 __device__ __forceinline__ float xor32_max(float x) {
   uintx2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float xor16_add(float x) {
-  uintx2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ float xor32_add(float x) {
   uintx2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -96,7 +77,7 @@ __device__ __forceinline__ halfx8 int8x8_to_f16(uint32_t lo, uint32_t hi) {
   return halfx8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Eight codes as an operand of the first or second product, and the product with another.
+// Eight codes as an operand of the first or second product.
 template <int KV>
 __device__ __forceinline__ auto widen_k8(uint32_t lo, uint32_t hi) {
   if constexpr (KV == kKvInt8Head) return int8x8_to_f16(lo, hi);
@@ -108,28 +89,9 @@ __device__ __forceinline__ auto widen_v8(uint32_t lo, uint32_t hi) {
   else if constexpr (KV == kKvInt8Head) return int8x8_to_f16(lo, hi);
   else return fp8x8_to_bf16(lo, hi);
 }
-__device__ __forceinline__ floatx4 mfma(bf16x8 x, bf16x8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
-__device__ __forceinline__ floatx4 mfma(halfx8 x, halfx8 y, floatx4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, z, 0, 0, 0); }
 
 // (worked out where it is used: the thread's index would take a register over the whole of a worker's rows)
 __device__ __forceinline__ int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }
-
-struct Cursor {
-  int b, r, blk;   // trajectory, row within it, block within the row
-  int n, len;      // blocks in the row, context length of the trajectory
-};
-
-// 16 bytes of a K or V row.  Where every byte of a run is read once per call, by one wave (see all_read_again), it is read
-// with the streaming hint.  Over FP8 pools that keeps page scales, 32 pages' to a cache line, from being displaced (384
-// contexts: 4.73 -> 4.54 GB read); over bf16 pools as many bytes come faster.  Worth 8 to 11 % of a launch: 64 contexts of
-// 512 .. 8k (32/8/128, bf16) 154.0 -> 138.1 us with the merge, 256 long-tailed ones (64/8/128) 1440 -> 1323 us, 384 over
-// FP8 pools (64/4/128) 798 -> 713 us (6.3 TB/s, what a streaming read reaches).
-template <bool STREAM>
-__device__ __forceinline__ uint4 load16(const unsigned char* p) {
-  typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
-  const uintx4 x = STREAM ? __builtin_nontemporal_load((const uintx4*)p) : *(const uintx4*)p;
-  return make_uint4(x[0], x[1], x[2], x[3]);
-}
 
 }  // namespace
 

@@ -235,7 +235,7 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
   };
   auto dma16 = [&](const unsigned char* base, unsigned int off, unsigned int dst) __attribute__((always_inline)) {
     const unsigned int m0 = __builtin_amdgcn_readfirstlane(dst);
-// (streamed: read once.  The tiles of larger drafts follow each other through the same blocks, and find some in the caches: 24 drafts of 24 .. 72
+    // (streamed: read once.  The tiles of larger drafts follow each other through the same blocks, and find some in the caches: 24 drafts of 24 .. 72
     // behind 1k .. 8k (64/4/128) 167 -> 161 us over bf16, 343 -> 321 over int8 pools; of one tile, 9 .. 16, 77 -> 78 and 123 -> 124.  Hint taken from
     // the smaller ones, 64 of 6 .. 16 behind 512 .. 8k (32/8/128): 140 -> 156.)
     if constexpr (W < 8) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(m0), "v"(off), "s"(base) : "memory");
@@ -497,6 +497,8 @@ __device__ __forceinline__ TreeSums<D> tree_blocks_of(const TreeArgs& a, const D
         exponentials(std::false_type{});
       }
       l_run += HEAD ? psum[0] * ivs[0] + psum[1] * ivs[1] : psum[0] + psum[1];
+      // The weights are rounded for the second product, the sum is not: to bf16 (2^-8 of each at most) where the values have bf16's range or a
+      // scale for their page, as in the other calls over such pools, and to f16 (2^-11) where codes are exact in it.
 #pragma unroll
       for (int i = 0; i < 16; ++i) pop[i >> 3][i & 7] = (op)(FP8 && !HEAD ? p[i] * vscale[i >> 3] : p[i]);
     }
