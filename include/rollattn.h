@@ -313,8 +313,8 @@ int attn_tree_mask(const int32_t *parents, const int32_t *q_lens, const int32_t 
  * mask need not be a tree's: rows may see later nodes, or nothing at all (a row that sees no token is zero, its lse -inf).  What a row
  * does not see, undefined values included, does not reach it.  lse [total_q][Hq] float (device) as in attn_append_lse, or NULL.  Element
  * types, pools and scales as in attn_append.  Queries over INT8_HEAD pools are scaled by a power of two per row and head as there.
- * max_q_len, 1 or more where total_q is, must not understate the longest draft: rows past it would stay unwritten.  Rows behind q_offsets[B] are left as they are.
- * Requires n_b <= L_b.  workspace of at least rollattn_tree_workspace_bytes(desc, total_q, max_q_len) bytes. */
+ * max_q_len, 1 or more where total_q is, must not understate the longest draft: rows past it would stay unwritten.  Rows behind
+ * q_offsets[B] are left as they are.  Requires n_b <= L_b.  workspace of at least rollattn_tree_workspace_bytes(desc, total_q, max_q_len) bytes. */
 int attn_tree(const rollattn_desc *desc, const void *q, const int32_t *q_lens, const int32_t *q_offsets, int32_t total_q, int32_t max_q_len,
               const uint64_t *tree_mask, int32_t mask_words, const void *k_pages, const void *v_pages, const int32_t *page_table,
               const int32_t *ctx_lens, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
